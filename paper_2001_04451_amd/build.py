@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "liblsh.so")
 ARCH = os.environ.get("LSH_OFFLOAD_ARCH", "gfx950")
 
 SOURCES = ["hash.hip", "sort.hip", "attn_fwd.hip", "attn_bwd.hip", "combine.hip", "dense.hip", "block.hip",
-           "lsh_api.cpp", "block_api.cpp"]
+           "qk.hip", "cache.hip", "cache_attn.hip",
+           "lsh_api.cpp", "block_api.cpp", "qk_api.cpp", "cache_api.cpp"]
 
 COMMON_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
