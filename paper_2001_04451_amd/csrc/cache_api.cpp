@@ -35,6 +35,7 @@ int check_cache(const lsh_cache_config* c, lsh::CacheArgs* a) {
     if (c->d != lsh::kHeadDimHost || c->H > 1024 || c->n_seq >= 1 << 20) return LSH_ERR_UNSUPPORTED;
     if (c->page < 16 || c->page > 4096 || (c->page & (c->page - 1)) != 0) return LSH_ERR_UNSUPPORTED;
     if ((int64_t)c->max_pages * c->page > (int64_t)1 << 30) return LSH_ERR_UNSUPPORTED;
+    if ((int64_t)c->n_pages * c->Hkv >= ((int64_t)1 << 34) / c->page) return LSH_ERR_UNSUPPORTED;
     if (c->T >= ((int64_t)1 << 31) / c->H) return LSH_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)c->H * c->d, kv = (int64_t)c->Hkv * c->d, most = (int64_t)1 << 31;
     if (!stride_ok(c->q_stride, rows) || !stride_ok(c->k_stride, kv) || !stride_ok(c->v_stride, kv))

@@ -1,12 +1,145 @@
-// Attention of new tokens over their sequences' cached rows (lsh_cache.h).
+// Attention of new tokens over their sequences' cached rows (lsh_cache.h):
+//   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = exp2(z_ij - m_i),  z_ij = scale log2(e) q_i.k_j,
+// with the maximum m_i, the sum and the output kept in fp32 over one pass.
 //
-// One wave a (token, head): a lane takes a key, forms its logit from the
-// cached row, and the running maximum and sum of the softmax are kept in
-// fp32; then a lane takes a dimension and adds the wave's 64 weighted values.
+// gfx950 design.  The rows of a sequence and key head are its new tokens times
+// the H / Hkv query heads that share the key head.  A work item is a tile of
+// these rows and a run of keys; runs are split so that items are alike in
+// length however ragged the batch is, and a second kernel joins the parts of
+// rows that were split.  The split is made by every workgroup for itself from
+// `first` and `length` (find_item), so that nothing is planned on the host and
+// a captured call serves any lengths.
+// Both kernels form S^T = K Q^T and O^T = V^T P^T on the matrix cores with 16
+// rows of queries as the columns (mfma_f32_16x16x32_bf16), so a lane's scores
+// of four keys of two 16-key tiles are, packed to bf16, its operand of the
+// second product, and V^T comes from LDS rows by the transposing read.  Codes
+// are turned to bf16 with their block's scale on the way (exact).
+//   narrow  16 rows (decoding, a few tokens): each of four waves walks its own
+//           keys, K rows straight from memory into operand registers, V rows
+//           through an LDS area of its own; the waves are joined at the end.
+//           Bound by HBM.
+//   wide    64 QT rows (chunks): the four waves share blocks of 64 keys staged
+//           in LDS, double-buffered.  Bound by the matrix cores and exp.
+#include "attn_common.h"
 #include "cache_common.h"
 
 namespace lsh {
 namespace {
+
+constexpr int kSwz = 1;  // LDS row layout (attn_common.h): 16-row operand reads
+constexpr int kNarrowRows = 16;
+constexpr int kStep = 32;  // keys a narrow wave takes at a time
+constexpr bf16x8 kOnes8 = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
+                           (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
+constexpr float kNegInf = -__builtin_inff();
+
+// How the keys are split: rows in (lo, hi] belong to this kernel, in tiles of
+// `rows`; parts are multiples of `unit` keys, about `target` items a head.
+struct Split {
+    int rows, lo, hi, unit, target;
+};
+
+struct Item {
+    int seq, tile, part, parts, keys;  // keys a part
+    int n_rows;                        // of the sequence and head
+    int64_t first, pos0;               // row of its first new token, and that token's position
+    int slot;                          // of the partial results, where parts > 1
+};
+
+__device__ __forceinline__ int cache_cap(const CacheArgs& a) { return a.max_pages << a.page_log2; }
+
+// What a sequence brings: its rows of this kernel's kind and its cached keys.
+__device__ __forceinline__ void seq_work(const CacheArgs& a, const Split& sp, int s, int& tiles, int& keys, int& rows) {
+    tiles = keys = rows = 0;
+    if (s >= a.n_seq) return;
+    const int64_t f0 = min(max((int64_t)a.first[s], (int64_t)0), a.T);
+    const int64_t f1 = min(max((int64_t)a.first[s + 1], f0), a.T);
+    rows = (int)(f1 - f0) * (a.H / a.Hkv);
+    if (rows <= sp.lo || rows > sp.hi) return;
+    tiles = (rows + sp.rows - 1) / sp.rows;
+    keys = min(max(a.length[s], 0), cache_cap(a));
+}
+
+// Item number `item` of the split, the same for all lanes; false past the last.
+// A part has C = max(unit, keys of all tiles / target) keys, rounded up to
+// units: at most target + tiles items, at most 2 target of them in sequences
+// that are split (a tile of keys > C makes at most 2 keys / C parts).
+__device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& it) {
+    const int lane = lane_id();
+    float work = 0.f;  // the same in every workgroup: the same sums in the same order
+    int tiles, keys, rows;
+    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+        seq_work(a, sp, s0 + lane, tiles, keys, rows);
+        work += (float)tiles * (float)keys;
+    }
+    for (int o = 32; o >= 1; o >>= 1) work += __shfl_xor(work, o);
+    const float want = fminf(work * 1.0001f / (float)sp.target, 1073741824.f);
+    const int C = (max((int)want + 1, sp.unit) + sp.unit - 1) / sp.unit * sp.unit;
+    int base = 0, slots = 0;
+    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+        if (a.n_seq > 64) seq_work(a, sp, s0 + lane, tiles, keys, rows);
+        const int parts = tiles ? max(1, (int)(((uint32_t)keys + (uint32_t)C - 1u) / (uint32_t)C)) : 0;
+        const int items = tiles * parts, split = parts > 1 ? items : 0;
+        int sum = items, sum2 = split;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(sum, o), y = __shfl_up(sum2, o);
+            if (lane >= o) sum += x, sum2 += y;
+        }
+        const uint64_t mine = __ballot(item - base < sum);
+        if (mine) {
+            const int l = __builtin_ctzll(mine);
+            it.seq = s0 + l;
+            const int at = item - base - __builtin_amdgcn_readlane(sum - items, l);
+            it.parts = __builtin_amdgcn_readlane(parts, l);
+            const int back = at / it.parts;  // the last tile, whose rows see the most, first
+            it.part = at - back * it.parts;
+            it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - back;
+            it.keys = C;
+            it.n_rows = __builtin_amdgcn_readlane(rows, l);
+            it.slot = slots + __builtin_amdgcn_readlane(sum2 - split, l) + it.tile * it.parts + it.part;
+            it.first = min(max((int64_t)a.first[it.seq], (int64_t)0), a.T);
+            it.pos0 = (int64_t)a.length[it.seq] - a.first[it.seq + 1] + it.first;
+            return true;
+        }
+        base += __builtin_amdgcn_readlane(sum, 63);
+        slots += __builtin_amdgcn_readlane(sum2, 63);
+    }
+    return false;
+}
+
+// Row r of the item's sequence and head: query head within the group, token,
+// and the number of cached positions from 0 on that it may see (with shared
+// QK without its own, which counts only where there is no other).
+struct QueryRow {
+    int token, group, limit;
+};
+__device__ __forceinline__ QueryRow query_row(const CacheArgs& a, const Item& it, int r, int G, int shared) {
+    QueryRow q;
+    q.token = r / G;
+    q.group = r - q.token * G;
+    const int64_t n = it.pos0 + q.token + (shared ? 0 : 1);
+    q.limit = r < it.n_rows ? (int)min(max(n, (int64_t)0), (int64_t)cache_cap(a)) : 0;
+    return q;
+}
+
+// Tiles of 16 positions, tile0 .. tile0 + 63 of a sequence and head, one a
+// lane: the number of the 16-slot run that holds it, or -1 for none (no slot,
+// or not before position `end`).
+__device__ __forceinline__ int tile_runs(const CacheArgs& a, int seq, int head, int tile, int end) {
+    if (tile * 16 >= end) return -1;  // end <= cache_cap: the table has an entry
+    const int shift = a.page_log2 - 4;
+    const int32_t page = a.table[(int64_t)seq * a.max_pages + (tile >> shift)];
+    if (page < 0 || page >= a.n_pages) return -1;
+    return (int)((((int64_t)page * a.Hkv + head) << shift) + (tile & ((1 << shift) - 1)));
+}
+
+// Partial results of split rows, in the workspace.
+struct Parts {
+    float* o;       // [slot][Hkv][tile rows][64]: sum of weights times values
+    f32x4* stat;    // [slot][Hkv][tile rows]: maximum (log2), sum of weights, sum of the weights as rounded
+    int2* of_seq;   // [n_seq]: parts a tile, first slot
+    int slots;      // enough for any `first` that does not decrease; the rest of others is left out
+};
 
 // Value d of a cached row.
 template <CacheType TYPE>
@@ -24,69 +157,740 @@ __device__ __forceinline__ float cached(const char* base, const uint8_t* scale, 
     }
 }
 
+// Four dimensions of a finished row (d0 .. d0+3): out and, by the caller that
+// has d0 = 0, lse.  A row without keys has its own key left (shared QK), or
+// nothing.
 template <CacheType TYPE>
-__global__ __launch_bounds__(64) void cache_attn_kernel(CacheArgs a, const uint16_t* __restrict__ q,
-                                                        uint16_t* __restrict__ out, float* __restrict__ lse) {
-    __shared__ float qs[kHeadDim];
-    const int64_t t = blockIdx.x / (unsigned)a.H;
-    const int h = blockIdx.x % (unsigned)a.H, lane = threadIdx.x;
-    const int s = seq_of(a.first, a.n_seq, t);
-    if (s < 0 || t >= a.first[s + 1]) return;
-    const int hk = h / (a.H / a.Hkv);
-    qs[lane] = bf16_bits_to_f32(q[t * a.q_stride + h * kHeadDim + lane]);
-    __syncthreads();
-    const int64_t pos = (int64_t)a.length[s] - a.first[s + 1] + t;
-    float m = -__builtin_inff(), l = 0.f, o = 0.f;
-    auto logit = [&](int64_t slot) {
-        float z = 0.f;
-        for (int d = 0; d < kHeadDim; ++d) z = fmaf(qs[d], cached<TYPE>(a.k, a.k_scale, slot, d), z);
-        return z * a.scale * (a.shared ? a.k_inv[slot] : 1.f);
-    };
-    const int64_t n = min(a.shared ? pos : pos + 1, (int64_t)a.max_pages << a.page_log2);
-    for (int64_t j0 = 0; j0 < n; j0 += 64) {
-        const int64_t slot = j0 + lane < n ? slot_of(a, s, j0 + lane, hk) : -1;
-        const float z = slot >= 0 ? logit(slot) : -__builtin_inff();
-        const float m1 = fmaxf(m, wave_max(z)), off = m1 > -__builtin_inff() ? m1 : 0.f;
-        const float corr = expf(m - off), p = slot >= 0 ? expf(z - off) : 0.f;
-        o *= corr;
-        l *= corr;
-        m = m1;
-        for (int j = 0; j < 64; ++j) {
-            const int64_t sj = __shfl(slot, j);
-            const float pj = __shfl(p, j);
-            if (sj < 0) continue;
-            l += pj;
-            o = fmaf(pj, cached<TYPE>(a.v, a.v_scale, sj, lane), o);
-        }
-    }
-    float z = m + logf(l);
-    if (l == 0.f) {  // no key but the token's own, or none
-        z = -__builtin_inff();
-        const int64_t self = a.shared ? slot_of(a, s, pos, hk) : -1;
+__device__ void finish_row(const CacheArgs& a, const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
+                           float* __restrict__ lse, int64_t t, int h, int seq, int64_t pos, int d0, f32x4 o, float m,
+                           float l, float rounded) {
+    float z = (m + __log2f(l)) * kLn2;
+    if (l == 0.f) {
+        o = f32x4{};
+        z = kNegInf;
+        const int64_t self = a.shared ? slot_of(a, seq, pos, h) : -1;
         if (self >= 0) {
-            z = logit(self) - a.self_mask;
-            o = cached<TYPE>(a.v, a.v_scale, self, lane);
+            float dot = 0.f;
+            for (int d = 0; d < kHeadDim; ++d)
+                dot = fmaf(bf16_bits_to_f32(q[t * a.q_stride + h * kHeadDim + d]),
+                           cached<TYPE>(a.k, a.k_scale, self, d), dot);
+            z = dot * a.scale * a.k_inv[self] - a.self_mask;
+            for (int e = 0; e < 4; ++e) o[e] = cached<TYPE>(a.v, a.v_scale, self, d0 + e);
         }
     } else {
-        o /= l;
+        o *= 1.f / rounded;
     }
-    out[(t * a.H + h) * kHeadDim + lane] = (uint16_t)f32_to_bf16_bits(o);
-    if (lse && lane == 0) lse[t * a.H + h] = z;
+    const int64_t row = t * a.H + h;
+    *reinterpret_cast<uint2*>(out + row * kHeadDim + d0) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+    if (lse && d0 == 0) lse[row] = z;
+}
+
+// ---- rows with values that are not finite ----
+// 0 times infinity is NaN, so a key that some rows of a tile may not see must
+// not enter their products with such values.  Tiles in which rows differ in
+// what they see look their V rows over; those with a non-finite value are
+// blanked in the product and added row by row to the queries that see them.
+
+// Bit r: row r of the 32 rows at V (swizzled 128-byte rows) has a value that is not finite.
+__device__ __forceinline__ uint32_t odd_rows(const char* V) {
+    const int lane = lane_id(), row = lane & 31;
+    bool odd = false;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const u32x4 w = lds_piece<kSwz>(V, row, (lane >> 5) * 4 + p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            odd |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
+    }
+    const uint64_t b = __ballot(odd);
+    return (uint32_t)b | (uint32_t)(b >> 32);
+}
+// The operand of 32 rows' values without those of the rows in `odd`: a lane's
+// eight keys are 4 g .. 4 g + 3 of both tiles.
+__device__ __forceinline__ bf16x8 blank(bf16x8 vt, uint32_t odd, int g) {
+    u32x4 w = __builtin_bit_cast(u32x4, vt);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t two = odd >> (16 * (i >> 1) + 4 * g + 2 * (i & 1));
+        w[i] &= ((two & 1) ? 0u : 0xFFFFu) | ((two & 2) ? 0u : 0xFFFF0000u);
+    }
+    return as_bf16x8(w);
+}
+// o (dimensions 16 dt + 4 g + e of query n) += the weight of row r times its
+// values, for queries whose limit is past the row's key (key0 + r).
+__device__ __forceinline__ void add_odd_rows(const char* V, uint32_t odd, bf16x8 pk, int key0, int limit, f32x4* o) {
+    const int lane = lane_id(), n = lane & 15, g = lane >> 4;
+    const u32x4 w = __builtin_bit_cast(u32x4, pk);
+    while (odd) {
+        const int r = __builtin_ctz(odd);
+        odd &= odd - 1;
+        const uint32_t lo = (r & 16) ? w[2] : w[0], hi = (r & 16) ? w[3] : w[1];
+        uint32_t bits = (r & 2) ? hi : lo;
+        bits = (uint32_t)__shfl((int)bits, 16 * ((r >> 2) & 3) + n);
+        const float p = __uint_as_float((r & 1) ? bits & 0xFFFF0000u : bits << 16);
+        if (key0 + r >= limit) continue;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+            const uint2 v = *reinterpret_cast<const uint2*>(V + row_piece_offset<kSwz>(r, 2 * dt + (g >> 1)) + 8 * (g & 1));
+            o[dt][0] += p * __uint_as_float(v.x << 16);
+            o[dt][1] += p * __uint_as_float(v.x & 0xFFFF0000u);
+            o[dt][2] += p * __uint_as_float(v.y << 16);
+            o[dt][3] += p * __uint_as_float(v.y & 0xFFFF0000u);
+        }
+    }
+}
+
+// The compiler must not move a lane's LDS reads across other lanes' writes of the same wave.
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// ---- narrow ----
+
+// One 16-key tile as loaded: K rows in operand order (lane: row lane % 16,
+// group g = lane / 16), V rows in memory order.
+template <CacheType TYPE>
+struct RawTile {
+    static constexpr int kPieces = TYPE == kCacheBf16 ? 2 : 1;
+    u32x4 k[kPieces], v[kPieces];
+    uint32_t ks, vs;
+    f32x4 inv;
+};
+
+template <CacheType TYPE, bool SHARED>
+__device__ __forceinline__ void load_tile(const CacheArgs& a, int run, RawTile<TYPE>& r) {
+    const int lane = lane_id(), n = lane & 15, g = lane >> 4;
+    const int64_t row0 = (int64_t)run * 16;
+    const char* k = a.k + row0 * kRowBytes<TYPE>;
+    const char* v = a.v + row0 * kRowBytes<TYPE>;
+    if constexpr (TYPE == kCacheBf16) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r.k[i] = *reinterpret_cast<const u32x4*>(k + n * 128 + 64 * i + 16 * g);
+            r.v[i] = *reinterpret_cast<const u32x4*>(v + 1024 * i + 16 * lane);
+        }
+    } else {
+        if constexpr (TYPE == kCacheE4m3) {
+            r.k[0] = *reinterpret_cast<const u32x4*>(k + n * 64 + 16 * g);
+            r.v[0] = *reinterpret_cast<const u32x4*>(v + 16 * lane);
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(k + n * 32 + 8 * g);
+            const uint2 y = *reinterpret_cast<const uint2*>(v + 8 * lane);
+            r.k[0] = u32x4{x.x, x.y, 0u, 0u};
+            r.v[0] = u32x4{y.x, y.y, 0u, 0u};
+        }
+        r.ks = a.k_scale[2 * (row0 + n) + (g >> 1)];
+        r.vs = a.v_scale[2 * (row0 + (lane >> 2)) + ((lane >> 1) & 1)];
+    }
+    if constexpr (SHARED) r.inv = *reinterpret_cast<const f32x4*>(a.k_inv + row0 + 4 * g);
+}
+
+// Sixteen codes (a lane's quarter of a row) as two operands of eight bf16.
+template <CacheType TYPE>
+__device__ __forceinline__ void widen16(u32x4 c, uint32_t byte, bf16x8* x) {
+    const float s = scale_of(byte);
+    if constexpr (TYPE == kCacheE4m3) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            x[h] = as_bf16x8(u32x4{pair_to_bf16<TYPE, 0>(c[2 * h], s), pair_to_bf16<TYPE, 1>(c[2 * h], s),
+                                   pair_to_bf16<TYPE, 0>(c[2 * h + 1], s), pair_to_bf16<TYPE, 1>(c[2 * h + 1], s)});
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            x[h] = as_bf16x8(u32x4{pair_to_bf16<TYPE, 0>(c[h], s), pair_to_bf16<TYPE, 1>(c[h], s),
+                                   pair_to_bf16<TYPE, 2>(c[h], s), pair_to_bf16<TYPE, 3>(c[h], s)});
+    }
+}
+
+template <CacheType TYPE, bool SHARED>
+__global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
+                                                              const uint16_t* __restrict__ q,
+                                                              uint16_t* __restrict__ out, float* __restrict__ lse) {
+    __shared__ __attribute__((aligned(16))) char Vs[4][kStep * 128];
+    __shared__ f32x4 stats[4][kNarrowRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int G = a.H / a.Hkv, head = blockIdx.x % (unsigned)a.Hkv;
+    Item it;
+    if (!find_item(a, sp, (int)(blockIdx.x / (unsigned)a.Hkv), it)) return;
+    if (it.tile == 0 && it.part == 0 && head == 0 && tid == 0)
+        parts.of_seq[it.seq] = make_int2(it.parts, it.slot);  // slot of tile 0, part 0
+    if (it.parts > 1 && it.slot >= parts.slots) return;
+    const int r0 = it.tile * kNarrowRows;
+    const QueryRow row = query_row(a, it, r0 + n, G, SHARED);
+    const int last = min(r0 + kNarrowRows, it.n_rows) - 1;
+    const int most = query_row(a, it, last, G, SHARED).limit;  // of any row of the tile
+    const int least = query_row(a, it, r0, G, SHARED).limit;
+    const int k0 = it.part * it.keys, k1 = min(k0 + it.keys, most);
+
+    // The queries' operand: the dimensions of K's in the same order.
+    bf16x8 qop[2];
+    {
+        const QueryRow in = query_row(a, it, min(r0 + n, it.n_rows - 1), G, SHARED);
+        const uint16_t* at = q + (it.first + in.token) * a.q_stride + (head * G + in.group) * kHeadDim;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            qop[i] = as_bf16x8(*reinterpret_cast<const u32x4*>(at + (TYPE == kCacheBf16 ? 32 * i + 8 * g : 16 * g + 8 * i)));
+    }
+    const float scale_log2e = a.scale * kLog2e;
+
+    float m = kNegInf, l = 0.f;  // l: this lane's keys
+    f32x4 o[4] = {}, rounded = {};
+    const int per = ((k1 - k0 + 4 * kStep - 1) / (4 * kStep)) * kStep;  // keys a wave
+    const int w0 = k0 + wave * per, w1 = min(w0 + per, k1);
+    const int steps = w0 < w1 ? (w1 - w0 + kStep - 1) / kStep : 0;
+    char* const V = Vs[wave];
+
+    int runs = steps ? tile_runs(a, it.seq, head, w0 / 16 + lane, w1) : -1, runs_next = -1;
+    RawTile<TYPE> raw[2], next[2];
+    int run[2], run_next[2] = {-1, -1};
+    auto fetch = [&](int st) {
+        if ((st & 31) == 0 && st) runs = runs_next;
+        if ((st & 31) == 0 && st + 32 < steps) runs_next = tile_runs(a, it.seq, head, w0 / 16 + 2 * st + 64 + lane, w1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            run_next[t] = __builtin_amdgcn_readlane(runs, (2 * st + t) & 63);
+            load_tile<TYPE, SHARED>(a, max(run_next[t], 0), next[t]);
+        }
+    };
+    if (steps) fetch(0);
+    for (int st = 0; st < steps; ++st) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) raw[t] = next[t], run[t] = run_next[t];
+        if (st + 1 < steps) fetch(st + 1);
+        const int key0 = w0 + st * kStep;
+        const bool edge = key0 + kStep > least || key0 + kStep > w1 || run[0] < 0 || run[1] < 0;
+
+        wave_lds_order();  // the last step's reads of V before this step's writes
+        f32x4 z[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            bf16x8 kop[2], vv[2];
+            if constexpr (TYPE == kCacheBf16) {
+                kop[0] = as_bf16x8(raw[t].k[0]), kop[1] = as_bf16x8(raw[t].k[1]);
+            } else {
+                widen16<TYPE>(raw[t].k[0], raw[t].ks, kop);
+            }
+            z[t] = mfma16x16x32(kop[0], qop[0], f32x4{});
+            z[t] = mfma16x16x32(kop[1], qop[1], z[t]);
+            if constexpr (TYPE == kCacheBf16) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x4 x = raw[t].v[i];
+                    const int r = 8 * i + (lane >> 3);
+                    if (edge && (run[t] < 0 || key0 + 16 * t + r >= w1)) x = u32x4{};
+                    *reinterpret_cast<u32x4*>(V + row_piece_offset<kSwz>(16 * t + r, lane & 7)) = x;
+                }
+            } else {
+                const int r = lane >> 2;
+                widen16<TYPE>(raw[t].v[0], raw[t].vs, vv);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x4 x = __builtin_bit_cast(u32x4, vv[i]);
+                    if (edge && (run[t] < 0 || key0 + 16 * t + r >= w1)) x = u32x4{};
+                    *reinterpret_cast<u32x4*>(V + row_piece_offset<kSwz>(16 * t + r, 2 * (lane & 3) + i)) = x;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[t][j] *= SHARED ? scale_log2e * raw[t].inv[j] : scale_log2e;
+            if (edge) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int key = key0 + 16 * t + 4 * g + j;
+                    z[t][j] = run[t] >= 0 && key < min(row.limit, w1) ? z[t][j] : kNegInf;
+                }
+            }
+        }
+        wave_lds_order();
+        float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
+                         fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+        mt = max_xor32(max_xor16(mt));
+        if (__any(mt > m)) {
+            const float m1 = fmaxf(m, mt);
+            const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
+            l *= corr;
+            rounded *= corr;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) o[dt] *= corr;
+            m = m1;
+        }
+        const float off = m > kNegInf ? m : 0.f;
+        u32x4 pw;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                z[t][j] = __builtin_amdgcn_exp2f(z[t][j] - off);
+                l += z[t][j];
+            }
+            pw[2 * t] = pack_bf16x2(z[t][0], z[t][1]);
+            pw[2 * t + 1] = pack_bf16x2(z[t][2], z[t][3]);
+        }
+        const bf16x8 pk = as_bf16x8(pw);
+        rounded = mfma16x16x32(kOnes8, pk, rounded);
+        const uint32_t odd = edge && least != most ? odd_rows(V) : 0u;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+            bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(0, 16 * dt, lane)), vt_read(V + vt_offset<kSwz>(16, 16 * dt, lane)));
+            if (odd) vt = blank(vt, odd, g);
+            o[dt] = mfma16x16x32(vt, pk, o[dt]);
+        }
+        if (odd) add_odd_rows(V, odd, pk, key0, row.limit, o);
+    }
+    l = sum_xor32(sum_xor16(l));
+
+    // Join the four waves: thread takes row tid / 16 and four dimensions.
+    __syncthreads();
+    float* const O = reinterpret_cast<float*>(Vs[wave]);  // [row][64]
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(O + n * kHeadDim + 16 * dt + 4 * g) = o[dt];
+    if (g == 0) stats[wave][n] = f32x4{m, l, rounded[0], 0.f};
+    __syncthreads();
+    const int r = tid >> 4, d0 = 4 * (tid & 15);
+    if (r0 + r >= it.n_rows) return;
+    f32x4 st[4];
+    float top = kNegInf;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        st[w] = stats[w][r];
+        top = fmaxf(top, st[w][0]);
+    }
+    f32x4 sum = {}, stat = {top, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (st[w][1] == 0.f) continue;  // no keys there
+        const float f = __builtin_amdgcn_exp2f(st[w][0] - top);
+        sum += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(Vs[w]) + r * kHeadDim + d0);
+        stat[1] += f * st[w][1];
+        stat[2] += f * st[w][2];
+    }
+    if (it.parts > 1) {
+        const int64_t at = ((int64_t)it.slot * a.Hkv + head) * sp.rows + r;
+        *reinterpret_cast<f32x4*>(parts.o + at * kHeadDim + d0) = sum;
+        if (d0 == 0) parts.stat[at] = stat;
+        return;
+    }
+    const QueryRow mine = query_row(a, it, r0 + r, G, SHARED);
+    finish_row<TYPE>(a, q, out, lse, it.first + mine.token, head * G + mine.group, it.seq, it.pos0 + mine.token, d0, sum,
+                     stat[0], stat[1], stat[2]);
+}
+
+// ---- wide ----
+
+template <bool SHARED>
+struct WideShared {
+    char Ks[2][64 * 128];
+    char Vs[2][64 * 128];
+    float cf[2][SHARED ? 64 : 4];  // scale log2(e) k_inv
+    int hole[2][4];                // tile without slots
+};
+
+template <bool B>
+struct Tag {
+    static constexpr bool value = B;
+};
+
+template <CacheType TYPE, bool SHARED, int QT, int OCC>
+__global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split sp, Parts parts,
+                                                              const uint16_t* __restrict__ q,
+                                                              uint16_t* __restrict__ out, float* __restrict__ lse,
+                                                              int items, int sets) {
+    constexpr int kRows = 64 * QT;
+    __shared__ __attribute__((aligned(16))) WideShared<SHARED> S;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int G = a.H / a.Hkv;
+    // Each XCD keeps to its own heads (or kXcds / sets XCDs share some), whose rows its L2 then serves.
+    const int xcd = (int)(blockIdx.x % kXcds), heads = a.Hkv / sets;
+    const int64_t turn = (int64_t)(blockIdx.x / kXcds) * (kXcds / sets) + xcd / sets;
+    const int head = (int)(turn % heads) * sets + xcd % sets;
+    if (turn / heads >= items) return;
+    Item it;
+    if (!find_item(a, sp, (int)(turn / heads), it)) return;
+    if (it.tile == 0 && it.part == 0 && head == 0 && tid == 0)
+        parts.of_seq[it.seq] = make_int2(it.parts, it.slot);  // slot of tile 0, part 0
+    if (it.parts > 1 && it.slot >= parts.slots) return;
+    const int r0 = it.tile * kRows, rw = r0 + 16 * QT * wave;
+    const int most = query_row(a, it, min(r0 + kRows, it.n_rows) - 1, G, SHARED).limit;
+    const int k0 = it.part * it.keys, k1 = min(k0 + it.keys, most);
+    const bool active = rw < it.n_rows;
+    // what this wave's rows see: all of them the first `least` keys, none more than `mine`
+    const int mine = active ? query_row(a, it, min(rw + 16 * QT, it.n_rows) - 1, G, SHARED).limit : 0;
+    const int least = active ? query_row(a, it, rw, G, SHARED).limit : 0;
+    const float scale_log2e = a.scale * kLog2e;
+
+    bf16x8 qop[QT][2];
+    int limit[QT];
+    float biggest = 0.f;
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        limit[qt] = query_row(a, it, rw + 16 * qt + n, G, SHARED).limit;
+        const QueryRow in = query_row(a, it, min(rw + 16 * qt + n, it.n_rows - 1), G, SHARED);
+        const uint16_t* at = q + (it.first + in.token) * a.q_stride + (head * G + in.group) * kHeadDim;
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(at + 32 * i + 8 * g);
+            qop[qt][i] = as_bf16x8(x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float lo = __uint_as_float(x[e] << 16), hi = __uint_as_float(x[e] & 0xFFFF0000u);
+                ss = fmaf(lo, lo, fmaf(hi, hi, ss));
+            }
+        }
+        ss = sum_xor32(sum_xor16(ss));
+        biggest = fmaxf(biggest, ss);
+    }
+
+    float m[QT], l[QT];
+    f32x4 o[QT][4], rounded[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        m[qt] = kNegInf;
+        l[qt] = 0.f;
+        rounded[qt] = f32x4{};
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) o[qt][dt] = f32x4{};
+    }
+
+    // Staging: wave w brings the block's 16-key tile w.  bf16 rows are copied
+    // straight to LDS; codes go through registers, where they are widened.
+    const int blocks = k0 < k1 ? (k1 - k0 + 63) / 64 : 0;
+    int runs = blocks ? tile_runs(a, it.seq, head, k0 / 16 + 4 * lane + wave, k1) : -1, runs_next = -1;
+    u32x4 kraw{}, vraw{};
+    uint32_t ks = 0, vs = 0;
+    float inv = 0.f;
+    int run = -1;
+    const int row16 = TYPE == kCacheBf16 ? lane >> 3 : lane >> 2;  // of the tile (bf16: and that plus 8)
+    auto fetch = [&](int kb, int b) {
+        if ((kb & 63) == 0 && kb) runs = runs_next;
+        if ((kb & 63) == 0 && kb + 64 < blocks)
+            runs_next = tile_runs(a, it.seq, head, k0 / 16 + 4 * (kb + 64 + lane) + wave, k1);
+        run = __builtin_amdgcn_readlane(runs, kb & 63);
+        const int64_t row0 = (int64_t)max(run, 0) * 16;
+        if constexpr (SHARED) inv = a.k_inv[row0 + n];
+        if constexpr (TYPE == kCacheBf16) {
+            if (run >= 0) {
+                // rows at k1 and past it repeat the last one before it
+                const int here = k1 - (k0 + kb * 64 + 16 * wave);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = 8 * i + row16;
+                    const int64_t off = (row0 + min(r, here - 1)) * 128 + swz<kSwz>(16 * wave + r, lane & 7) * 16;
+                    copy16_to_lds(a.k + off, S.Ks[b] + (16 * wave + 8 * i) * 128);
+                    copy16_to_lds(a.v + off, S.Vs[b] + (16 * wave + 8 * i) * 128);
+                }
+            }
+        } else {
+            if constexpr (TYPE == kCacheE4m3) {
+                kraw = *reinterpret_cast<const u32x4*>(a.k + row0 * 64 + 16 * lane);
+                vraw = *reinterpret_cast<const u32x4*>(a.v + row0 * 64 + 16 * lane);
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(a.k + row0 * 32 + 8 * lane);
+                const uint2 y = *reinterpret_cast<const uint2*>(a.v + row0 * 32 + 8 * lane);
+                kraw = u32x4{x.x, x.y, 0u, 0u};
+                vraw = u32x4{y.x, y.y, 0u, 0u};
+            }
+            ks = a.k_scale[2 * (row0 + row16) + ((lane >> 1) & 1)];
+            vs = a.v_scale[2 * (row0 + row16) + ((lane >> 1) & 1)];
+        }
+    };
+    auto place = [&](int kb, int b) {  // what fetch(kb) brought, into buffer b
+        if (lane == 0) S.hole[b][wave] = run < 0;
+        if constexpr (SHARED)
+            if (g == 0) S.cf[b][16 * wave + n] = scale_log2e * inv;
+        if constexpr (TYPE == kCacheBf16) {
+            if (run < 0) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    *reinterpret_cast<u32x4*>(S.Ks[b] + (16 * wave + 8 * i) * 128 + 16 * lane) = u32x4{};
+                    *reinterpret_cast<u32x4*>(S.Vs[b] + (16 * wave + 8 * i) * 128 + 16 * lane) = u32x4{};
+                }
+            }
+        } else {
+            const bool gone = run < 0 || k0 + kb * 64 + 16 * wave + row16 >= k1;
+            bf16x8 kk[2], vv[2];
+            widen16<TYPE>(kraw, ks, kk);
+            widen16<TYPE>(vraw, vs, vv);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t off = row_piece_offset<kSwz>(16 * wave + row16, 2 * (lane & 3) + i);
+                *reinterpret_cast<u32x4*>(S.Ks[b] + off) = __builtin_bit_cast(u32x4, kk[i]);
+                *reinterpret_cast<u32x4*>(S.Vs[b] + off) = gone ? u32x4{} : __builtin_bit_cast(u32x4, vv[i]);
+            }
+        }
+    };
+    auto attend = [&](int b, int key0, uint32_t hole, auto fast_tag, auto edge_tag) {
+        constexpr bool FAST = decltype(fast_tag)::value, EDGE = decltype(edge_tag)::value;
+        const char* const Ks = S.Ks[b];
+        const char* const Vb = S.Vs[b];
+#pragma unroll
+        for (int kp = 0; kp < 2; ++kp) {
+            bf16x8 kop[2][2];
+            f32x4 cf[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int r = 32 * kp + 16 * t;
+                kop[t][0] = as_bf16x8(lds_piece<kSwz>(Ks, r + n, g));
+                kop[t][1] = as_bf16x8(lds_piece<kSwz>(Ks, r + n, 4 + g));
+                if constexpr (SHARED) cf[t] = *reinterpret_cast<const f32x4*>(&S.cf[b][r + 4 * g]);
+            }
+            bf16x8 pk[QT];
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+                f32x4 z[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    z[t] = mfma16x16x32(kop[t][0], qop[qt][0], f32x4{});
+                    z[t] = mfma16x16x32(kop[t][1], qop[qt][1], z[t]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        z[t][j] *= SHARED ? cf[t][j] : scale_log2e;
+                        if constexpr (EDGE) {
+                            const int key = key0 + 32 * kp + 16 * t + 4 * g + j;
+                            const bool ok = key < min(limit[qt], k1) && !(hole >> (2 * kp + t) & 1);
+                            z[t][j] = ok ? z[t][j] : kNegInf;
+                        }
+                    }
+                }
+                float off = 0.f;
+                if constexpr (!FAST) {
+                    float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
+                                     fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+                    mt = max_xor32(max_xor16(mt));
+                    if (__any(mt > m[qt])) {
+                        const float m1 = fmaxf(m[qt], mt);
+                        const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m[qt] - m1) : 1.f;
+                        l[qt] *= corr;
+                        rounded[qt] *= corr;
+#pragma unroll
+                        for (int dt = 0; dt < 4; ++dt) o[qt][dt] *= corr;
+                        m[qt] = m1;
+                    }
+                    off = m[qt] > kNegInf ? m[qt] : 0.f;
+                }
+                u32x4 pw;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) z[t][j] = __builtin_amdgcn_exp2f(z[t][j] - off);
+                    l[qt] += (z[t][0] + z[t][1]) + (z[t][2] + z[t][3]);
+                    pw[2 * t] = pack_bf16x2(z[t][0], z[t][1]);
+                    pw[2 * t + 1] = pack_bf16x2(z[t][2], z[t][3]);
+                }
+                pk[qt] = as_bf16x8(pw);
+                rounded[qt] = mfma16x16x32(kOnes8, pk[qt], rounded[qt]);
+            }
+            uint32_t odd = 0;
+            if constexpr (EDGE) odd = odd_rows(Vb + 32 * kp * 128);
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                bf16x8 vt = cat4(vt_read(Vb + vt_offset<kSwz>(32 * kp, 16 * dt, lane)),
+                                 vt_read(Vb + vt_offset<kSwz>(32 * kp + 16, 16 * dt, lane)));
+                if (EDGE && odd) vt = blank(vt, odd, g);
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mfma16x16x32(vt, pk[qt], o[qt][dt]);
+            }
+            if (EDGE && odd)
+                for (int qt = 0; qt < QT; ++qt)
+                    add_odd_rows(Vb + 32 * kp * 128, odd, pk[qt], key0 + 32 * kp, min(limit[qt], k1), o[qt]);
+        }
+    };
+
+    // No running maximum where every logit of the workgroup is within 2^-60 and
+    // 2^60 of one: normalised keys bound it by the query's length.
+    const bool fast = SHARED && __syncthreads_and(fabsf(scale_log2e) * sqrtf(biggest) <= 60.f);
+    auto walk = [&](auto fast_tag) {
+        for (int kb = 0; kb < blocks; ++kb) {
+            const int b = kb & 1, key0 = k0 + kb * 64;
+            if (kb + 1 < blocks) fetch(kb + 1, b ^ 1);
+            if (key0 < mine) {
+                const int4 none = *reinterpret_cast<const int4*>(S.hole[b]);
+                const uint32_t hole = __builtin_amdgcn_readfirstlane(none.x | none.y << 1 | none.z << 2 | none.w << 3);
+                if (key0 + 64 > least || key0 + 64 > k1 || hole)
+                    attend(b, key0, hole, fast_tag, Tag<true>{});
+                else
+                    attend(b, key0, 0u, fast_tag, Tag<false>{});
+            }
+            if (kb + 1 < blocks) place(kb + 1, b ^ 1);
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+        }
+    };
+    if (blocks) {
+        fetch(0, 0);
+        place(0, 0);
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+    }
+    if (fast)
+        walk(Tag<true>{});
+    else
+        walk(Tag<false>{});
+    if (!active) return;
+
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        const float sum = sum_xor32(sum_xor16(l[qt])), top = fast ? 0.f : m[qt];
+        const int r = 16 * QT * wave + 16 * qt + n;
+        if (r0 + r >= it.n_rows) continue;
+        if (it.parts > 1) {
+            const int64_t at = ((int64_t)it.slot * a.Hkv + head) * sp.rows + r;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
+                *reinterpret_cast<f32x4*>(parts.o + at * kHeadDim + 16 * dt + 4 * g) = o[qt][dt];
+            if (g == 0) parts.stat[at] = f32x4{top, sum, rounded[qt][0], 0.f};
+            continue;
+        }
+        const QueryRow at = query_row(a, it, r0 + r, G, SHARED);
+        const int64_t t = it.first + at.token, where = t * a.H + head * G + at.group;
+        if (sum == 0.f) {
+#pragma unroll 1
+            for (int dt = 0; dt < 4; ++dt)
+                finish_row<TYPE>(a, q, out, lse, t, head * G + at.group, it.seq, it.pos0 + at.token, 16 * dt + 4 * g,
+                                 f32x4{}, 0.f, 0.f, 0.f);
+            continue;
+        }
+        const float over = 1.f / rounded[qt][0];
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+            *reinterpret_cast<uint2*>(out + where * kHeadDim + 16 * dt + 4 * g) =
+                make_uint2(pack_bf16x2(o[qt][dt][0] * over, o[qt][dt][1] * over),
+                           pack_bf16x2(o[qt][dt][2] * over, o[qt][dt][3] * over));
+        if (lse && g == 0) lse[where] = (top + __log2f(sum)) * kLn2;
+    }
+}
+
+// ---- joining split rows ----
+
+// One wave a (token, query head): lane takes four dimensions of every fourth
+// part, in order, so the result does not depend on which part came first.
+template <CacheType TYPE>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narrow, Split wide, bool any_wide, Parts np, Parts wp,
+                                                         const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
+                                                         float* __restrict__ lse) {
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t t = item / a.H;
+    const int h = (int)(item - t * a.H), lane = lane_id(), G = a.H / a.Hkv, head = h / G;
+    if (t >= a.T) return;
+    const int s = seq_of(a.first, a.n_seq, t);
+    if (s < 0 || t >= a.first[s + 1]) return;
+    const int64_t f0 = max((int64_t)a.first[s], (int64_t)0), f1 = min((int64_t)a.first[s + 1], a.T);
+    const int rows = (int)(f1 - f0) * G;
+    const bool is_narrow = rows <= wide.lo || !any_wide;
+    const Split sp = is_narrow ? narrow : wide;
+    const Parts p = is_narrow ? np : wp;
+    const int2 of = p.of_seq[s];
+    const int r = (int)(t - f0) * G + h % G, tile = r / sp.rows;
+    if (of.x <= 1 || of.y < 0 || of.y + ((int64_t)tile + 1) * of.x > p.slots) return;
+    const int64_t at0 = ((int64_t)(of.y + tile * of.x) * a.Hkv + head) * sp.rows + r % sp.rows;
+    const int64_t step = (int64_t)a.Hkv * sp.rows;
+    const int sub = lane >> 4, d0 = 4 * (lane & 15);
+    float top = kNegInf, sum = 0.f, rounded = 0.f;
+    f32x4 o = {};
+#pragma unroll 4
+    for (int i = sub; i < of.x; i += 4) {
+        const int64_t at = at0 + i * step;
+        const f32x4 st = p.stat[at];
+        const f32x4 x = *reinterpret_cast<const f32x4*>(p.o + at * kHeadDim + d0);
+        if (st[1] == 0.f) continue;  // no keys there
+        const float m1 = fmaxf(top, st[0]);
+        const float fa = top > kNegInf ? __builtin_amdgcn_exp2f(top - m1) : 0.f, fb = __builtin_amdgcn_exp2f(st[0] - m1);
+        o = o * fa + x * fb;
+        sum = sum * fa + st[1] * fb;
+        rounded = rounded * fa + st[2] * fb;
+        top = m1;
+    }
+    const float all = max_xor32(max_xor16(top));
+    const float f = top > kNegInf ? __builtin_amdgcn_exp2f(top - all) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = sum_xor32(sum_xor16(o[e] * f));
+    sum = sum_xor32(sum_xor16(sum * f));
+    rounded = sum_xor32(sum_xor16(rounded * f));
+    if (sub == 0)
+        finish_row<TYPE>(a, q, out, lse, t, h, s, (int64_t)a.length[s] - a.first[s + 1] + t, d0, o, all, sum, rounded);
+}
+// The kernels and splits of a call.
+struct Plan {
+    bool narrow, wide, join;
+    int qt;
+    Split n, w;
+    int64_t n_items, w_items;  // a head, at most
+    size_t n_slots, w_slots, bytes;
+};
+
+Plan plan_of(const CacheArgs& a, int max_new) {
+    const int64_t G = a.H / a.Hkv, rows = a.T * G, cap = (int64_t)a.max_pages << a.page_log2;
+    const int64_t most = (max_new > 0 ? std::min<int64_t>(max_new, a.T) : a.T) * G;  // rows of a sequence, if the hint holds
+    constexpr int kAll = 0x7FFFFFFF;
+    Plan p{};
+    p.narrow = most <= kNarrowRows || a.n_seq > 1;
+    p.wide = most > kNarrowRows;
+    p.qt = most > 64 ? 4 : 1;
+    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, 4 * kStep, (2048 + a.Hkv - 1) / a.Hkv};
+    p.w = {64 * p.qt, p.narrow ? kNarrowRows : 0, kAll, 64, ((p.qt == 4 ? 512 : 768) + a.Hkv - 1) / a.Hkv};
+    const int64_t seqs = std::min<int64_t>(a.n_seq, a.T);
+    size_t off = align256((size_t)a.n_seq * sizeof(int2));
+    auto size = [&](const Split& s, int64_t tiles, int64_t& items, size_t& slots) {
+        const int64_t parts = (cap + s.unit - 1) / s.unit;  // of a tile, at most
+        items = std::min<int64_t>(s.target, tiles * (parts - 1)) + tiles;
+        slots = parts > 1 ? (size_t)std::min<int64_t>(2 * (int64_t)s.target, tiles * parts) : 0;
+        off += align256(slots * a.Hkv * s.rows * kHeadDim * sizeof(float)) + align256(slots * a.Hkv * s.rows * sizeof(f32x4));
+    };
+    if (p.narrow) size(p.n, p.wide ? seqs : rows / kNarrowRows + seqs, p.n_items, p.n_slots);
+    if (p.wide) size(p.w, rows / p.w.rows + seqs, p.w_items, p.w_slots);
+    p.join = p.n_slots + p.w_slots > 0;
+    p.bytes = off;
+    return p;
+}
+
+template <CacheType TYPE, bool SHARED>
+hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t* out, float* lse, void* workspace,
+                  hipStream_t stream) {
+    char* at = static_cast<char*>(workspace) + align256((size_t)a.n_seq * sizeof(int2));
+    auto carve = [&](size_t slots, const Split& s) {
+        Parts r;
+        r.of_seq = static_cast<int2*>(workspace);
+        r.slots = (int)slots;
+        r.o = reinterpret_cast<float*>(at);
+        at += align256(slots * a.Hkv * s.rows * kHeadDim * sizeof(float));
+        r.stat = reinterpret_cast<f32x4*>(at);
+        at += align256(slots * a.Hkv * s.rows * sizeof(f32x4));
+        return r;
+    };
+    const Parts np = carve(p.n_slots, p.n), wp = carve(p.w_slots, p.w);
+    if (p.wide) {
+        int sets = kXcds;
+        while (a.Hkv % sets != 0) sets /= 2;
+        const int64_t turns = p.w_items * (a.Hkv / sets), per = kXcds / sets;
+        const unsigned grid = (unsigned)((turns + per - 1) / per * kXcds);
+        auto go = [&](auto kernel) {
+            kernel<<<grid, 256, 0, stream>>>(a, p.w, wp, q, out, lse, (int)p.w_items, sets);
+        };
+        p.qt == 4 ? go(cache_wide_kernel<TYPE, SHARED, 4, 2>) : go(cache_wide_kernel<TYPE, SHARED, 1, 3>);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (p.narrow) {
+        cache_narrow_kernel<TYPE, SHARED><<<(unsigned)(p.n_items * a.Hkv), 256, 0, stream>>>(a, p.n, np, q, out, lse);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (p.join)
+        cache_join_kernel<TYPE><<<(unsigned)((a.T * a.H + 3) / 4), 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t cache_attn_workspace_bytes(const CacheArgs&, int) { return 256; }
+size_t cache_attn_workspace_bytes(const CacheArgs& a, int max_new) { return plan_of(a, max_new).bytes; }
 
-hipError_t launch_cache_attn(const CacheArgs& a, CacheType type, int, const uint16_t* q, uint16_t* out, float* lse,
-                             void*, hipStream_t stream) {
-    auto go = [&](auto kernel) { kernel<<<(unsigned)(a.T * a.H), 64, 0, stream>>>(a, q, out, lse); };
+hipError_t launch_cache_attn(const CacheArgs& a, CacheType type, int max_new, const uint16_t* q, uint16_t* out,
+                             float* lse, void* workspace, hipStream_t stream) {
+    const Plan p = plan_of(a, max_new);
+    auto go = [&](auto one, auto other) { return (a.shared ? one : other)(a, p, q, out, lse, workspace, stream); };
     switch (type) {
-        case kCacheBf16: go(cache_attn_kernel<kCacheBf16>); break;
-        case kCacheE4m3: go(cache_attn_kernel<kCacheE4m3>); break;
-        default: go(cache_attn_kernel<kCacheE2m1>);
+        case kCacheBf16: return go(launch<kCacheBf16, true>, launch<kCacheBf16, false>);
+        case kCacheE4m3: return go(launch<kCacheE4m3, true>, launch<kCacheE4m3, false>);
+        default: return go(launch<kCacheE2m1, true>, launch<kCacheE2m1, false>);
     }
-    return hipGetLastError();
 }
 
 }  // namespace lsh
