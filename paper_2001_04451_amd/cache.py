@@ -78,13 +78,22 @@ class CacheConfig:
     v_stride: int = 0
 
     def c(self) -> CacheConfigC:
-        scale = 1.0 / math.sqrt(self.d) if self.scale is None else self.scale
-        return CacheConfigC(self.T, self.q_stride, self.k_stride, self.v_stride, self.n_seq, self.H, self.Hkv, self.d,
-                            self.page, self.n_pages, self.max_pages, TYPES[self.type], int(bool(self.shared_qk)),
-                            self.max_new, scale, self.self_mask)
+        c = self.__dict__.get("_c")  # the configuration is frozen: one structure serves all calls
+        if c is None:
+            scale = 1.0 / math.sqrt(self.d) if self.scale is None else self.scale
+            c = CacheConfigC(self.T, self.q_stride, self.k_stride, self.v_stride, self.n_seq, self.H, self.Hkv, self.d,
+                             self.page, self.n_pages, self.max_pages, TYPES[self.type], int(bool(self.shared_qk)),
+                             self.max_new, scale, self.self_mask)
+            object.__setattr__(self, "_c", c)
+        return c
+
+    def strides(self, **own) -> "CacheConfig":
+        """This configuration with the tensors' token strides."""
+        own = {k: v for k, v in own.items() if v != getattr(self, k)}
+        return replace(self, **own) if own else self
 
 
-@dataclass
+@dataclass(frozen=True)
 class Pages:
     """The pool: k, v uint8 [n_pages, Hkv, page, row bytes], k_scale, v_scale uint8 [n_pages, Hkv, page, 2]
     (None for bf16), k_inv fp32 [n_pages, Hkv, page] (None unless shared_qk)."""
@@ -101,14 +110,13 @@ class Pages:
         def new(*more, dtype=torch.uint8):
             return torch.empty(slots + more, dtype=dtype, device=device)
 
-        p = Pages(new(ROW_BYTES[cfg.type]), new(ROW_BYTES[cfg.type]))
-        if cfg.type != "bf16":
-            p.k_scale, p.v_scale = new(2), new(2)
-        if cfg.shared_qk:
-            p.k_inv = new(dtype=torch.float32)
-        return p
+        scales = [None, None] if cfg.type == "bf16" else [new(2), new(2)]
+        return Pages(new(ROW_BYTES[cfg.type]), new(ROW_BYTES[cfg.type]), *scales,
+                     new(dtype=torch.float32) if cfg.shared_qk else None)
 
     def check(self, cfg: CacheConfig) -> None:
+        if self.__dict__.get("_checked") is cfg:  # these tensors against this configuration: once
+            return
         slots = (cfg.n_pages, cfg.Hkv, cfg.page)
         want = [("k", (ROW_BYTES[cfg.type],), torch.uint8), ("v", (ROW_BYTES[cfg.type],), torch.uint8)]
         if cfg.type != "bf16":
@@ -122,39 +130,46 @@ class Pages:
             lsh._need(t, slots + more, dtype, name)
             if t.device != self.k.device:
                 raise ValueError(f"{name} is on {t.device}, k on {self.k.device}")
+        object.__setattr__(self, "_checked", cfg)
 
     def c(self) -> CachePagesC:
         return CachePagesC(*[lsh._ptr(t) for t in (self.k, self.v, self.k_scale, self.v_scale, self.k_inv)])
 
 
-@dataclass
+@dataclass(frozen=True)
 class Sequences:
-    """first [n_seq + 1], length [n_seq], table [n_seq, max_pages], all int32 on the GPU."""
+    """first [n_seq + 1], length [n_seq], table [n_seq, max_pages], all int32 on the GPU.  What they hold may
+    change between calls."""
     first: torch.Tensor
     length: torch.Tensor
     table: torch.Tensor
 
     def check(self, cfg: CacheConfig, device) -> None:
+        if self.__dict__.get("_checked") is cfg:
+            return
         for name, shape in (("first", (cfg.n_seq + 1,)), ("length", (cfg.n_seq,)), ("table", (cfg.n_seq, cfg.max_pages))):
             t = getattr(self, name)
             lsh._need(t, shape, torch.int32, name)
             if t.device != device:
                 raise ValueError(f"{name} is on {t.device}, the pages on {device}")
+        object.__setattr__(self, "_checked", cfg)
 
     def c(self) -> CacheSeqsC:
         return CacheSeqsC(lsh._ptr(self.first), lsh._ptr(self.length), lsh._ptr(self.table))
 
 
 def _rows(t: torch.Tensor, cfg: CacheConfig, H: int, name: str, stride: int, device, dtype=None) -> int:
-    """Token stride of rows t [T, H, 64], whose heads are next to each other."""
+    """Token stride of rows t [T, H, 64], whose heads are next to each other (0: packed)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the pages on {device}")
-    if tuple(t.shape) != (cfg.T, H, cfg.d):
+    if t.shape != (cfg.T, H, cfg.d):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(cfg.T, H, cfg.d)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if stride == 0 and t.is_contiguous():
+        return 0
     if t.stride(2) != 1 or (H > 1 and t.stride(1) != cfg.d):
         raise ValueError(f"{name}'s heads must be contiguous")
     own = t.stride(0) if cfg.T > 1 else 0
@@ -177,9 +192,9 @@ def lsh_cache_write(cfg: CacheConfig, pages: Pages, seqs: Sequences, k, v) -> No
     pages.check(cfg)
     dev = pages.k.device
     seqs.check(cfg, dev)
-    cfg = replace(cfg, k_stride=_rows(k, cfg, cfg.Hkv, "k", cfg.k_stride, dev),
-                  v_stride=_rows(v, cfg, cfg.Hkv, "v", cfg.v_stride, dev, k.dtype))
-    with torch.cuda.device(dev):
+    cfg = cfg.strides(k_stride=_rows(k, cfg, cfg.Hkv, "k", cfg.k_stride, dev),
+                      v_stride=_rows(v, cfg, cfg.Hkv, "v", cfg.v_stride, dev, k.dtype))
+    with lsh.on_device(dev):
         lsh._check("lsh_cache_write",
                    lib().lsh_cache_write(ctypes.byref(cfg.c()), lsh._dtype_code(k), ctypes.byref(pages.c()),
                                          ctypes.byref(seqs.c()), lsh._ptr(k), lsh._ptr(v), lsh._stream(dev)))
@@ -193,9 +208,9 @@ def lsh_cache_read(cfg: CacheConfig, pages: Pages, seqs: Sequences, dtype: torch
     seqs.check(cfg, dev)
     k = torch.empty((cfg.T, cfg.Hkv, cfg.d), dtype=dtype, device=dev) if k is None else k
     v = torch.empty((cfg.T, cfg.Hkv, cfg.d), dtype=dtype, device=dev) if v is None else v
-    cfg = replace(cfg, k_stride=_rows(k, cfg, cfg.Hkv, "k", cfg.k_stride, dev, dtype),
-                  v_stride=_rows(v, cfg, cfg.Hkv, "v", cfg.v_stride, dev, dtype))
-    with torch.cuda.device(dev):
+    cfg = cfg.strides(k_stride=_rows(k, cfg, cfg.Hkv, "k", cfg.k_stride, dev, dtype),
+                      v_stride=_rows(v, cfg, cfg.Hkv, "v", cfg.v_stride, dev, dtype))
+    with lsh.on_device(dev):
         lsh._check("lsh_cache_read",
                    lib().lsh_cache_read(ctypes.byref(cfg.c()), lsh._dtype_code(k), ctypes.byref(pages.c()),
                                         ctypes.byref(seqs.c()), lsh._ptr(k), lsh._ptr(v), lsh._stream(dev)))
@@ -207,7 +222,7 @@ def lsh_cache_attn_fwd(cfg: CacheConfig, pages: Pages, seqs: Sequences, q, out=N
     pages.check(cfg)
     dev = pages.k.device
     seqs.check(cfg, dev)
-    cfg = replace(cfg, q_stride=_rows(q, cfg, cfg.H, "q", cfg.q_stride, dev, torch.bfloat16))
+    cfg = cfg.strides(q_stride=_rows(q, cfg, cfg.H, "q", cfg.q_stride, dev, torch.bfloat16))
     if out is None:
         out = torch.empty((cfg.T, cfg.H, cfg.d), dtype=torch.bfloat16, device=dev)
     if lse is None:
@@ -219,7 +234,7 @@ def lsh_cache_attn_fwd(cfg: CacheConfig, pages: Pages, seqs: Sequences, q, out=N
     for name, t in (("out", out), ("lse", lse), ("workspace", workspace)):
         if t.device != dev:
             raise ValueError(f"{name} is on {t.device}, the pages on {dev}")
-    with torch.cuda.device(dev):
+    with lsh.on_device(dev):
         lsh._check("lsh_cache_attn_fwd",
                    lib().lsh_cache_attn_fwd(ctypes.byref(cfg.c()), lsh.LSH_BF16, ctypes.byref(pages.c()),
                                             ctypes.byref(seqs.c()), lsh._ptr(q), lsh._ptr(out), lsh._ptr(lse),

@@ -122,6 +122,13 @@ __device__ __forceinline__ QueryRow query_row(const CacheArgs& a, const Item& it
     return q;
 }
 
+// The query of row r (of the last row, past it).
+__device__ __forceinline__ const uint16_t* query_at(const CacheArgs& a, const Item& it, const uint16_t* __restrict__ q,
+                                                    int head, int G, int r) {
+    const int rc = min(r, it.n_rows - 1), token = rc / G;
+    return q + (it.first + token) * a.q_stride + (head * G + rc - token * G) * kHeadDim;
+}
+
 // Tiles of 16 positions, tile0 .. tile0 + 63 of a sequence and head, one a
 // lane: the number of the 16-slot run that holds it, or -1 for none (no slot,
 // or not before position `end`).
@@ -185,58 +192,53 @@ __device__ void finish_row(const CacheArgs& a, const uint16_t* __restrict__ q, u
     if (lse && d0 == 0) lse[row] = z;
 }
 
-// ---- rows with values that are not finite ----
-// 0 times infinity is NaN, so a key that some rows of a tile may not see must
-// not enter their products with such values.  Tiles in which rows differ in
-// what they see look their V rows over; those with a non-finite value are
-// blanked in the product and added row by row to the queries that see them.
+// ---- values that are not finite ----
+// 0 times infinity is NaN, so such a value must not enter the products of a
+// tile in which some rows do not see its key.  There it is blanked in the
+// operand, and after the walk added to the rows that do see it: a positive
+// weight times such a value is the value, and a logit of -inf makes it NaN.
 
-// Bit r: row r of the 32 rows at V (swizzled 128-byte rows) has a value that is not finite.
-__device__ __forceinline__ uint32_t odd_rows(const char* V) {
-    const int lane = lane_id(), row = lane & 31;
-    bool odd = false;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const u32x4 w = lds_piece<kSwz>(V, row, (lane >> 5) * 4 + p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            odd |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
-    }
-    const uint64_t b = __ballot(odd);
-    return (uint32_t)b | (uint32_t)(b >> 32);
-}
-// The operand of 32 rows' values without those of the rows in `odd`: a lane's
-// eight keys are 4 g .. 4 g + 3 of both tiles.
-__device__ __forceinline__ bf16x8 blank(bf16x8 vt, uint32_t odd, int g) {
+// The operand without its non-finite values; found is set where it had one.
+__device__ __forceinline__ bf16x8 blank(bf16x8 vt, uint32_t& found) {
     u32x4 w = __builtin_bit_cast(u32x4, vt);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t two = odd >> (16 * (i >> 1) + 4 * g + 2 * (i & 1));
-        w[i] &= ((two & 1) ? 0u : 0xFFFFu) | ((two & 2) ? 0u : 0xFFFF0000u);
+        // a half's exponent is all ones: adding one to it carries into the half's top bit
+        const uint32_t odd = (((w[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15;
+        found |= odd;
+        w[i] &= ~(odd * 0xFFFFu);
     }
     return as_bf16x8(w);
 }
-// o (dimensions 16 dt + 4 g + e of query n) += the weight of row r times its
-// values, for queries whose limit is past the row's key (key0 + r).
-__device__ __forceinline__ void add_odd_rows(const char* V, uint32_t odd, bf16x8 pk, int key0, int limit, f32x4* o) {
-    const int lane = lane_id(), n = lane & 15, g = lane >> 4;
-    const u32x4 w = __builtin_bit_cast(u32x4, pk);
-    while (odd) {
-        const int r = __builtin_ctz(odd);
-        odd &= odd - 1;
-        const uint32_t lo = (r & 16) ? w[2] : w[0], hi = (r & 16) ? w[3] : w[1];
-        uint32_t bits = (r & 2) ? hi : lo;
-        bits = (uint32_t)__shfl((int)bits, 16 * ((r >> 2) & 3) + n);
-        const float p = __uint_as_float((r & 1) ? bits & 0xFFFF0000u : bits << 16);
-        if (key0 + r >= limit) continue;
+// o (dimensions 16 dt + 4 g + e of row `row`, whose query is at q) with the
+// non-finite values of the positions from .. to - 1 that it sees.
+template <CacheType TYPE>
+__device__ __forceinline__ void add_odd(const CacheArgs& a, int seq, int head, int from, int to, int limit, int g,
+                                        const uint16_t* __restrict__ q, f32x4 (&o)[4]) {
+#pragma unroll 1
+    for (int key = from; key < min(to, limit); ++key) {
+        const int64_t slot = slot_of(a, seq, key, head);
+        if (slot < 0) continue;
+        f32x4 x[4];
+        bool odd = false;
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-            const uint2 v = *reinterpret_cast<const uint2*>(V + row_piece_offset<kSwz>(r, 2 * dt + (g >> 1)) + 8 * (g & 1));
-            o[dt][0] += p * __uint_as_float(v.x << 16);
-            o[dt][1] += p * __uint_as_float(v.x & 0xFFFF0000u);
-            o[dt][2] += p * __uint_as_float(v.y << 16);
-            o[dt][3] += p * __uint_as_float(v.y & 0xFFFF0000u);
-        }
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = cached<TYPE>(a.v, a.v_scale, slot, 16 * dt + 4 * g + e);
+                const bool finite = fabsf(v) < __builtin_inff();
+                x[dt][e] = finite ? 0.f : v;
+                odd |= !finite;
+            }
+        if (!odd) continue;
+        float z = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < kHeadDim; ++d) z = fmaf(bf16_bits_to_f32(q[d]), cached<TYPE>(a.k, a.k_scale, slot, d), z);
+        const bool none = z * a.scale == kNegInf;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[dt][e] += none && x[dt][e] != 0.f ? __builtin_nanf("") : x[dt][e];
     }
 }
 
@@ -325,39 +327,35 @@ __global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split
 
     // The queries' operand: the dimensions of K's in the same order.
     bf16x8 qop[2];
-    {
-        const QueryRow in = query_row(a, it, min(r0 + n, it.n_rows - 1), G, SHARED);
-        const uint16_t* at = q + (it.first + in.token) * a.q_stride + (head * G + in.group) * kHeadDim;
+    const uint16_t* const qrow = query_at(a, it, q, head, G, r0 + n);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            qop[i] = as_bf16x8(*reinterpret_cast<const u32x4*>(at + (TYPE == kCacheBf16 ? 32 * i + 8 * g : 16 * g + 8 * i)));
-    }
+    for (int i = 0; i < 2; ++i)
+        qop[i] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + (TYPE == kCacheBf16 ? 32 * i + 8 * g : 16 * g + 8 * i)));
     const float scale_log2e = a.scale * kLog2e;
 
     float m = kNegInf, l = 0.f;  // l: this lane's keys
     f32x4 o[4] = {}, rounded = {};
+    uint32_t odd = 0;   // a non-finite value was blanked,
+    int edge0 = 0x7FFFFFFF;  // at this position or later
     const int per = ((k1 - k0 + 4 * kStep - 1) / (4 * kStep)) * kStep;  // keys a wave
     const int w0 = k0 + wave * per, w1 = min(w0 + per, k1);
     const int steps = w0 < w1 ? (w1 - w0 + kStep - 1) / kStep : 0;
     char* const V = Vs[wave];
 
     int runs = steps ? tile_runs(a, it.seq, head, w0 / 16 + lane, w1) : -1, runs_next = -1;
-    RawTile<TYPE> raw[2], next[2];
-    int run[2], run_next[2] = {-1, -1};
+    RawTile<TYPE> raw[2];
+    int run[2] = {-1, -1};
     auto fetch = [&](int st) {
         if ((st & 31) == 0 && st) runs = runs_next;
         if ((st & 31) == 0 && st + 32 < steps) runs_next = tile_runs(a, it.seq, head, w0 / 16 + 2 * st + 64 + lane, w1);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            run_next[t] = __builtin_amdgcn_readlane(runs, (2 * st + t) & 63);
-            load_tile<TYPE, SHARED>(a, max(run_next[t], 0), next[t]);
+            run[t] = __builtin_amdgcn_readlane(runs, (2 * st + t) & 63);
+            load_tile<TYPE, SHARED>(a, max(run[t], 0), raw[t]);
         }
     };
     if (steps) fetch(0);
     for (int st = 0; st < steps; ++st) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) raw[t] = next[t], run[t] = run_next[t];
-        if (st + 1 < steps) fetch(st + 1);
         const int key0 = w0 + st * kStep;
         const bool edge = key0 + kStep > least || key0 + kStep > w1 || run[0] < 0 || run[1] < 0;
 
@@ -401,6 +399,7 @@ __global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split
                 }
             }
         }
+        if (st + 1 < steps) fetch(st + 1);  // into the registers just used up
         wave_lds_order();
         float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
                          fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
@@ -428,16 +427,17 @@ __global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split
         }
         const bf16x8 pk = as_bf16x8(pw);
         rounded = mfma16x16x32(kOnes8, pk, rounded);
-        const uint32_t odd = edge && least != most ? odd_rows(V) : 0u;
+        const bool differ = edge && least != most;
+        if (differ) edge0 = min(edge0, key0);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) {
             bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(0, 16 * dt, lane)), vt_read(V + vt_offset<kSwz>(16, 16 * dt, lane)));
-            if (odd) vt = blank(vt, odd, g);
+            if (differ) vt = blank(vt, odd);
             o[dt] = mfma16x16x32(vt, pk, o[dt]);
         }
-        if (odd) add_odd_rows(V, odd, pk, key0, row.limit, o);
     }
     l = sum_xor32(sum_xor16(l));
+    if (__any(odd)) add_odd<TYPE>(a, it.seq, head, edge0, w1, row.limit, g, qrow, o);
 
     // Join the four waves: thread takes row tid / 16 and four dimensions.
     __syncthreads();
@@ -477,12 +477,15 @@ __global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split
 
 // ---- wide ----
 
-template <bool SHARED>
+template <CacheType TYPE>
 struct WideShared {
     char Ks[2][64 * 128];
     char Vs[2][64 * 128];
-    float cf[2][SHARED ? 64 : 4];  // scale log2(e) k_inv
-    int hole[2][4];                // tile without slots
+    float inv[2][4][64];  // k_inv of a tile's rows in the first 16 of each 64
+    int hole[2][4];       // tile without slots
+    // a tile's codes and scales as copied: K's and V's
+    char raw[4][TYPE == kCacheBf16 ? 16 : 2 * 16 * kRowBytes<TYPE>];
+    uint32_t scales[4][TYPE == kCacheBf16 ? 4 : 64];
 };
 
 template <bool B>
@@ -496,7 +499,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
                                                               uint16_t* __restrict__ out, float* __restrict__ lse,
                                                               int items, int sets) {
     constexpr int kRows = 64 * QT;
-    __shared__ __attribute__((aligned(16))) WideShared<SHARED> S;
+    __shared__ __attribute__((aligned(16))) WideShared<TYPE> S;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
     const int G = a.H / a.Hkv;
     // Each XCD keeps to its own heads (or kXcds / sets XCDs share some), whose rows its L2 then serves.
@@ -519,13 +522,12 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
     const float scale_log2e = a.scale * kLog2e;
 
     bf16x8 qop[QT][2];
-    int limit[QT];
+    uint32_t past = 0;  // byte qt: what row 16 qt + n of the wave sees beyond `least` (at most 63 positions)
     float biggest = 0.f;
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        limit[qt] = query_row(a, it, rw + 16 * qt + n, G, SHARED).limit;
-        const QueryRow in = query_row(a, it, min(rw + 16 * qt + n, it.n_rows - 1), G, SHARED);
-        const uint16_t* at = q + (it.first + in.token) * a.q_stride + (head * G + in.group) * kHeadDim;
+        past |= (uint32_t)max(query_row(a, it, rw + 16 * qt + n, G, SHARED).limit - least, 0) << (8 * qt);
+        const uint16_t* at = query_at(a, it, q, head, G, rw + 16 * qt + n);
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -543,6 +545,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
 
     float m[QT], l[QT];
     f32x4 o[QT][4], rounded[QT];
+    uint32_t odd = 0;  // a non-finite value was blanked
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         m[qt] = kNegInf;
@@ -552,73 +555,71 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
         for (int dt = 0; dt < 4; ++dt) o[qt][dt] = f32x4{};
     }
 
-    // Staging: wave w brings the block's 16-key tile w.  bf16 rows are copied
-    // straight to LDS; codes go through registers, where they are widened.
+    // Staging: wave w brings the block's 16-key tile w by copies to LDS, bf16
+    // rows to their places, codes to an area of the wave's own, from where they
+    // are widened once the block before is done with: nothing of it lives in
+    // registers meanwhile.
     const int blocks = k0 < k1 ? (k1 - k0 + 63) / 64 : 0;
-    int runs = blocks ? tile_runs(a, it.seq, head, k0 / 16 + 4 * lane + wave, k1) : -1, runs_next = -1;
-    u32x4 kraw{}, vraw{};
-    uint32_t ks = 0, vs = 0;
-    float inv = 0.f;
-    int run = -1;
-    const int row16 = TYPE == kCacheBf16 ? lane >> 3 : lane >> 2;  // of the tile (bf16: and that plus 8)
+    int runs = -1, run = -1;
     auto fetch = [&](int kb, int b) {
-        if ((kb & 63) == 0 && kb) runs = runs_next;
-        if ((kb & 63) == 0 && kb + 64 < blocks)
-            runs_next = tile_runs(a, it.seq, head, k0 / 16 + 4 * (kb + 64 + lane) + wave, k1);
+        if ((kb & 63) == 0) runs = tile_runs(a, it.seq, head, k0 / 16 + 4 * (kb + lane) + wave, k1);
         run = __builtin_amdgcn_readlane(runs, kb & 63);
-        const int64_t row0 = (int64_t)max(run, 0) * 16;
-        if constexpr (SHARED) inv = a.k_inv[row0 + n];
+        if (run < 0) return;
+        const int64_t row0 = (int64_t)run * 16;
+        if constexpr (SHARED) copy4_to_lds(a.k_inv + row0 + n, S.inv[b][wave]);
         if constexpr (TYPE == kCacheBf16) {
-            if (run >= 0) {
-                // rows at k1 and past it repeat the last one before it
-                const int here = k1 - (k0 + kb * 64 + 16 * wave);
+            // rows at k1 and past it repeat the last one before it
+            const int here = k1 - (k0 + kb * 64 + 16 * wave);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = 8 * i + row16;
-                    const int64_t off = (row0 + min(r, here - 1)) * 128 + swz<kSwz>(16 * wave + r, lane & 7) * 16;
-                    copy16_to_lds(a.k + off, S.Ks[b] + (16 * wave + 8 * i) * 128);
-                    copy16_to_lds(a.v + off, S.Vs[b] + (16 * wave + 8 * i) * 128);
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int r = 8 * i + (lane >> 3);
+                const int64_t off = (row0 + min(r, here - 1)) * 128 + swz<kSwz>(16 * wave + r, lane & 7) * 16;
+                copy16_to_lds(a.k + off, S.Ks[b] + (16 * wave + 8 * i) * 128);
+                copy16_to_lds(a.v + off, S.Vs[b] + (16 * wave + 8 * i) * 128);
             }
         } else {
             if constexpr (TYPE == kCacheE4m3) {
-                kraw = *reinterpret_cast<const u32x4*>(a.k + row0 * 64 + 16 * lane);
-                vraw = *reinterpret_cast<const u32x4*>(a.v + row0 * 64 + 16 * lane);
+                copy16_to_lds(a.k + row0 * 64 + 16 * lane, S.raw[wave]);
+                copy16_to_lds(a.v + row0 * 64 + 16 * lane, S.raw[wave] + 1024);
             } else {
-                const uint2 x = *reinterpret_cast<const uint2*>(a.k + row0 * 32 + 8 * lane);
-                const uint2 y = *reinterpret_cast<const uint2*>(a.v + row0 * 32 + 8 * lane);
-                kraw = u32x4{x.x, x.y, 0u, 0u};
-                vraw = u32x4{y.x, y.y, 0u, 0u};
+                copy16_to_lds((lane < 32 ? a.k : a.v) + row0 * 32 + 16 * (lane & 31), S.raw[wave]);
             }
-            ks = a.k_scale[2 * (row0 + row16) + ((lane >> 1) & 1)];
-            vs = a.v_scale[2 * (row0 + row16) + ((lane >> 1) & 1)];
+            copy4_to_lds((lane & 8 ? a.v_scale : a.k_scale) + 2 * row0 + 4 * (lane & 7), S.scales[wave]);
         }
     };
     auto place = [&](int kb, int b) {  // what fetch(kb) brought, into buffer b
         if (lane == 0) S.hole[b][wave] = run < 0;
-        if constexpr (SHARED)
-            if (g == 0) S.cf[b][16 * wave + n] = scale_log2e * inv;
-        if constexpr (TYPE == kCacheBf16) {
-            if (run < 0) {
+        if (TYPE != kCacheBf16 && run >= 0) {
+            __builtin_amdgcn_s_waitcnt(0);
+            const int r = lane >> 2;
+            const bool gone = k0 + kb * 64 + 16 * wave + r >= k1;
+            const uint8_t* scale = reinterpret_cast<const uint8_t*>(S.scales[wave]) + 2 * r + ((lane >> 1) & 1);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    *reinterpret_cast<u32x4*>(S.Ks[b] + (16 * wave + 8 * i) * 128 + 16 * lane) = u32x4{};
-                    *reinterpret_cast<u32x4*>(S.Vs[b] + (16 * wave + 8 * i) * 128 + 16 * lane) = u32x4{};
+            for (int v = 0; v < 2; ++v) {
+                u32x4 c{};
+                if constexpr (TYPE == kCacheE4m3) {
+                    c = *reinterpret_cast<const u32x4*>(S.raw[wave] + 1024 * v + 16 * lane);
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(S.raw[wave] + 512 * v + 8 * lane);
+                    c[0] = x.x, c[1] = x.y;
                 }
+                bf16x8 x[2];
+                widen16<TYPE == kCacheBf16 ? kCacheE4m3 : TYPE>(c, scale[32 * v], x);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    *reinterpret_cast<u32x4*>((v ? S.Vs[b] : S.Ks[b]) + row_piece_offset<kSwz>(16 * wave + r, 2 * (lane & 3) + i)) =
+                        v && gone ? u32x4{} : __builtin_bit_cast(u32x4, x[i]);
             }
-        } else {
-            const bool gone = run < 0 || k0 + kb * 64 + 16 * wave + row16 >= k1;
-            bf16x8 kk[2], vv[2];
-            widen16<TYPE>(kraw, ks, kk);
-            widen16<TYPE>(vraw, vs, vv);
+        }
+        if (run < 0) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t off = row_piece_offset<kSwz>(16 * wave + row16, 2 * (lane & 3) + i);
-                *reinterpret_cast<u32x4*>(S.Ks[b] + off) = __builtin_bit_cast(u32x4, kk[i]);
-                *reinterpret_cast<u32x4*>(S.Vs[b] + off) = gone ? u32x4{} : __builtin_bit_cast(u32x4, vv[i]);
+                *reinterpret_cast<u32x4*>(S.Ks[b] + (16 * wave + 8 * i) * 128 + 16 * lane) = u32x4{};
+                *reinterpret_cast<u32x4*>(S.Vs[b] + (16 * wave + 8 * i) * 128 + 16 * lane) = u32x4{};
             }
         }
     };
+
     auto attend = [&](int b, int key0, uint32_t hole, auto fast_tag, auto edge_tag) {
         constexpr bool FAST = decltype(fast_tag)::value, EDGE = decltype(edge_tag)::value;
         const char* const Ks = S.Ks[b];
@@ -632,7 +633,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
                 const int r = 32 * kp + 16 * t;
                 kop[t][0] = as_bf16x8(lds_piece<kSwz>(Ks, r + n, g));
                 kop[t][1] = as_bf16x8(lds_piece<kSwz>(Ks, r + n, 4 + g));
-                if constexpr (SHARED) cf[t] = *reinterpret_cast<const f32x4*>(&S.cf[b][r + 4 * g]);
+                if constexpr (SHARED) cf[t] = scale_log2e * *reinterpret_cast<const f32x4*>(&S.inv[b][2 * kp + t][4 * g]);
             }
             bf16x8 pk[QT];
 #pragma unroll
@@ -647,7 +648,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
                         z[t][j] *= SHARED ? cf[t][j] : scale_log2e;
                         if constexpr (EDGE) {
                             const int key = key0 + 32 * kp + 16 * t + 4 * g + j;
-                            const bool ok = key < min(limit[qt], k1) && !(hole >> (2 * kp + t) & 1);
+                            const bool ok = key < min(least + (int)(past >> (8 * qt) & 255), k1) && !(hole >> (2 * kp + t) & 1);
                             z[t][j] = ok ? z[t][j] : kNegInf;
                         }
                     }
@@ -680,58 +681,71 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
                 pk[qt] = as_bf16x8(pw);
                 rounded[qt] = mfma16x16x32(kOnes8, pk[qt], rounded[qt]);
             }
-            uint32_t odd = 0;
-            if constexpr (EDGE) odd = odd_rows(Vb + 32 * kp * 128);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 bf16x8 vt = cat4(vt_read(Vb + vt_offset<kSwz>(32 * kp, 16 * dt, lane)),
                                  vt_read(Vb + vt_offset<kSwz>(32 * kp + 16, 16 * dt, lane)));
-                if (EDGE && odd) vt = blank(vt, odd, g);
+                if constexpr (EDGE) vt = blank(vt, odd);
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mfma16x16x32(vt, pk[qt], o[qt][dt]);
             }
-            if (EDGE && odd)
-                for (int qt = 0; qt < QT; ++qt)
-                    add_odd_rows(Vb + 32 * kp * 128, odd, pk[qt], key0 + 32 * kp, min(limit[qt], k1), o[qt]);
         }
     };
 
     // No running maximum where every logit of the workgroup is within 2^-60 and
     // 2^60 of one: normalised keys bound it by the query's length.
     const bool fast = SHARED && __syncthreads_and(fabsf(scale_log2e) * sqrtf(biggest) <= 60.f);
-    auto walk = [&](auto fast_tag) {
-        for (int kb = 0; kb < blocks; ++kb) {
-            const int b = kb & 1, key0 = k0 + kb * 64;
-            if (kb + 1 < blocks) fetch(kb + 1, b ^ 1);
-            if (key0 < mine) {
-                const int4 none = *reinterpret_cast<const int4*>(S.hole[b]);
-                const uint32_t hole = __builtin_amdgcn_readfirstlane(none.x | none.y << 1 | none.z << 2 | none.w << 3);
-                if (key0 + 64 > least || key0 + 64 > k1 || hole)
-                    attend(b, key0, hole, fast_tag, Tag<true>{});
-                else
-                    attend(b, key0, 0u, fast_tag, Tag<false>{});
-            }
-            if (kb + 1 < blocks) place(kb + 1, b ^ 1);
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-        }
-    };
+    if (fast)
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) m[qt] = 0.f;
     if (blocks) {
         fetch(0, 0);
         place(0, 0);
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
     }
+    int kb = 0;
+    auto hole = [&] {
+        const int4 none = *reinterpret_cast<const int4*>(S.hole[kb & 1]);
+        return (uint32_t)__builtin_amdgcn_readfirstlane(none.x | none.y << 1 | none.z << 2 | none.w << 3);
+    };
+    auto step = [&](auto use) {
+        const int b = kb & 1;
+        if (kb + 1 < blocks) fetch(kb + 1, b ^ 1);
+        use(b, k0 + kb * 64);
+        if (kb + 1 < blocks) place(kb + 1, b ^ 1);
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        ++kb;
+    };
+    // First the blocks that all rows of the workgroup see in full, up to the
+    // first hole; then the others, whose keys are tested one by one.  Loops of
+    // their own: the choice within one cost 30 registers.
+    const int whole = min(blocks, max(query_row(a, it, r0, G, SHARED).limit - k0, 0) / 64);
+    auto walk = [&](auto fast_tag) {
+        while (kb < whole && !hole())
+            step([&](int b, int key0) {
+                if (active) attend(b, key0, 0u, fast_tag, Tag<false>{});
+            });
+    };
     if (fast)
         walk(Tag<true>{});
     else
         walk(Tag<false>{});
+    const int edge0 = k0 + kb * 64;
+    while (kb < blocks)
+        step([&](int b, int key0) {
+            if (key0 < mine) attend(b, key0, hole(), Tag<false>{}, Tag<true>{});
+        });
     if (!active) return;
 
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        const float sum = sum_xor32(sum_xor16(l[qt])), top = fast ? 0.f : m[qt];
+        const float sum = sum_xor32(sum_xor16(l[qt])), top = m[qt];
         const int r = 16 * QT * wave + 16 * qt + n;
+        if (__any(odd))
+            add_odd<TYPE>(a, it.seq, head, edge0, k1, least + (int)(past >> (8 * qt) & 255), g,
+                          query_at(a, it, q, head, G, rw + 16 * qt + n), o[qt]);
         if (r0 + r >= it.n_rows) continue;
         if (it.parts > 1) {
             const int64_t at = ((int64_t)it.slot * a.Hkv + head) * sp.rows + r;

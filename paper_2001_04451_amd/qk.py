@@ -56,6 +56,13 @@ class QkConfig:
     dx_stride: int = 0
 
     def c(self) -> QkConfigC:
+        c = self.__dict__.get("_c")  # the configuration is frozen: one structure serves all calls
+        if c is None:
+            c = self._make()
+            object.__setattr__(self, "_c", c)
+        return c
+
+    def _make(self) -> QkConfigC:
         return QkConfigC(self.T, self.L, self.x_stride, self.dx_stride, self.Hq, self.Hk, self.d, self.rot,
                          int(bool(self.interleaved)), int(bool(self.gain_per_head)), self.eps)
 
@@ -71,11 +78,13 @@ def qk_workspace_bytes(cfg: QkConfig) -> int:
 
 
 def _token_rows(t: torch.Tensor, T: int, width: int, name: str, stride: int) -> int:
-    """Stride between the rows of t, which holds T rows of at least `width` elements."""
+    """Stride between the rows of t, which holds T rows of at least `width` elements (0: packed)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dim() != 2 or t.shape[0] != T or t.shape[1] < width:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({T}, {width} or more)")
+    if stride == 0 and t.shape[1] == width and t.is_contiguous():
+        return 0
     if t.stride(1) != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
     own = t.stride(0) if T > 1 else 0
@@ -85,7 +94,9 @@ def _token_rows(t: torch.Tensor, T: int, width: int, name: str, stride: int) -> 
 
 
 def _check_inputs(cfg: QkConfig, x, gain_q, gain_k, freq, pos) -> QkConfig:
-    cfg = replace(cfg, x_stride=_token_rows(x, cfg.T, (cfg.Hq + cfg.Hk) * cfg.d, "x", cfg.x_stride))
+    stride = _token_rows(x, cfg.T, (cfg.Hq + cfg.Hk) * cfg.d, "x", cfg.x_stride)
+    if stride != cfg.x_stride:
+        cfg = replace(cfg, x_stride=stride)
     lsh._need(gain_q, cfg.gain_shape(cfg.Hq), torch.float32, "gain_q")
     if cfg.Hk:
         if gain_k is None:
@@ -115,7 +126,7 @@ def lsh_qk_norm_rotate_fwd(cfg: QkConfig, x, gain_q, gain_k, freq, pos=None, q=N
     q = _out(q, cfg.out_shape(cfg.Hq), x.dtype, x, "q")
     k = _out(k, cfg.out_shape(cfg.Hk), x.dtype, x, "k") if cfg.Hk else None
     p = lsh._ptr
-    with torch.cuda.device(x.device):
+    with lsh.on_device(x.device):
         lsh._check("lsh_qk_norm_rotate_fwd",
                    lib().lsh_qk_norm_rotate_fwd(ctypes.byref(cfg.c()), lsh._dtype_code(x), p(x), p(gain_q), p(gain_k),
                                                 p(freq), p(pos), p(q), p(k), lsh._stream(x.device)))
@@ -137,13 +148,15 @@ def lsh_qk_norm_rotate_bwd(cfg: QkConfig, x, gain_q, gain_k, freq, pos, dq, dk=N
         dx = torch.empty((cfg.T, width), dtype=torch.float32, device=x.device)
     if dx.dtype != torch.float32 or dx.device != x.device:
         raise ValueError(f"dx must be float32 on {x.device}")
-    cfg = replace(cfg, dx_stride=_token_rows(dx, cfg.T, width, "dx", cfg.dx_stride))
+    stride = _token_rows(dx, cfg.T, width, "dx", cfg.dx_stride)
+    if stride != cfg.dx_stride:
+        cfg = replace(cfg, dx_stride=stride)
     dgain_q = _out(dgain_q, cfg.gain_shape(cfg.Hq), torch.float32, x, "dgain_q")
     dgain_k = _out(dgain_k, cfg.gain_shape(cfg.Hk), torch.float32, x, "dgain_k") if cfg.Hk else None
     if workspace is None:
         workspace = torch.empty(max(qk_workspace_bytes(cfg), 256), dtype=torch.uint8, device=x.device)
     p = lsh._ptr
-    with torch.cuda.device(x.device):
+    with lsh.on_device(x.device):
         lsh._check("lsh_qk_norm_rotate_bwd",
                    lib().lsh_qk_norm_rotate_bwd(ctypes.byref(cfg.c()), lsh._dtype_code(x), p(x), p(gain_q), p(gain_k),
                                                 p(freq), p(pos), p(dq), p(dk), p(dx), p(dgain_q), p(dgain_k),
