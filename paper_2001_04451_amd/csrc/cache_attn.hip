@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kSwz = 1;  // LDS row layout (attn_common.h): 16-row operand reads
 constexpr int kNarrowRows = 16;
-constexpr int kStep = 32;  // keys a narrow wave takes at a time
+constexpr int kNarrowUnit = 256;  // keys a part is a multiple of: 64 a wave
 constexpr bf16x8 kOnes8 = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
                            (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
 constexpr float kNegInf = -__builtin_inff();
@@ -60,6 +60,22 @@ __device__ __forceinline__ void seq_work(const CacheArgs& a, const Split& sp, in
     keys = min(max(a.length[s], 0), cache_cap(a));
 }
 
+// Sums over lanes 0 .. own, by moves within rows of sixteen and then from row
+// to row (no LDS round trips).
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1, 2, 4, 8 lanes below in the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // last lane of row 0 into row 1, 2 into 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31 into rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {  // the same in every lane
+    x = group8_sum(x);
+    return sum_xor32(sum_xor16(x + dpp_f32<kDppMirror>(x)));
+}
+
 // Item number `item` of the split, the same for all lanes; false past the last.
 // A part has C = max(unit, keys of all tiles / target) keys, rounded up to
 // units: at most target + tiles items, at most 2 target of them in sequences
@@ -72,7 +88,7 @@ __device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& i
         seq_work(a, sp, s0 + lane, tiles, keys, rows);
         work += (float)tiles * (float)keys;
     }
-    for (int o = 32; o >= 1; o >>= 1) work += __shfl_xor(work, o);
+    work = wave_sum(work);
     const float want = fminf(work * 1.0001f / (float)sp.target, 1073741824.f);
     const int C = (max((int)want + 1, sp.unit) + sp.unit - 1) / sp.unit * sp.unit;
     int base = 0, slots = 0;
@@ -80,11 +96,7 @@ __device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& i
         if (a.n_seq > 64) seq_work(a, sp, s0 + lane, tiles, keys, rows);
         const int parts = tiles ? max(1, (int)(((uint32_t)keys + (uint32_t)C - 1u) / (uint32_t)C)) : 0;
         const int items = tiles * parts, split = parts > 1 ? items : 0;
-        int sum = items, sum2 = split;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(sum, o), y = __shfl_up(sum2, o);
-            if (lane >= o) sum += x, sum2 += y;
-        }
+        const int sum = wave_scan(items), sum2 = wave_scan(split);
         const uint64_t mine = __ballot(item - base < sum);
         if (mine) {
             const int l = __builtin_ctzll(mine);
@@ -248,7 +260,19 @@ __device__ __forceinline__ void wave_lds_order() {
     __builtin_amdgcn_wave_barrier();
 }
 
+template <bool B>
+struct Tag {
+    static constexpr bool value = B;
+};
+
+
 // ---- narrow ----
+
+// 16-key tiles that a wave takes a step (its loads under way), and workgroups a CU.
+template <CacheType TYPE>
+constexpr int kTiles = 2;
+template <CacheType TYPE>
+constexpr int kNarrowOcc = 3;
 
 // One 16-key tile as loaded: K rows in operand order (lane: row lane % 16,
 // group g = lane / 16), V rows in memory order.
@@ -257,10 +281,9 @@ struct RawTile {
     static constexpr int kPieces = TYPE == kCacheBf16 ? 2 : 1;
     u32x4 k[kPieces], v[kPieces];
     uint32_t ks, vs;
-    f32x4 inv;
 };
 
-template <CacheType TYPE, bool SHARED>
+template <CacheType TYPE>
 __device__ __forceinline__ void load_tile(const CacheArgs& a, int run, RawTile<TYPE>& r) {
     const int lane = lane_id(), n = lane & 15, g = lane >> 4;
     const int64_t row0 = (int64_t)run * 16;
@@ -285,7 +308,6 @@ __device__ __forceinline__ void load_tile(const CacheArgs& a, int run, RawTile<T
         r.ks = a.k_scale[2 * (row0 + n) + (g >> 1)];
         r.vs = a.v_scale[2 * (row0 + (lane >> 2)) + ((lane >> 1) & 1)];
     }
-    if constexpr (SHARED) r.inv = *reinterpret_cast<const f32x4*>(a.k_inv + row0 + 4 * g);
 }
 
 // Sixteen codes (a lane's quarter of a row) as two operands of eight bf16.
@@ -306,10 +328,12 @@ __device__ __forceinline__ void widen16(u32x4 c, uint32_t byte, bf16x8* x) {
 }
 
 template <CacheType TYPE, bool SHARED>
-__global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
+__global__ __launch_bounds__(256, kNarrowOcc<TYPE>) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
                                                               const uint16_t* __restrict__ q,
                                                               uint16_t* __restrict__ out, float* __restrict__ lse) {
+    constexpr int NT = kTiles<TYPE>, kStep = 16 * NT;
     __shared__ __attribute__((aligned(16))) char Vs[4][kStep * 128];
+    __shared__ __attribute__((aligned(16))) float invs[4][kStep];  // k_inv of the step's keys
     __shared__ f32x4 stats[4][kNarrowRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
     const int G = a.H / a.Hkv, head = blockIdx.x % (unsigned)a.Hkv;
@@ -326,116 +350,161 @@ __global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split
     const int k0 = it.part * it.keys, k1 = min(k0 + it.keys, most);
 
     // The queries' operand: the dimensions of K's in the same order.
+    // A negative scale turns the queries round, which is exact, so that the
+    // largest logit is the largest product.
     bf16x8 qop[2];
     const uint16_t* const qrow = query_at(a, it, q, head, G, r0 + n);
+    float qq = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        qop[i] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + (TYPE == kCacheBf16 ? 32 * i + 8 * g : 16 * g + 8 * i)));
-    const float scale_log2e = a.scale * kLog2e;
+    for (int i = 0; i < 2; ++i) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(qrow + (TYPE == kCacheBf16 ? 32 * i + 8 * g : 16 * g + 8 * i));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (a.scale < 0.f) x[e] ^= 0x80008000u;
+            const float lo = __uint_as_float(x[e] << 16), hi = __uint_as_float(x[e] & 0xFFFF0000u);
+            qq = fmaf(lo, lo, fmaf(hi, hi, qq));
+        }
+        qop[i] = as_bf16x8(x);
+    }
+    const float scale_log2e = fabsf(a.scale) * kLog2e;
+    // No running maximum where normalised keys keep every logit within 2^-60 and 2^60 of one.
+    const bool fast = SHARED && __all(scale_log2e * sqrtf(sum_xor32(sum_xor16(qq))) <= 60.f);
 
-    float m = kNegInf, l = 0.f;  // l: this lane's keys
+    float m = fast ? 0.f : kNegInf, l = 0.f;  // l: this lane's keys
     f32x4 o[4] = {}, rounded = {};
-    uint32_t odd = 0;   // a non-finite value was blanked,
-    int edge0 = 0x7FFFFFFF;  // at this position or later
+    uint32_t odd = 0;            // a non-finite value was blanked,
+    int edge0 = 0x7FFFFFFF;      // at this position or later
     const int per = ((k1 - k0 + 4 * kStep - 1) / (4 * kStep)) * kStep;  // keys a wave
     const int w0 = k0 + wave * per, w1 = min(w0 + per, k1);
     const int steps = w0 < w1 ? (w1 - w0 + kStep - 1) / kStep : 0;
     char* const V = Vs[wave];
 
+    constexpr int kRun = 64 / NT;  // steps that the runs of a wave's lanes last
     int runs = steps ? tile_runs(a, it.seq, head, w0 / 16 + lane, w1) : -1, runs_next = -1;
-    RawTile<TYPE> raw[2];
-    int run[2] = {-1, -1};
+    RawTile<TYPE> raw[NT];
+    float inv = 0.f;    // k_inv of key `lane` of the step
+    uint32_t gone = 0;  // bit t: tile t of the step has no slots
     auto fetch = [&](int st) {
-        if ((st & 31) == 0 && st) runs = runs_next;
-        if ((st & 31) == 0 && st + 32 < steps) runs_next = tile_runs(a, it.seq, head, w0 / 16 + 2 * st + 64 + lane, w1);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            run[t] = __builtin_amdgcn_readlane(runs, (2 * st + t) & 63);
-            load_tile<TYPE, SHARED>(a, max(run[t], 0), raw[t]);
+        if (st % kRun == 0) {
+            if (st) runs = runs_next;
+            if (st + kRun < steps) runs_next = tile_runs(a, it.seq, head, w0 / 16 + NT * (st + kRun) + lane, w1);
         }
-    };
-    if (steps) fetch(0);
-    for (int st = 0; st < steps; ++st) {
-        const int key0 = w0 + st * kStep;
-        const bool edge = key0 + kStep > least || key0 + kStep > w1 || run[0] < 0 || run[1] < 0;
-
-        wave_lds_order();  // the last step's reads of V before this step's writes
-        f32x4 z[2];
+        gone = 0;
+        int mine = 0;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bf16x8 kop[2], vv[2];
+        for (int t = 0; t < NT; ++t) {
+            const int run = __builtin_amdgcn_readlane(runs, (NT * st + t) & 63);
+            gone |= run < 0 ? 1u << t : 0u;
+            load_tile<TYPE>(a, max(run, 0), raw[t]);
+            if (t == 0 || lane >= 16 * t) mine = max(run, 0);
+        }
+        if constexpr (SHARED) inv = a.k_inv[(int64_t)mine * 16 + n];
+    };
+    int st = 0;
+    // EDGE: keys of the step may be hidden from some or all rows.
+    auto step = [&](auto fast_tag, auto edge_tag) {
+        constexpr bool FAST = decltype(fast_tag)::value, EDGE = decltype(edge_tag)::value;
+        const int key0 = w0 + st * kStep;
+        const bool differ = EDGE && least != most;
+        if (differ) edge0 = min(edge0, key0);
+        wave_lds_order();  // the last step's reads of V before this step's writes
+        f32x4 z[NT];
+        if (SHARED && lane < kStep) invs[wave][lane] = scale_log2e * inv;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            bf16x8 kop[2];
+            u32x4 vrow[2];
             if constexpr (TYPE == kCacheBf16) {
-                kop[0] = as_bf16x8(raw[t].k[0]), kop[1] = as_bf16x8(raw[t].k[1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) kop[i] = as_bf16x8(raw[t].k[i]), vrow[i] = raw[t].v[i];
             } else {
+                bf16x8 x[2];
                 widen16<TYPE>(raw[t].k[0], raw[t].ks, kop);
+                widen16<TYPE>(raw[t].v[0], raw[t].vs, x);
+                vrow[0] = __builtin_bit_cast(u32x4, x[0]), vrow[1] = __builtin_bit_cast(u32x4, x[1]);
             }
             z[t] = mfma16x16x32(kop[0], qop[0], f32x4{});
             z[t] = mfma16x16x32(kop[1], qop[1], z[t]);
-            if constexpr (TYPE == kCacheBf16) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    u32x4 x = raw[t].v[i];
-                    const int r = 8 * i + (lane >> 3);
-                    if (edge && (run[t] < 0 || key0 + 16 * t + r >= w1)) x = u32x4{};
-                    *reinterpret_cast<u32x4*>(V + row_piece_offset<kSwz>(16 * t + r, lane & 7)) = x;
-                }
-            } else {
-                const int r = lane >> 2;
-                widen16<TYPE>(raw[t].v[0], raw[t].vs, vv);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    u32x4 x = __builtin_bit_cast(u32x4, vv[i]);
-                    if (edge && (run[t] < 0 || key0 + 16 * t + r >= w1)) x = u32x4{};
-                    *reinterpret_cast<u32x4*>(V + row_piece_offset<kSwz>(16 * t + r, 2 * (lane & 3) + i)) = x;
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int r = TYPE == kCacheBf16 ? 8 * i + (lane >> 3) : lane >> 2;
+                const int piece = TYPE == kCacheBf16 ? lane & 7 : 2 * (lane & 3) + i;
+                if (EDGE && ((gone >> t & 1) || key0 + 16 * t + r >= w1)) vrow[i] = u32x4{};
+                *reinterpret_cast<u32x4*>(V + row_piece_offset<kSwz>(16 * t + r, piece)) = vrow[i];
             }
+        }
+        const uint32_t hidden = gone;
+        if (st + 1 < steps) fetch(st + 1);  // into the registers just used up
+        wave_lds_order();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) z[t][j] *= SHARED ? scale_log2e * raw[t].inv[j] : scale_log2e;
-            if (edge) {
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (SHARED) z[t] *= *reinterpret_cast<const f32x4*>(&invs[wave][16 * t + 4 * g]);
+            if constexpr (EDGE)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int key = key0 + 16 * t + 4 * g + j;
-                    z[t][j] = run[t] >= 0 && key < min(row.limit, w1) ? z[t][j] : kNegInf;
+                    z[t][j] = !(hidden >> t & 1) && key < min(row.limit, w1) ? z[t][j] : kNegInf;
                 }
+        }
+        const float c = SHARED ? 1.f : scale_log2e;  // what z still lacks
+        float off = 0.f;
+        if constexpr (!FAST) {
+            float mt = kNegInf;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                mt = fmaxf(fmaxf(mt, fmaxf(z[t][0], z[t][1])), fmaxf(z[t][2], z[t][3]));
+            mt = max_xor32(max_xor16(mt));
+            if constexpr (!SHARED) mt = mt > kNegInf ? mt * c : mt;
+            if (__any(mt > m)) {
+                const float m1 = fmaxf(m, mt);
+                const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
+                l *= corr;
+                rounded *= corr;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) o[dt] *= corr;
+                m = m1;
+            }
+            off = m > kNegInf ? m : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+            u32x4 pw;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f32x4& p = z[t + i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (EDGE && !SHARED)  // the scale of 0 leaves a hidden key hidden
+                        p[j] = p[j] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(p[j], c, -off));
+                    else
+                        p[j] = __builtin_amdgcn_exp2f(SHARED ? p[j] - off : fmaf(p[j], c, -off));
+                }
+                l += (p[0] + p[1]) + (p[2] + p[3]);
+                pw[2 * i] = pack_bf16x2(p[0], p[1]);
+                pw[2 * i + 1] = pack_bf16x2(p[2], p[3]);
+            }
+            const bf16x8 pk = as_bf16x8(pw);
+            rounded = mfma16x16x32(kOnes8, pk, rounded);
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(16 * t, 16 * dt, lane)),
+                                 vt_read(V + vt_offset<kSwz>(16 * t + 16, 16 * dt, lane)));
+                if (EDGE && differ) vt = blank(vt, odd);
+                o[dt] = mfma16x16x32(vt, pk, o[dt]);
             }
         }
-        if (st + 1 < steps) fetch(st + 1);  // into the registers just used up
-        wave_lds_order();
-        float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
-                         fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-        mt = max_xor32(max_xor16(mt));
-        if (__any(mt > m)) {
-            const float m1 = fmaxf(m, mt);
-            const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
-            l *= corr;
-            rounded *= corr;
-#pragma unroll
-            for (int dt = 0; dt < 4; ++dt) o[dt] *= corr;
-            m = m1;
-        }
-        const float off = m > kNegInf ? m : 0.f;
-        u32x4 pw;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[t][j] = __builtin_amdgcn_exp2f(z[t][j] - off);
-                l += z[t][j];
-            }
-            pw[2 * t] = pack_bf16x2(z[t][0], z[t][1]);
-            pw[2 * t + 1] = pack_bf16x2(z[t][2], z[t][3]);
-        }
-        const bf16x8 pk = as_bf16x8(pw);
-        rounded = mfma16x16x32(kOnes8, pk, rounded);
-        const bool differ = edge && least != most;
-        if (differ) edge0 = min(edge0, key0);
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-            bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(0, 16 * dt, lane)), vt_read(V + vt_offset<kSwz>(16, 16 * dt, lane)));
-            if (differ) vt = blank(vt, odd);
-            o[dt] = mfma16x16x32(vt, pk, o[dt]);
-        }
-    }
+        ++st;
+    };
+    if (steps) fetch(0);
+    const int whole = max(min(least, w1) - w0, 0) / kStep;
+    auto walk = [&](auto fast_tag) {
+        while (st < whole && !gone) step(fast_tag, Tag<false>{});
+    };
+    if (fast)
+        walk(Tag<true>{});
+    else
+        walk(Tag<false>{});
+    while (st < steps) step(Tag<false>{}, Tag<true>{});
     l = sum_xor32(sum_xor16(l));
     if (__any(odd)) add_odd<TYPE>(a, it.seq, head, edge0, w1, row.limit, g, qrow, o);
 
@@ -448,21 +517,21 @@ __global__ __launch_bounds__(256, 4) void cache_narrow_kernel(CacheArgs a, Split
     __syncthreads();
     const int r = tid >> 4, d0 = 4 * (tid & 15);
     if (r0 + r >= it.n_rows) return;
-    f32x4 st[4];
+    f32x4 ws[4];
     float top = kNegInf;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        st[w] = stats[w][r];
-        top = fmaxf(top, st[w][0]);
+        ws[w] = stats[w][r];
+        if (ws[w][1] != 0.f) top = fmaxf(top, ws[w][0]);
     }
     f32x4 sum = {}, stat = {top, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        if (st[w][1] == 0.f) continue;  // no keys there
-        const float f = __builtin_amdgcn_exp2f(st[w][0] - top);
+        if (ws[w][1] == 0.f) continue;  // no keys there
+        const float f = __builtin_amdgcn_exp2f(ws[w][0] - top);
         sum += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(Vs[w]) + r * kHeadDim + d0);
-        stat[1] += f * st[w][1];
-        stat[2] += f * st[w][2];
+        stat[1] += f * ws[w][1];
+        stat[2] += f * ws[w][2];
     }
     if (it.parts > 1) {
         const int64_t at = ((int64_t)it.slot * a.Hkv + head) * sp.rows + r;
@@ -486,11 +555,6 @@ struct WideShared {
     // a tile's codes and scales as copied: K's and V's
     char raw[4][TYPE == kCacheBf16 ? 16 : 2 * 16 * kRowBytes<TYPE>];
     uint32_t scales[4][TYPE == kCacheBf16 ? 4 : 64];
-};
-
-template <bool B>
-struct Tag {
-    static constexpr bool value = B;
 };
 
 template <CacheType TYPE, bool SHARED, int QT, int OCC>
@@ -776,15 +840,20 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
 
 // ---- joining split rows ----
 
-// One wave a (token, query head): lane takes four dimensions of every fourth
-// part, in order, so the result does not depend on which part came first.
-template <CacheType TYPE>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narrow, Split wide, bool any_wide, Parts np, Parts wp,
-                                                         const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
-                                                         float* __restrict__ lse) {
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+// W waves a (token, query head): a lane takes four dimensions of every 4 W-th
+// part, and the lanes are added in a fixed order, so the result does not
+// depend on which part came first.
+template <CacheType TYPE, int W>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narrow, Split wide, bool any_wide, Parts np,
+                                                         Parts wp, const uint16_t* __restrict__ q,
+                                                         uint16_t* __restrict__ out, float* __restrict__ lse) {
+    __shared__ f32x4 sums[4][16];
+    __shared__ f32x4 stats[4];
+    const int wave = threadIdx.x >> 6, lane = lane_id();
+    const int64_t item = (int64_t)blockIdx.x * (4 / W) + wave / W;
     const int64_t t = item / a.H;
-    const int h = (int)(item - t * a.H), lane = lane_id(), G = a.H / a.Hkv, head = h / G;
+    const int h = (int)(item - t * a.H), G = a.H / a.Hkv, head = h / G;
+    // with W = 4 the whole workgroup leaves
     if (t >= a.T) return;
     const int s = seq_of(a.first, a.n_seq, t);
     if (s < 0 || t >= a.first[s + 1]) return;
@@ -798,31 +867,48 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narr
     if (of.x <= 1 || of.y < 0 || of.y + ((int64_t)tile + 1) * of.x > p.slots) return;
     const int64_t at0 = ((int64_t)(of.y + tile * of.x) * a.Hkv + head) * sp.rows + r % sp.rows;
     const int64_t step = (int64_t)a.Hkv * sp.rows;
-    const int sub = lane >> 4, d0 = 4 * (lane & 15);
-    float top = kNegInf, sum = 0.f, rounded = 0.f;
-    f32x4 o = {};
-#pragma unroll 4
-    for (int i = sub; i < of.x; i += 4) {
-        const int64_t at = at0 + i * step;
-        const f32x4 st = p.stat[at];
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p.o + at * kHeadDim + d0);
-        if (st[1] == 0.f) continue;  // no keys there
-        const float m1 = fmaxf(top, st[0]);
-        const float fa = top > kNegInf ? __builtin_amdgcn_exp2f(top - m1) : 0.f, fb = __builtin_amdgcn_exp2f(st[0] - m1);
-        o = o * fa + x * fb;
-        sum = sum * fa + st[1] * fb;
-        rounded = rounded * fa + st[2] * fb;
-        top = m1;
+    const int d0 = 4 * (lane & 15);
+    f32x4 stat = {kNegInf, 0.f, 0.f, 0.f}, o = {};
+    auto add = [&](f32x4 st, f32x4 x) {
+        const bool some = st[1] != 0.f;  // keys there (x is not written otherwise)
+        const float m1 = some ? fmaxf(stat[0], st[0]) : stat[0];
+        const float fa = stat[1] != 0.f ? __builtin_amdgcn_exp2f(stat[0] - m1) : 0.f;
+        const float fb = some ? __builtin_amdgcn_exp2f(st[0] - m1) : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * fa + (some ? x[e] * fb : 0.f);
+        stat = f32x4{m1, stat[1] * fa + st[1] * fb, stat[2] * fa + (some ? st[2] * fb : 0.f), 0.f};
+    };
+    constexpr int kAtOnce = 4;  // loads under way
+    for (int i = (wave % W) * 4 + (lane >> 4); i < of.x; i += 4 * W * kAtOnce) {
+        f32x4 st[kAtOnce], x[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t at = at0 + min(i + 4 * W * u, of.x - 1) * step;
+            st[u] = p.stat[at];
+            x[u] = *reinterpret_cast<const f32x4*>(p.o + at * kHeadDim + d0);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (i + 4 * W * u < of.x) add(st[u], x[u]);
     }
-    const float all = max_xor32(max_xor16(top));
-    const float f = top > kNegInf ? __builtin_amdgcn_exp2f(top - all) : 0.f;
+    // the four lanes of a wave that share dimensions
+    const float top = max_xor32(max_xor16(stat[0]));
+    const float f = stat[1] != 0.f ? __builtin_amdgcn_exp2f(stat[0] - top) : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = sum_xor32(sum_xor16(o[e] * f));
-    sum = sum_xor32(sum_xor16(sum * f));
-    rounded = sum_xor32(sum_xor16(rounded * f));
-    if (sub == 0)
-        finish_row<TYPE>(a, q, out, lse, t, h, s, (int64_t)a.length[s] - a.first[s + 1] + t, d0, o, all, sum, rounded);
+    stat = f32x4{top, sum_xor32(sum_xor16(stat[1] * f)), sum_xor32(sum_xor16(stat[2] * f)), 0.f};
+    if constexpr (W > 1) {
+        if (lane < 16) sums[wave][lane] = o;
+        if (lane == 0) stats[wave] = stat;
+        __syncthreads();
+        if (threadIdx.x >= 16) return;
+        for (int w = 1; w < W; ++w) add(stats[w], sums[w][lane]);
+    }
+    if (lane < 16)
+        finish_row<TYPE>(a, q, out, lse, t, h, s, (int64_t)a.length[s] - a.first[s + 1] + t, d0, o, stat[0], stat[1],
+                         stat[2]);
 }
+
 // The kernels and splits of a call.
 struct Plan {
     bool narrow, wide, join;
@@ -840,7 +926,7 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     p.narrow = most <= kNarrowRows || a.n_seq > 1;
     p.wide = most > kNarrowRows;
     p.qt = most > 64 ? 4 : 1;
-    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, 4 * kStep, (2048 + a.Hkv - 1) / a.Hkv};
+    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, kNarrowUnit, (2048 + a.Hkv - 1) / a.Hkv};
     p.w = {64 * p.qt, p.narrow ? kNarrowRows : 0, kAll, 64, ((p.qt == 4 ? 512 : 768) + a.Hkv - 1) / a.Hkv};
     const int64_t seqs = std::min<int64_t>(a.n_seq, a.T);
     size_t off = align256((size_t)a.n_seq * sizeof(int2));
@@ -887,8 +973,15 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
         cache_narrow_kernel<TYPE, SHARED><<<(unsigned)(p.n_items * a.Hkv), 256, 0, stream>>>(a, p.n, np, q, out, lse);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    if (p.join)
-        cache_join_kernel<TYPE><<<(unsigned)((a.T * a.H + 3) / 4), 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
+    if (p.join) {
+        // few rows have many parts each
+        const int64_t rows = a.T * a.H;
+        if (rows <= 1024)
+            cache_join_kernel<TYPE, 4><<<(unsigned)rows, 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
+        else
+            cache_join_kernel<TYPE, 1><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q,
+                                                                                     out, lse);
+    }
     return hipGetLastError();
 }
 
