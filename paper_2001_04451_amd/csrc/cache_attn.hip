@@ -583,7 +583,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
     // what this wave's rows see: all of them the first `least` keys, none more than `mine`
     const int mine = active ? query_row(a, it, min(rw + 16 * QT, it.n_rows) - 1, G, SHARED).limit : 0;
     const int least = active ? query_row(a, it, rw, G, SHARED).limit : 0;
-    const float scale_log2e = a.scale * kLog2e;
+    const float scale_log2e = fabsf(a.scale) * kLog2e;  // a negative scale turns the queries round, which is exact
 
     bf16x8 qop[QT][2];
     uint32_t past = 0;  // byte qt: what row 16 qt + n of the wave sees beyond `least` (at most 63 positions)
@@ -595,13 +595,14 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(at + 32 * i + 8 * g);
-            qop[qt][i] = as_bf16x8(x);
+            u32x4 x = *reinterpret_cast<const u32x4*>(at + 32 * i + 8 * g);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
+                if (a.scale < 0.f) x[e] ^= 0x80008000u;
                 const float lo = __uint_as_float(x[e] << 16), hi = __uint_as_float(x[e] & 0xFFFF0000u);
                 ss = fmaf(lo, lo, fmaf(hi, hi, ss));
             }
+            qop[qt][i] = as_bf16x8(x);
         }
         ss = sum_xor32(sum_xor16(ss));
         biggest = fmaxf(biggest, ss);
@@ -684,72 +685,132 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
         }
     };
 
-    auto attend = [&](int b, int key0, uint32_t hole, auto fast_tag, auto edge_tag) {
+    // The pieces of a block's work for keys 32 kp .. +31 (two 16-key tiles) and
+    // the wave's query tile qt.
+    auto load_k = [&](int b, int kp, bf16x8 (&kop)[2][2], f32x4 (&cf)[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int r = 32 * kp + 16 * t;
+            kop[t][0] = as_bf16x8(lds_piece<kSwz>(S.Ks[b], r + n, g));
+            kop[t][1] = as_bf16x8(lds_piece<kSwz>(S.Ks[b], r + n, 4 + g));
+            if constexpr (SHARED) cf[t] = scale_log2e * *reinterpret_cast<const f32x4*>(&S.inv[b][2 * kp + t][4 * g]);
+        }
+    };
+    auto load_v = [&](int b, int kp, int dt) {
+        return cat4(vt_read(S.Vs[b] + vt_offset<kSwz>(32 * kp, 16 * dt, lane)),
+                    vt_read(S.Vs[b] + vt_offset<kSwz>(32 * kp + 16, 16 * dt, lane)));
+    };
+    auto scores = [&](int qt, const bf16x8 (&kop)[2][2], f32x4 (&z)[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            z[t] = mfma16x16x32(kop[t][0], qop[qt][0], f32x4{});
+            z[t] = mfma16x16x32(kop[t][1], qop[qt][1], z[t]);
+        }
+    };
+    // z: products, with shared QK times their keys' factors, -inf where hidden.
+    auto weights = [&](int qt, f32x4 (&z)[2], auto fast_tag, auto edge_tag) {
         constexpr bool FAST = decltype(fast_tag)::value, EDGE = decltype(edge_tag)::value;
-        const char* const Ks = S.Ks[b];
-        const char* const Vb = S.Vs[b];
+        float off = 0.f;
+        if constexpr (!FAST) {
+            float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
+                             fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+            mt = max_xor32(max_xor16(mt));
+            if constexpr (!SHARED) mt = mt > kNegInf ? mt * scale_log2e : mt;
+            if (__any(mt > m[qt])) {
+                const float m1 = fmaxf(m[qt], mt);
+                const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m[qt] - m1) : 1.f;
+                l[qt] *= corr;
+                rounded[qt] *= corr;
 #pragma unroll
-        for (int kp = 0; kp < 2; ++kp) {
-            bf16x8 kop[2][2];
-            f32x4 cf[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int r = 32 * kp + 16 * t;
-                kop[t][0] = as_bf16x8(lds_piece<kSwz>(Ks, r + n, g));
-                kop[t][1] = as_bf16x8(lds_piece<kSwz>(Ks, r + n, 4 + g));
-                if constexpr (SHARED) cf[t] = scale_log2e * *reinterpret_cast<const f32x4*>(&S.inv[b][2 * kp + t][4 * g]);
+                for (int dt = 0; dt < 4; ++dt) o[qt][dt] *= corr;
+                m[qt] = m1;
             }
-            bf16x8 pk[QT];
+            off = m[qt] > kNegInf ? m[qt] : 0.f;
+        }
+        u32x4 pw;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            f32x4 p = z[t];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (EDGE && !SHARED)  // a scale of 0 leaves a hidden key hidden
+                    p[j] = p[j] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(p[j], scale_log2e, -off));
+                else
+                    p[j] = __builtin_amdgcn_exp2f(FAST ? p[j] : SHARED ? p[j] - off : fmaf(p[j], scale_log2e, -off));
+            }
+            l[qt] += (p[0] + p[1]) + (p[2] + p[3]);
+            pw[2 * t] = pack_bf16x2(p[0], p[1]);
+            pw[2 * t + 1] = pack_bf16x2(p[2], p[3]);
+        }
+        return as_bf16x8(pw);
+    };
+
+    // A block that the wave's rows see in full, as a pipeline over units of 32
+    // keys and 16 queries: while a unit's weights are formed, the matrix cores
+    // take the next one's scores and the last one's values.
+    auto attend_whole = [&](int b, auto fast_tag) {
+        constexpr int kUnits = 2 * QT;
+        bf16x8 kop[2][2], vt[4], pk[2];
+        f32x4 cf[2], cf_next[2], z[2][2];
+        load_k(b, 0, kop, cf);
+        scores(0, kop, z[0]);
+        if constexpr (QT == 1) {
+            load_k(b, 1, kop, cf_next);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            if (u == 0 || u == QT + 1)
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) vt[dt] = load_v(b, u / QT, dt);
+            if (u + 1 < kUnits) scores((u + 1) % QT, kop, z[(u + 1) & 1]);
+            if (u + 2 == QT) load_k(b, 1, kop, cf_next);  // the last scores of these keys are on their way
+            if (u == QT) cf[0] = cf_next[0], cf[1] = cf_next[1];
+            auto values = [&] {
+                const int qt = (u - 1) % QT;
+                rounded[qt] = mfma16x16x32(kOnes8, pk[(u - 1) & 1], rounded[qt]);
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) o[qt][dt] = mfma16x16x32(vt[dt], pk[(u - 1) & 1], o[qt][dt]);
+            };
+            if (QT == 1 && u > 0) values();  // a new maximum rescales this very tile's sums
+            if constexpr (SHARED) z[u & 1][0] *= cf[0], z[u & 1][1] *= cf[1];
+            pk[u & 1] = weights(u % QT, z[u & 1], fast_tag, Tag<false>{});
+            if (QT > 1 && u > 0) values();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (QT == 1)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) vt[dt] = load_v(b, 1, dt);
+        rounded[QT - 1] = mfma16x16x32(kOnes8, pk[1], rounded[QT - 1]);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) o[QT - 1][dt] = mfma16x16x32(vt[dt], pk[1], o[QT - 1][dt]);
+    };
+    // Any block: every key is tested against every row.
+    auto attend_edge = [&](int b, int key0, uint32_t hole) {
+#pragma unroll 1
+        for (int kp = 0; kp < 2; ++kp) {
+            bf16x8 kop[2][2], pk[QT];
+            f32x4 cf[2];
+            load_k(b, kp, kop, cf);
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
                 f32x4 z[2];
+                scores(qt, kop, z);
+                const int end = min(least + (int)(past >> (8 * qt) & 255), k1);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    z[t] = mfma16x16x32(kop[t][0], qop[qt][0], f32x4{});
-                    z[t] = mfma16x16x32(kop[t][1], qop[qt][1], z[t]);
+                    if constexpr (SHARED) z[t] *= cf[t];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        z[t][j] *= SHARED ? cf[t][j] : scale_log2e;
-                        if constexpr (EDGE) {
-                            const int key = key0 + 32 * kp + 16 * t + 4 * g + j;
-                            const bool ok = key < min(least + (int)(past >> (8 * qt) & 255), k1) && !(hole >> (2 * kp + t) & 1);
-                            z[t][j] = ok ? z[t][j] : kNegInf;
-                        }
+                        const int key = key0 + 32 * kp + 16 * t + 4 * g + j;
+                        z[t][j] = key < end && !(hole >> (2 * kp + t) & 1) ? z[t][j] : kNegInf;
                     }
                 }
-                float off = 0.f;
-                if constexpr (!FAST) {
-                    float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
-                                     fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-                    mt = max_xor32(max_xor16(mt));
-                    if (__any(mt > m[qt])) {
-                        const float m1 = fmaxf(m[qt], mt);
-                        const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m[qt] - m1) : 1.f;
-                        l[qt] *= corr;
-                        rounded[qt] *= corr;
-#pragma unroll
-                        for (int dt = 0; dt < 4; ++dt) o[qt][dt] *= corr;
-                        m[qt] = m1;
-                    }
-                    off = m[qt] > kNegInf ? m[qt] : 0.f;
-                }
-                u32x4 pw;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) z[t][j] = __builtin_amdgcn_exp2f(z[t][j] - off);
-                    l[qt] += (z[t][0] + z[t][1]) + (z[t][2] + z[t][3]);
-                    pw[2 * t] = pack_bf16x2(z[t][0], z[t][1]);
-                    pw[2 * t + 1] = pack_bf16x2(z[t][2], z[t][3]);
-                }
-                pk[qt] = as_bf16x8(pw);
+                pk[qt] = weights(qt, z, Tag<false>{}, Tag<true>{});
                 rounded[qt] = mfma16x16x32(kOnes8, pk[qt], rounded[qt]);
             }
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
-                bf16x8 vt = cat4(vt_read(Vb + vt_offset<kSwz>(32 * kp, 16 * dt, lane)),
-                                 vt_read(Vb + vt_offset<kSwz>(32 * kp + 16, 16 * dt, lane)));
-                if constexpr (EDGE) vt = blank(vt, odd);
+                const bf16x8 vt = blank(load_v(b, kp, dt), odd);
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mfma16x16x32(vt, pk[qt], o[qt][dt]);
             }
@@ -758,7 +819,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
 
     // No running maximum where every logit of the workgroup is within 2^-60 and
     // 2^60 of one: normalised keys bound it by the query's length.
-    const bool fast = SHARED && __syncthreads_and(fabsf(scale_log2e) * sqrtf(biggest) <= 60.f);
+    const bool fast = SHARED && __syncthreads_and(scale_log2e * sqrtf(biggest) <= 60.f);
     if (fast)
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) m[qt] = 0.f;
@@ -788,8 +849,8 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
     const int whole = min(blocks, max(query_row(a, it, r0, G, SHARED).limit - k0, 0) / 64);
     auto walk = [&](auto fast_tag) {
         while (kb < whole && !hole())
-            step([&](int b, int key0) {
-                if (active) attend(b, key0, 0u, fast_tag, Tag<false>{});
+            step([&](int b, int) {
+                if (active) attend_whole(b, fast_tag);
             });
     };
     if (fast)
@@ -799,7 +860,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
     const int edge0 = k0 + kb * 64;
     while (kb < blocks)
         step([&](int b, int key0) {
-            if (key0 < mine) attend(b, key0, hole(), Tag<false>{}, Tag<true>{});
+            if (key0 < mine) attend_edge(b, key0, hole());
         });
     if (!active) return;
 
