@@ -28,15 +28,17 @@ namespace {
 
 constexpr int kSwz = 1;  // LDS row layout (attn_common.h): 16-row operand reads
 constexpr int kNarrowRows = 16;
-constexpr int kNarrowUnit = 256;  // keys a part is a multiple of: 64 a wave
 constexpr bf16x8 kOnes8 = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
                            (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
 constexpr float kNegInf = -__builtin_inff();
 
 // How the keys are split: rows in (lo, hi] belong to this kernel, in tiles of
-// `rows`; parts are multiples of `unit` keys, about `target` items a head.
+// `rows`; parts are multiples of `step` keys.  Up to `target` items a head,
+// but parts of fewer than `longer` keys only to have `few` items a head, and
+// none of fewer than `shorter`: each part costs a workgroup's start and its
+// results' way through memory.
 struct Split {
-    int rows, lo, hi, unit, target;
+    int rows, lo, hi, step, shorter, longer, few, target;
 };
 
 struct Item {
@@ -77,9 +79,9 @@ __device__ __forceinline__ float wave_sum(float x) {  // the same in every lane
 }
 
 // Item number `item` of the split, the same for all lanes; false past the last.
-// A part has C = max(unit, keys of all tiles / target) keys, rounded up to
-// units: at most target + tiles items, at most 2 target of them in sequences
-// that are split (a tile of keys > C makes at most 2 keys / C parts).
+// A part has at most C >= keys of all tiles / target keys: at most target +
+// tiles items, at most 2 target of them in sequences that are split (a tile
+// of keys > C makes at most 2 keys / C parts).
 __device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& it) {
     const int lane = lane_id();
     float work = 0.f;  // the same in every workgroup: the same sums in the same order
@@ -89,8 +91,8 @@ __device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& i
         work += (float)tiles * (float)keys;
     }
     work = wave_sum(work);
-    const float want = fminf(work * 1.0001f / (float)sp.target, 1073741824.f);
-    const int C = (max((int)want + 1, sp.unit) + sp.unit - 1) / sp.unit * sp.unit;
+    const float few = fminf(fmaxf(work / (float)sp.few, (float)sp.shorter), (float)sp.longer);
+    const int C = (int)fminf(fmaxf(work * 1.0001f / (float)sp.target, few), 1073741824.f) + 1;
     int base = 0, slots = 0;
     for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
         if (a.n_seq > 64) seq_work(a, sp, s0 + lane, tiles, keys, rows);
@@ -106,7 +108,9 @@ __device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& i
             const int back = at / it.parts;  // the last tile, whose rows see the most, first
             it.part = at - back * it.parts;
             it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - back;
-            it.keys = C;
+            // alike parts, in whole steps
+            it.keys = (__builtin_amdgcn_readlane(keys, l) + it.parts - 1) / it.parts;
+            it.keys = (it.keys + sp.step - 1) / sp.step * sp.step;
             it.n_rows = __builtin_amdgcn_readlane(rows, l);
             it.slot = slots + __builtin_amdgcn_readlane(sum2 - split, l) + it.tile * it.parts + it.part;
             it.first = min(max((int64_t)a.first[it.seq], (int64_t)0), a.T);
@@ -269,10 +273,9 @@ struct Tag {
 // ---- narrow ----
 
 // 16-key tiles that a wave takes a step (its loads under way), and workgroups a CU.
-template <CacheType TYPE>
 constexpr int kTiles = 2;
-template <CacheType TYPE>
 constexpr int kNarrowOcc = 3;
+constexpr int kNarrowStep = 4 * 16 * kTiles;  // of the four waves
 
 // One 16-key tile as loaded: K rows in operand order (lane: row lane % 16,
 // group g = lane / 16), V rows in memory order.
@@ -328,10 +331,10 @@ __device__ __forceinline__ void widen16(u32x4 c, uint32_t byte, bf16x8* x) {
 }
 
 template <CacheType TYPE, bool SHARED>
-__global__ __launch_bounds__(256, kNarrowOcc<TYPE>) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
+__global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
                                                               const uint16_t* __restrict__ q,
                                                               uint16_t* __restrict__ out, float* __restrict__ lse) {
-    constexpr int NT = kTiles<TYPE>, kStep = 16 * NT;
+    constexpr int NT = kTiles, kStep = 16 * NT;
     __shared__ __attribute__((aligned(16))) char Vs[4][kStep * 128];
     __shared__ __attribute__((aligned(16))) float invs[4][kStep];  // k_inv of the step's keys
     __shared__ f32x4 stats[4][kNarrowRows];
@@ -901,23 +904,26 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
 
 // ---- joining split rows ----
 
-// W waves a (token, query head): a lane takes four dimensions of every 4 W-th
-// part, and the lanes are added in a fixed order, so the result does not
-// depend on which part came first.
-template <CacheType TYPE, int W>
+// LANES lanes a (token, query head), 16, 64 or 256: a lane takes four
+// dimensions of every LANES / 16-th part, and the lanes are added in a fixed
+// order, so the result does not depend on which part came first.
+template <CacheType TYPE, int LANES>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narrow, Split wide, bool any_wide, Parts np,
                                                          Parts wp, const uint16_t* __restrict__ q,
                                                          uint16_t* __restrict__ out, float* __restrict__ lse) {
+    constexpr int kSub = LANES / 16;  // lanes that share dimensions
     __shared__ f32x4 sums[4][16];
     __shared__ f32x4 stats[4];
     const int wave = threadIdx.x >> 6, lane = lane_id();
-    const int64_t item = (int64_t)blockIdx.x * (4 / W) + wave / W;
-    const int64_t t = item / a.H;
+    const int64_t item = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int64_t t = item / a.H, t0 = (item - (LANES == 16 ? lane >> 4 : 0)) / a.H;  // of the wave's first row
     const int h = (int)(item - t * a.H), G = a.H / a.Hkv, head = h / G;
-    // with W = 4 the whole workgroup leaves
-    if (t >= a.T) return;
-    const int s = seq_of(a.first, a.n_seq, t);
-    if (s < 0 || t >= a.first[s + 1]) return;
+    // rows leave whole (with LANES = 256 the workgroup)
+    if (t0 >= a.T) return;
+    int s = max(seq_of(a.first, a.n_seq, t0), 0);
+    if (LANES == 16)
+        while (s + 1 < a.n_seq && a.first[s + 1] <= t) ++s;
+    if (t >= a.T || t < a.first[s] || t >= a.first[s + 1]) return;
     const int64_t f0 = max((int64_t)a.first[s], (int64_t)0), f1 = min((int64_t)a.first[s + 1], a.T);
     const int rows = (int)(f1 - f0) * G;
     const bool is_narrow = rows <= wide.lo || !any_wide;
@@ -940,32 +946,33 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narr
         stat = f32x4{m1, stat[1] * fa + st[1] * fb, stat[2] * fa + (some ? st[2] * fb : 0.f), 0.f};
     };
     constexpr int kAtOnce = 4;  // loads under way
-    for (int i = (wave % W) * 4 + (lane >> 4); i < of.x; i += 4 * W * kAtOnce) {
+    for (int i = (threadIdx.x % LANES) >> 4; i < of.x; i += kSub * kAtOnce) {
         f32x4 st[kAtOnce], x[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int64_t at = at0 + min(i + 4 * W * u, of.x - 1) * step;
+            const int64_t at = at0 + min(i + kSub * u, of.x - 1) * step;
             st[u] = p.stat[at];
             x[u] = *reinterpret_cast<const f32x4*>(p.o + at * kHeadDim + d0);
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u)
-            if (i + 4 * W * u < of.x) add(st[u], x[u]);
+            if (i + kSub * u < of.x) add(st[u], x[u]);
     }
-    // the four lanes of a wave that share dimensions
-    const float top = max_xor32(max_xor16(stat[0]));
-    const float f = stat[1] != 0.f ? __builtin_amdgcn_exp2f(stat[0] - top) : 0.f;
+    if constexpr (LANES > 16) {  // the four lanes of a wave that share dimensions
+        const float top = max_xor32(max_xor16(stat[0]));
+        const float f = stat[1] != 0.f ? __builtin_amdgcn_exp2f(stat[0] - top) : 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = sum_xor32(sum_xor16(o[e] * f));
-    stat = f32x4{top, sum_xor32(sum_xor16(stat[1] * f)), sum_xor32(sum_xor16(stat[2] * f)), 0.f};
-    if constexpr (W > 1) {
+        for (int e = 0; e < 4; ++e) o[e] = sum_xor32(sum_xor16(o[e] * f));
+        stat = f32x4{top, sum_xor32(sum_xor16(stat[1] * f)), sum_xor32(sum_xor16(stat[2] * f)), 0.f};
+    }
+    if constexpr (LANES > 64) {
         if (lane < 16) sums[wave][lane] = o;
         if (lane == 0) stats[wave] = stat;
         __syncthreads();
         if (threadIdx.x >= 16) return;
-        for (int w = 1; w < W; ++w) add(stats[w], sums[w][lane]);
+        for (int w = 1; w < 4; ++w) add(stats[w], sums[w][lane]);
     }
-    if (lane < 16)
+    if (LANES == 16 || lane < 16)
         finish_row<TYPE>(a, q, out, lse, t, h, s, (int64_t)a.length[s] - a.first[s + 1] + t, d0, o, stat[0], stat[1],
                          stat[2]);
 }
@@ -986,13 +993,15 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     Plan p{};
     p.narrow = most <= kNarrowRows || a.n_seq > 1;
     p.wide = most > kNarrowRows;
-    p.qt = most > 64 ? 4 : 1;
-    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, kNarrowUnit, (2048 + a.Hkv - 1) / a.Hkv};
-    p.w = {64 * p.qt, p.narrow ? kNarrowRows : 0, kAll, 64, ((p.qt == 4 ? 512 : 768) + a.Hkv - 1) / a.Hkv};
+    const int64_t pairs = a.T * a.H * cap;
+    p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
+    auto a_head = [&](int items) { return (items + a.Hkv - 1) / a.Hkv; };
+    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, kNarrowStep, kNarrowStep, 4 * kNarrowStep, a_head(256), a_head(2048)};
+    p.w = {64 * p.qt, p.narrow ? kNarrowRows : 0, kAll, 64, 64, 128, a_head(128), a_head(p.qt == 1 ? 768 : 512)};
     const int64_t seqs = std::min<int64_t>(a.n_seq, a.T);
     size_t off = align256((size_t)a.n_seq * sizeof(int2));
     auto size = [&](const Split& s, int64_t tiles, int64_t& items, size_t& slots) {
-        const int64_t parts = (cap + s.unit - 1) / s.unit;  // of a tile, at most
+        const int64_t parts = (cap + s.shorter - 1) / s.shorter;  // of a tile, at most
         items = std::min<int64_t>(s.target, tiles * (parts - 1)) + tiles;
         slots = parts > 1 ? (size_t)std::min<int64_t>(2 * (int64_t)s.target, tiles * parts) : 0;
         off += align256(slots * a.Hkv * s.rows * kHeadDim * sizeof(float)) + align256(slots * a.Hkv * s.rows * sizeof(f32x4));
@@ -1027,7 +1036,11 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
         auto go = [&](auto kernel) {
             kernel<<<grid, 256, 0, stream>>>(a, p.w, wp, q, out, lse, (int)p.w_items, sets);
         };
-        p.qt == 4 ? go(cache_wide_kernel<TYPE, SHARED, 4, 2>) : go(cache_wide_kernel<TYPE, SHARED, 1, 3>);
+        switch (p.qt) {
+            case 4: go(cache_wide_kernel<TYPE, SHARED, 4, 2>); break;
+            case 2: go(cache_wide_kernel<TYPE, SHARED, 2, 2>); break;
+            default: go(cache_wide_kernel<TYPE, SHARED, 1, 3>);
+        }
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.narrow) {
@@ -1035,13 +1048,17 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.join) {
-        // few rows have many parts each
+        // Few rows have many parts each, many rows few.
         const int64_t rows = a.T * a.H;
+        auto go = [&](auto kernel, int lanes) {
+            kernel<<<(unsigned)((rows * lanes + 255) / 256), 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
+        };
         if (rows <= 1024)
-            cache_join_kernel<TYPE, 4><<<(unsigned)rows, 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
+            go(cache_join_kernel<TYPE, 256>, 256);
+        else if (rows <= 16384)
+            go(cache_join_kernel<TYPE, 64>, 64);
         else
-            cache_join_kernel<TYPE, 1><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q,
-                                                                                     out, lse);
+            go(cache_join_kernel<TYPE, 16>, 16);
     }
     return hipGetLastError();
 }
