@@ -1,6 +1,6 @@
 // Attention of new tokens over their sequences' cached rows (lsh_cache.h):
 //   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = exp2(z_ij - m_i),  z_ij = scale log2(e) q_i.k_j,
-// with the maximum m_i, the sum and the output kept in fp32 over one pass.
+// with the offset m_i (near the running maximum), the sum and the output kept in fp32 over one pass.
 //
 // gfx950 design.  The rows of a sequence and key head are its new tokens times
 // the H / Hkv query heads that share the key head.  A work item is a tile of
@@ -31,6 +31,11 @@ constexpr int kNarrowRows = 16;
 constexpr bf16x8 kOnes8 = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f,
                            (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
 constexpr float kNegInf = -__builtin_inff();
+// The offset that weights are taken against follows the running maximum only
+// when that has risen by more than this (in log2): weights stay below 2^16,
+// sums far within fp32, and neither the four lanes of a query nor the sums so
+// far need to be brought into line at every step.
+constexpr float kSlack = 16.f;
 
 // How the keys are split: rows in (lo, hi] belong to this kernel, in tiles of
 // `rows`; parts are multiples of `step` keys.  Up to `target` items a head,
@@ -456,9 +461,9 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
 #pragma unroll
             for (int t = 0; t < NT; ++t)
                 mt = fmaxf(fmaxf(mt, fmaxf(z[t][0], z[t][1])), fmaxf(z[t][2], z[t][3]));
-            mt = max_xor32(max_xor16(mt));
             if constexpr (!SHARED) mt = mt > kNegInf ? mt * c : mt;
-            if (__any(mt > m)) {
+            if (__any(mt > m + kSlack)) {
+                mt = max_xor32(max_xor16(mt));
                 const float m1 = fmaxf(m, mt);
                 const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
                 l *= corr;
@@ -717,9 +722,9 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
         if constexpr (!FAST) {
             float mt = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
                              fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-            mt = max_xor32(max_xor16(mt));
             if constexpr (!SHARED) mt = mt > kNegInf ? mt * scale_log2e : mt;
-            if (__any(mt > m[qt])) {
+            if (__any(mt > m[qt] + kSlack)) {
+                mt = max_xor32(max_xor16(mt));
                 const float m1 = fmaxf(m[qt], mt);
                 const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m[qt] - m1) : 1.f;
                 l[qt] *= corr;
@@ -996,7 +1001,9 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     const int64_t pairs = a.T * a.H * cap;
     p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
     auto a_head = [&](int items) { return (items + a.Hkv - 1) / a.Hkv; };
-    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, kNarrowStep, kNarrowStep, 4 * kNarrowStep, a_head(256), a_head(2048)};
+    // with a sequence and head for every CU, short parts are not needed, and short caches no join
+    const int shorter = a.n_seq * (int64_t)a.Hkv >= 256 ? 4 * kNarrowStep : kNarrowStep;
+    p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, kNarrowStep, shorter, 4 * kNarrowStep, a_head(256), a_head(2048)};
     p.w = {64 * p.qt, p.narrow ? kNarrowRows : 0, kAll, 64, 64, 128, a_head(128), a_head(p.qt == 1 ? 768 : 512)};
     const int64_t seqs = std::min<int64_t>(a.n_seq, a.T);
     size_t off = align256((size_t)a.n_seq * sizeof(int2));
