@@ -78,14 +78,18 @@ class CacheConfig:
     v_stride: int = 0
 
     def c(self) -> CacheConfigC:
-        c = self.__dict__.get("_c")  # the configuration is frozen: one structure serves all calls
+        scale = 1.0 / math.sqrt(self.d) if self.scale is None else self.scale
+        return CacheConfigC(self.T, self.q_stride, self.k_stride, self.v_stride, self.n_seq, self.H, self.Hkv, self.d,
+                            self.page, self.n_pages, self.max_pages, TYPES[self.type], int(bool(self.shared_qk)),
+                            self.max_new, scale, self.self_mask)
+
+    def ref(self):
+        """A reference to the C structure, made once: the configuration is frozen."""
+        c = self.__dict__.get("_c")
         if c is None:
-            scale = 1.0 / math.sqrt(self.d) if self.scale is None else self.scale
-            c = CacheConfigC(self.T, self.q_stride, self.k_stride, self.v_stride, self.n_seq, self.H, self.Hkv, self.d,
-                             self.page, self.n_pages, self.max_pages, TYPES[self.type], int(bool(self.shared_qk)),
-                             self.max_new, scale, self.self_mask)
+            c = self.c()
             object.__setattr__(self, "_c", c)
-        return c
+        return ctypes.byref(c)
 
     def strides(self, **own) -> "CacheConfig":
         """This configuration with the tensors' token strides."""
@@ -179,7 +183,7 @@ def _rows(t: torch.Tensor, cfg: CacheConfig, H: int, name: str, stride: int, dev
 
 
 def workspace_bytes(cfg: CacheConfig) -> int:
-    return int(lib().lsh_cache_workspace_bytes(ctypes.byref(cfg.c())))
+    return int(lib().lsh_cache_workspace_bytes(cfg.ref()))
 
 
 def workspace(cfg: CacheConfig, device) -> torch.Tensor:
@@ -196,7 +200,7 @@ def lsh_cache_write(cfg: CacheConfig, pages: Pages, seqs: Sequences, k, v) -> No
                       v_stride=_rows(v, cfg, cfg.Hkv, "v", cfg.v_stride, dev, k.dtype))
     with lsh.on_device(dev):
         lsh._check("lsh_cache_write",
-                   lib().lsh_cache_write(ctypes.byref(cfg.c()), lsh._dtype_code(k), ctypes.byref(pages.c()),
+                   lib().lsh_cache_write(cfg.ref(), lsh._dtype_code(k), ctypes.byref(pages.c()),
                                          ctypes.byref(seqs.c()), lsh._ptr(k), lsh._ptr(v), lsh._stream(dev)))
 
 
@@ -212,7 +216,7 @@ def lsh_cache_read(cfg: CacheConfig, pages: Pages, seqs: Sequences, dtype: torch
                       v_stride=_rows(v, cfg, cfg.Hkv, "v", cfg.v_stride, dev, dtype))
     with lsh.on_device(dev):
         lsh._check("lsh_cache_read",
-                   lib().lsh_cache_read(ctypes.byref(cfg.c()), lsh._dtype_code(k), ctypes.byref(pages.c()),
+                   lib().lsh_cache_read(cfg.ref(), lsh._dtype_code(k), ctypes.byref(pages.c()),
                                         ctypes.byref(seqs.c()), lsh._ptr(k), lsh._ptr(v), lsh._stream(dev)))
     return k, v
 
@@ -236,7 +240,7 @@ def lsh_cache_attn_fwd(cfg: CacheConfig, pages: Pages, seqs: Sequences, q, out=N
             raise ValueError(f"{name} is on {t.device}, the pages on {dev}")
     with lsh.on_device(dev):
         lsh._check("lsh_cache_attn_fwd",
-                   lib().lsh_cache_attn_fwd(ctypes.byref(cfg.c()), lsh.LSH_BF16, ctypes.byref(pages.c()),
+                   lib().lsh_cache_attn_fwd(cfg.ref(), lsh.LSH_BF16, ctypes.byref(pages.c()),
                                             ctypes.byref(seqs.c()), lsh._ptr(q), lsh._ptr(out), lsh._ptr(lse),
                                             lsh._ptr(workspace), workspace.numel(), lsh._stream(dev)))
     return out, lse

@@ -56,15 +56,16 @@ class QkConfig:
     dx_stride: int = 0
 
     def c(self) -> QkConfigC:
-        c = self.__dict__.get("_c")  # the configuration is frozen: one structure serves all calls
-        if c is None:
-            c = self._make()
-            object.__setattr__(self, "_c", c)
-        return c
-
-    def _make(self) -> QkConfigC:
         return QkConfigC(self.T, self.L, self.x_stride, self.dx_stride, self.Hq, self.Hk, self.d, self.rot,
                          int(bool(self.interleaved)), int(bool(self.gain_per_head)), self.eps)
+
+    def ref(self):
+        """A reference to the C structure, made once: the configuration is frozen."""
+        c = self.__dict__.get("_c")
+        if c is None:
+            c = self.c()
+            object.__setattr__(self, "_c", c)
+        return ctypes.byref(c)
 
     def out_shape(self, H: int) -> tuple:
         return (self.T // self.L, H, self.L, self.d) if self.L > 0 else (self.T, H, self.d)
@@ -74,7 +75,7 @@ class QkConfig:
 
 
 def qk_workspace_bytes(cfg: QkConfig) -> int:
-    return int(lib().lsh_qk_workspace_bytes(ctypes.byref(cfg.c())))
+    return int(lib().lsh_qk_workspace_bytes(cfg.ref()))
 
 
 def _token_rows(t: torch.Tensor, T: int, width: int, name: str, stride: int) -> int:
@@ -128,7 +129,7 @@ def lsh_qk_norm_rotate_fwd(cfg: QkConfig, x, gain_q, gain_k, freq, pos=None, q=N
     p = lsh._ptr
     with lsh.on_device(x.device):
         lsh._check("lsh_qk_norm_rotate_fwd",
-                   lib().lsh_qk_norm_rotate_fwd(ctypes.byref(cfg.c()), lsh._dtype_code(x), p(x), p(gain_q), p(gain_k),
+                   lib().lsh_qk_norm_rotate_fwd(cfg.ref(), lsh._dtype_code(x), p(x), p(gain_q), p(gain_k),
                                                 p(freq), p(pos), p(q), p(k), lsh._stream(x.device)))
     return q, k
 
@@ -158,7 +159,7 @@ def lsh_qk_norm_rotate_bwd(cfg: QkConfig, x, gain_q, gain_k, freq, pos, dq, dk=N
     p = lsh._ptr
     with lsh.on_device(x.device):
         lsh._check("lsh_qk_norm_rotate_bwd",
-                   lib().lsh_qk_norm_rotate_bwd(ctypes.byref(cfg.c()), lsh._dtype_code(x), p(x), p(gain_q), p(gain_k),
+                   lib().lsh_qk_norm_rotate_bwd(cfg.ref(), lsh._dtype_code(x), p(x), p(gain_q), p(gain_k),
                                                 p(freq), p(pos), p(dq), p(dk), p(dx), p(dgain_q), p(dgain_k),
                                                 p(workspace), workspace.numel(), lsh._stream(x.device)))
     return dx, dgain_q, dgain_k

@@ -157,3 +157,16 @@ def test_binding_refuses_before_the_library():
         qk.lsh_qk_norm_rotate_fwd(_qk(), torch.zeros(6, 192), torch.ones(64), torch.ones(64), torch.ones(32))
     with pytest.raises(KeyError):
         _cache(type="int8").c()
+
+
+def test_configurations_copy_and_compare(built):
+    """A configuration that has been used compares, copies and pickles as one that has not, and c() is the caller's own."""
+    import copy
+    import pickle
+    for make in (_cache, _qk):
+        used = make()
+        used.ref()
+        assert used == make() and hash(used) == hash(make())
+        assert pickle.loads(pickle.dumps(used)) == used and copy.deepcopy(used) == used
+        used.c().T = 99
+        assert used.c().T == make().T
