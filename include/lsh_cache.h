@@ -44,7 +44,7 @@
  * multiples of 8), out and lse are packed.  Pointers are 16-byte aligned.
  * Supported: d = 64, page a power of two from 16 to 4096,
  * max_pages * page <= 2^30, n_pages * Hkv * page < 2^34, H <= 1024,
- * n_seq < 2^20, T * H < 2^31 (LSH_ERR_UNSUPPORTED otherwise).
+ * n_seq <= 2^14, T * H < 2^31 (LSH_ERR_UNSUPPORTED otherwise).
  */
 #ifndef LSH_CACHE_H
 #define LSH_CACHE_H

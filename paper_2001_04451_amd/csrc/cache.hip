@@ -22,20 +22,19 @@ __device__ __forceinline__ int group8_max_int(int x) {
     return max(x, __builtin_amdgcn_mov_dpp(x, kDppHalfMirror, 0xF, 0xF, true));
 }
 
-// Where the lane's row goes.  Wave: eight tokens of one head of k or of v.
-struct RowOf {
-    int64_t t, slot;  // slot < 0: none
-    int head;
-    bool value, mine;  // v (not k); the row belongs to a sequence
+// The lane's token and where its rows are.  A wave takes eight consecutive
+// tokens and `per` of their rows (k and v of each head).
+struct Place {
+    int64_t t, slot;  // slot of head 0; < 0: none
+    int row0;         // first of the wave's rows: 2 * head, and 1 more for v
+    bool mine;        // the token belongs to a sequence
 };
-__device__ __forceinline__ RowOf row_of(const CacheArgs& a) {
+__device__ __forceinline__ Place place_of(const CacheArgs& a, int per) {
     const int64_t wave = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    const int per = 2 * a.Hkv;
-    RowOf r;
-    const int64_t tile = wave / per;
-    const int hk = (int)(wave - tile * per);
-    r.head = hk >> 1;
-    r.value = hk & 1;
+    const int groups = (2 * a.Hkv + per - 1) / per;
+    Place r;
+    const int64_t tile = wave / groups;
+    r.row0 = (int)(wave - tile * groups) * per;
     const int64_t t0 = tile * 8;
     r.t = t0 + (lane_id() >> 3);
     r.slot = -1;
@@ -45,31 +44,32 @@ __device__ __forceinline__ RowOf row_of(const CacheArgs& a) {
     while (s + 1 < a.n_seq && a.first[s + 1] <= r.t) ++s;
     const int64_t end = a.first[s + 1];
     r.mine = r.t < a.T && a.first[s] <= r.t && r.t < end;
-    if (r.mine) r.slot = slot_of(a, s, a.length[s] - end + r.t, r.head);
+    if (r.mine) r.slot = slot_of(a, s, a.length[s] - end + r.t, 0);
     return r;
 }
 
-template <CacheType TYPE, bool F32>
-__global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a, const void* __restrict__ k,
-                                                          const void* __restrict__ v) {
-    const RowOf r = row_of(a);
-    const int l = lane_id() & 7;
-    const int64_t at = r.slot < 0 ? 0 : r.t * (r.value ? a.v_stride : a.k_stride) + r.head * kHeadDim + 8 * l;
-    float x[8];
+// Eight values of a row of fp32 or bf16.
+template <bool F32>
+__device__ __forceinline__ void load8(const void* base, int64_t at, float* x) {
     if constexpr (F32) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(r.value ? v : k) + at);
+        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
         const f32x4 lo = p[0], hi = p[1];
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = lo[e], x[4 + e] = hi[e];
     } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(r.value ? v : k) + at);
+        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             x[2 * e] = __uint_as_float(w[e] << 16);
             x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
         }
     }
-    uint32_t big = 0;  // bits of the largest magnitude; those of infinities and NaN are the largest
+}
+
+template <CacheType TYPE>
+__device__ __forceinline__ void write_row(const CacheArgs& a, int64_t slot, bool value, float* x) {
+    const int l = lane_id() & 7;
+    char* const dst = value ? a.v : a.k;
     if constexpr (TYPE == kCacheBf16) {
         u32x4 w;
 #pragma unroll
@@ -78,48 +78,40 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a, const voi
             x[2 * e] = __uint_as_float(w[e] << 16);
             x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
         }
-        if (r.slot >= 0) *reinterpret_cast<u32x4*>((r.value ? a.v : a.k) + r.slot * 128 + 16 * l) = w;
+        if (slot >= 0) *reinterpret_cast<u32x4*>(dst + slot * 128 + 16 * l) = w;
     }
+    uint32_t big = 0;  // bits of the largest magnitude; those of infinities and NaN are the largest
 #pragma unroll
     for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[e]) & 0x7FFFFFFFu);
     big = block_max_u32(big);
-    int exp = (int)(big >> 23);  // the row's values are multiples of 2^(exp - 127) or so, for its length
+    int exp = (int)(big >> 23);
     if constexpr (TYPE != kCacheBf16) {
-        // LARGEST is 1.75 * 2^8 (e4m3) or 1.5 * 2^2 (e2m1)
+        // the largest code is 1.75 * 2^8 (e4m3) or 1.5 * 2^2 (e2m1)
         constexpr int kTop = TYPE == kCacheE4m3 ? 8 : 2;
         constexpr uint32_t kFrac = TYPE == kCacheE4m3 ? 0x600000u : 0x400000u;
         const bool finite = exp < 255;
         const int byte = finite ? max(exp - kTop + ((big & 0x7FFFFFu) > kFrac ? 1 : 0), 0) : 255;
         exp = byte;
-        uint32_t w0 = 0, w1 = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = finite ? ldexpf(x[e], 127 - byte) : 0.f;
+        uint32_t w0 = 0, w1 = 0;
         if constexpr (TYPE == kCacheE4m3) {
             w0 = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], (int)w0, false);
             w0 = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], (int)w0, true);
             w1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], (int)w1, false);
             w1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], (int)w1, true);
-            if (r.slot >= 0)
-                *reinterpret_cast<uint2*>((r.value ? a.v : a.k) + r.slot * 64 + 8 * l) = make_uint2(w0, w1);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x2 lo = pair_to_f32<TYPE, 0>(h ? w1 : w0), hi = pair_to_f32<TYPE, 1>(h ? w1 : w0);
-                x[4 * h] = lo[0], x[4 * h + 1] = lo[1], x[4 * h + 2] = hi[0], x[4 * h + 3] = hi[1];
-            }
+            if (slot >= 0) *reinterpret_cast<uint2*>(dst + slot * 64 + 8 * l) = make_uint2(w0, w1);
         } else {
             w0 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w0, x[0], x[1], 1.f, 0);
             w0 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w0, x[2], x[3], 1.f, 1);
             w0 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w0, x[4], x[5], 1.f, 2);
             w0 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w0, x[6], x[7], 1.f, 3);
-            if (r.slot >= 0) *reinterpret_cast<uint32_t*>((r.value ? a.v : a.k) + r.slot * 32 + 4 * l) = w0;
-            const f32x2 p0 = pair_to_f32<TYPE, 0>(w0), p1 = pair_to_f32<TYPE, 1>(w0), p2 = pair_to_f32<TYPE, 2>(w0),
-                        p3 = pair_to_f32<TYPE, 3>(w0);
-            x[0] = p0[0], x[1] = p0[1], x[2] = p1[0], x[3] = p1[1];
-            x[4] = p2[0], x[5] = p2[1], x[6] = p3[0], x[7] = p3[1];
+            if (slot >= 0) *reinterpret_cast<uint32_t*>(dst + slot * 32 + 4 * l) = w0;
         }
-        if (r.slot >= 0 && (l & 3) == 0) (r.value ? a.v_scale : a.k_scale)[2 * r.slot + (l >> 2)] = (uint8_t)byte;
+        if (slot >= 0 && (l & 3) == 0) (value ? a.v_scale : a.k_scale)[2 * slot + (l >> 2)] = (uint8_t)byte;
+        if (a.shared && !value) widen8<TYPE>(w0, w1, x);
     }
-    if (!a.shared || r.value) return;  // whole waves leave
+    if (!a.shared || value) return;  // the same for the whole wave
     // 1 / length of the stored row, its values brought near one by the larger
     // block's exponent: neither their squares nor their sum leave fp32's range.
     const int top = group8_max_int(exp);
@@ -134,56 +126,87 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a, const voi
     float inv = ldexpf(1.f / sqrtf(ss), 127 - top);
     if (!(ss > 0.f) || inv > 8.5070591730234616e37f) inv = 0.f;  // 2^126
     if (top == 255) inv = __builtin_nanf("");
-    if (l == 0 && r.slot >= 0) a.k_inv[r.slot] = inv;
+    if (l == 0 && slot >= 0) a.k_inv[slot] = inv;
 }
 
-template <CacheType TYPE, bool F32>
+template <CacheType TYPE, bool F32, int PER>
+__global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a, const void* __restrict__ k,
+                                                          const void* __restrict__ v) {
+    const Place r = place_of(a, PER);
+    const int l = lane_id() & 7, last = 2 * a.Hkv - 1;
+    float x[PER][8];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int row = min(r.row0 + i, last);
+        const bool value = row & 1;
+        const int64_t at = r.slot < 0 ? 0 : r.t * (value ? a.v_stride : a.k_stride) + (row >> 1) * kHeadDim + 8 * l;
+        load8<F32>(value ? v : k, at, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int row = r.row0 + i;
+        if (row > last) break;
+        write_row<TYPE>(a, r.slot < 0 ? -1 : r.slot + ((int64_t)(row >> 1) << a.page_log2), row & 1, x[i]);
+    }
+}
+
+template <CacheType TYPE, bool F32, int PER>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a, void* __restrict__ k, void* __restrict__ v) {
-    const RowOf r = row_of(a);
-    void* dst = r.value ? v : k;
-    if (!dst || !r.mine) return;
-    const int l = lane_id() & 7;
-    float x[8] = {};
-    if (r.slot >= 0) {
-        const char* base = r.value ? a.v : a.k;
+    const Place r = place_of(a, PER);
+    if (!r.mine) return;
+    const int l = lane_id() & 7, last = 2 * a.Hkv - 1;
+    u32x4 w[PER];
+    int byte[PER];
+    float inv[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int row = min(r.row0 + i, last);
+        const bool value = row & 1;
+        const int64_t slot = max(r.slot, (int64_t)0) + ((int64_t)(row >> 1) << a.page_log2);
+        const char* const src = value ? a.v : a.k;
         if constexpr (TYPE == kCacheBf16) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(base + r.slot * 128 + 16 * l);
+            w[i] = *reinterpret_cast<const u32x4*>(src + slot * 128 + 16 * l);
+        } else if constexpr (TYPE == kCacheE4m3) {
+            const uint2 c = *reinterpret_cast<const uint2*>(src + slot * 64 + 8 * l);
+            w[i] = u32x4{c.x, c.y, 0u, 0u};
+        } else {
+            w[i] = u32x4{*reinterpret_cast<const uint32_t*>(src + slot * 32 + 4 * l), 0u, 0u, 0u};
+        }
+        if constexpr (TYPE != kCacheBf16) byte[i] = (value ? a.v_scale : a.k_scale)[2 * slot + (l >> 2)];
+        inv[i] = a.shared && !value ? a.k_inv[slot] : 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int row = r.row0 + i;
+        if (row > last) break;
+        const bool value = row & 1;
+        void* const dst = value ? v : k;
+        if (!dst) continue;
+        float x[8];
+        if constexpr (TYPE == kCacheBf16) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __uint_as_float(w[e] << 16);
-                x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+                x[2 * e] = __uint_as_float(w[i][e] << 16);
+                x[2 * e + 1] = __uint_as_float(w[i][e] & 0xFFFF0000u);
             }
         } else {
-            const int byte = (r.value ? a.v_scale : a.k_scale)[2 * r.slot + (l >> 2)];
-            f32x2 p[4];
-            if constexpr (TYPE == kCacheE4m3) {
-                const uint2 w = *reinterpret_cast<const uint2*>(base + r.slot * 64 + 8 * l);
-                p[0] = pair_to_f32<TYPE, 0>(w.x), p[1] = pair_to_f32<TYPE, 1>(w.x);
-                p[2] = pair_to_f32<TYPE, 0>(w.y), p[3] = pair_to_f32<TYPE, 1>(w.y);
-            } else {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(base + r.slot * 32 + 4 * l);
-                p[0] = pair_to_f32<TYPE, 0>(w), p[1] = pair_to_f32<TYPE, 1>(w);
-                p[2] = pair_to_f32<TYPE, 2>(w), p[3] = pair_to_f32<TYPE, 3>(w);
-            }
+            widen8<TYPE>(w[i][0], w[i][1], x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = byte == 255 ? __builtin_nanf("") : ldexpf(p[e >> 1][e & 1], byte - 127);
+            for (int e = 0; e < 8; ++e) x[e] = byte[i] == 255 ? __builtin_nanf("") : ldexpf(x[e], byte[i] - 127);
         }
-        if (a.shared && !r.value) {
-            const float inv = a.k_inv[r.slot];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= inv;
+        for (int e = 0; e < 8; ++e) x[e] = r.slot < 0 ? 0.f : x[e] * inv[i];
+        const int64_t at = r.t * (value ? a.v_stride : a.k_stride) + (row >> 1) * kHeadDim + 8 * l;
+        if constexpr (F32) {
+            f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(dst) + at);
+            p[0] = f32x4{x[0], x[1], x[2], x[3]};
+            p[1] = f32x4{x[4], x[5], x[6], x[7]};
+        } else {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + at) = y;
         }
-    }
-    const int64_t at = r.t * (r.value ? a.v_stride : a.k_stride) + r.head * kHeadDim + 8 * l;
-    if constexpr (F32) {
-        f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(dst) + at);
-        p[0] = f32x4{x[0], x[1], x[2], x[3]};
-        p[1] = f32x4{x[4], x[5], x[6], x[7]};
-    } else {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + at) = w;
     }
 }
 
@@ -197,7 +220,12 @@ hipError_t by_type(CacheType type, bool f32, Go go) {
     return hipGetLastError();
 }
 
-unsigned row_grid(const CacheArgs& a) { return (unsigned)(((a.T + 7) / 8 * 2 * a.Hkv + 3) / 4); }
+// Rows a wave: four, whose loads are under way together, where that leaves
+// enough waves to fill the chip.
+bool four_rows(const CacheArgs& a) { return (a.T + 7) / 8 * a.Hkv >= 4096; }
+unsigned row_grid(const CacheArgs& a, int per) {
+    return (unsigned)(((a.T + 7) / 8 * ((2 * a.Hkv + per - 1) / per) + 3) / 4);
+}
 
 struct GoWrite {
     const CacheArgs& a;
@@ -205,7 +233,10 @@ struct GoWrite {
     hipStream_t stream;
     template <CacheType TYPE, bool F32>
     void operator()() const {
-        cache_write_kernel<TYPE, F32><<<row_grid(a), 256, 0, stream>>>(a, k, v);
+        if (four_rows(a))
+            cache_write_kernel<TYPE, F32, 4><<<row_grid(a, 4), 256, 0, stream>>>(a, k, v);
+        else
+            cache_write_kernel<TYPE, F32, 1><<<row_grid(a, 1), 256, 0, stream>>>(a, k, v);
     }
 };
 struct GoRead {
@@ -214,7 +245,10 @@ struct GoRead {
     hipStream_t stream;
     template <CacheType TYPE, bool F32>
     void operator()() const {
-        cache_read_kernel<TYPE, F32><<<row_grid(a), 256, 0, stream>>>(a, k, v);
+        if (four_rows(a))
+            cache_read_kernel<TYPE, F32, 4><<<row_grid(a, 4), 256, 0, stream>>>(a, k, v);
+        else
+            cache_read_kernel<TYPE, F32, 1><<<row_grid(a, 1), 256, 0, stream>>>(a, k, v);
     }
 };
 

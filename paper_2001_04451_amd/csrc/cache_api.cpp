@@ -32,7 +32,7 @@ int check_cache(const lsh_cache_config* c, lsh::CacheArgs* a) {
     if (c->type < LSH_CACHE_BF16 || c->type > LSH_CACHE_E2M1) return LSH_ERR_INVALID;
     if (c->H % c->Hkv != 0 || (c->shared_qk && c->H != c->Hkv)) return LSH_ERR_INVALID;
     if (!std::isfinite(c->scale) || !std::isfinite(c->self_mask)) return LSH_ERR_INVALID;
-    if (c->d != lsh::kHeadDimHost || c->H > 1024 || c->n_seq >= 1 << 20) return LSH_ERR_UNSUPPORTED;
+    if (c->d != lsh::kHeadDimHost || c->H > 1024 || c->n_seq > 1 << 14) return LSH_ERR_UNSUPPORTED;
     if (c->page < 16 || c->page > 4096 || (c->page & (c->page - 1)) != 0) return LSH_ERR_UNSUPPORTED;
     if ((int64_t)c->max_pages * c->page > (int64_t)1 << 30) return LSH_ERR_UNSUPPORTED;
     if ((int64_t)c->n_pages * c->Hkv >= ((int64_t)1 << 34) / c->page) return LSH_ERR_UNSUPPORTED;

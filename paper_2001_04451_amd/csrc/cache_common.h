@@ -61,4 +61,19 @@ __device__ __forceinline__ f32x2 pair_to_f32(uint32_t codes) {
         return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, P);
 }
 
+// Eight codes to fp32 without their scale.
+template <CacheType TYPE>
+__device__ __forceinline__ void widen8(uint32_t w0, uint32_t w1, float* x) {
+    f32x2 p[4];
+    if constexpr (TYPE == kCacheE4m3) {
+        p[0] = pair_to_f32<TYPE, 0>(w0), p[1] = pair_to_f32<TYPE, 1>(w0);
+        p[2] = pair_to_f32<TYPE, 0>(w1), p[3] = pair_to_f32<TYPE, 1>(w1);
+    } else {
+        p[0] = pair_to_f32<TYPE, 0>(w0), p[1] = pair_to_f32<TYPE, 1>(w0);
+        p[2] = pair_to_f32<TYPE, 2>(w0), p[3] = pair_to_f32<TYPE, 3>(w0);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e >> 1][e & 1];
+}
+
 }  // namespace lsh

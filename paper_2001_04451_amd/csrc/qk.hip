@@ -17,15 +17,18 @@ namespace {
 
 constexpr int kMaxTokens = 16;  // whose angles a workgroup holds at a time
 constexpr int kGroups = 32;     // eight-lane groups of a workgroup
+constexpr int kAtOnce = 2;      // rows of a group whose loads are under way
 
 struct Angles {
     float c[kMaxTokens][32];
     float s[kMaxTokens][32];
+    int b[kMaxTokens], l[kMaxTokens];  // batch entry and position in it (L > 0)
 };
 
 struct QkArgs {
     int64_t T, L, x_stride, dx_stride;
-    int Hq, Hk, rot, per_head;
+    int Hq, Hk, rot;
+    uint32_t h_magic;  // row / (Hq + Hk) as a product (more than one head)
     float eps;
 };
 
@@ -33,9 +36,13 @@ __device__ __forceinline__ void form_angles(Angles& A, int64_t t0, int tokens, i
                                             const float* __restrict__ freq, const int32_t* __restrict__ pos) {
     for (int i = threadIdx.x; i < tokens * 32; i += blockDim.x) {
         const int t = i >> 5, p = i & 31;
+        const uint32_t at = (uint32_t)(t0 + t);  // T < 2^31
+        if (p == 0 && a.L > 0) {
+            A.b[t] = (int)(at / (uint32_t)a.L);
+            A.l[t] = (int)(at % (uint32_t)a.L);
+        }
         if (p >= pairs) continue;
-        const int64_t at = t0 + t;
-        const double where = pos ? (double)pos[at] : (double)(a.L > 0 ? at % a.L : at);
+        const double where = pos ? (double)pos[at] : (double)(a.L > 0 ? at % (uint32_t)a.L : at);
         double rev = where * (double)freq[p] * 0.15915494309189535;  // 1 / (2 pi)
         rev -= rint(rev);
         float s, c;
@@ -93,10 +100,22 @@ __device__ __forceinline__ void turn(float* y, const Angles& A, int t, int l, in
     } else {
         const int hl = rot >> 4;  // lanes in half of the turned dimensions
         const bool low = l < hl, in = l < 2 * hl;
-        const int other = (threadIdx.x & 63) + (in ? (low ? hl : -hl) : 0);
         float z[8];
+        if (hl == 4) {  // lane l ^ 4: the banks of four lanes trade places by moves within their row
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other);
+            for (int e = 0; e < 8; ++e) {
+                const int x = __float_as_int(y[e]);
+                const int up = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xF, 0x5, false);  // banks 0, 2: from l + 4
+                z[e] = __int_as_float(__builtin_amdgcn_update_dpp(up, x, 0x114, 0xF, 0xA, false));  // 1, 3: from l - 4
+            }
+        } else if (hl == 2) {  // lane l ^ 2
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = dpp_f32<kDppXor2>(y[e]);
+        } else {
+            const int other = (threadIdx.x & 63) + (in ? (low ? hl : -hl) : 0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other);
+        }
         if (!in) return;
         const int p0 = 8 * (low ? l : l - hl);
 #pragma unroll
@@ -115,13 +134,15 @@ __device__ __forceinline__ float inv_rms(const float* x, float eps) {
     return ms > 0.f ? 1.f / sqrtf(ms) : ms == 0.f ? 0.f : ms;
 }
 
-// Where head h (of H) of token t starts in q, k and their gradients.
-__device__ __forceinline__ int64_t out_row(const QkArgs& a, int64_t t, int h, int H) {
-    if (a.L > 0) return ((t / a.L * H + h) * a.L + t % a.L) * kHeadDim;
-    return (t * H + h) * kHeadDim;
+// Where head h (of H) of the workgroup's token t0 + t starts in q, k and their gradients.
+__device__ __forceinline__ int64_t out_row(const QkArgs& a, const Angles& A, int64_t t0, int t, int h, int H) {
+    if (a.L > 0) return (((int64_t)A.b[t] * H + h) * a.L + A.l[t]) * kHeadDim;
+    return ((t0 + t) * H + h) * kHeadDim;
 }
 
-template <bool F32, bool INTER>
+// The rows (tokens times heads) of a workgroup's tokens, kAtOnce a group at a
+// time: their loads are under way while the angles are formed.
+template <bool F32, bool INTER, bool PER_HEAD>
 __global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a, int tokens_wg, const void* __restrict__ x,
                                                      const float* __restrict__ gq, const float* __restrict__ gk,
                                                      const float* __restrict__ freq, const int32_t* __restrict__ pos,
@@ -129,37 +150,60 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a, int tokens_wg, co
     __shared__ Angles A;
     const int64_t t0 = (int64_t)blockIdx.x * tokens_wg;
     const int tokens = (int)min((int64_t)tokens_wg, a.T - t0);
-    form_angles(A, t0, tokens, a.rot >> 1, a, freq, pos);
-    __syncthreads();
-    const int l = threadIdx.x & 7, H = a.Hq + a.Hk, rows = tokens * H;
-    for (int r0 = 0; r0 < rows; r0 += kGroups) {
-        const int r = min(r0 + (int)(threadIdx.x >> 3), rows - 1);  // idle groups redo the last row
-        const int t = (int)((uint32_t)r / (uint32_t)H), h = r - t * H;
-        const bool key = h >= a.Hq;
-        const int hh = key ? h - a.Hq : h;
-        float v[8], g[8];
-        load8<F32>(x, (t0 + t) * a.x_stride + h * kHeadDim + 8 * l, v);
-        load8<true>(key ? gk : gq, (a.per_head ? hh * kHeadDim : 0) + 8 * l, g);
-        const float inv = inv_rms(v, a.eps);
+    const int l = threadIdx.x & 7, group = threadIdx.x >> 3, H = a.Hq + a.Hk, rows = tokens * H;
+    float gs[2][8];
+    if constexpr (!PER_HEAD) {
+        load8<true>(gq, 8 * l, gs[0]);
+        load8<true>(a.Hk ? gk : gq, 8 * l, gs[1]);
+    }
+    for (int r0 = 0; r0 < rows; r0 += kGroups * kAtOnce) {
+        float v[kAtOnce][8];
+        int t[kAtOnce], h[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = v[e] * inv * g[e];
-        turn<INTER>(v, A, t, l, a.rot, 1.f);
-        if (r0 + (int)(threadIdx.x >> 3) < rows)
-            store8<F32>(key ? k : q, out_row(a, t0 + t, hh, key ? a.Hk : a.Hq) + 8 * l, v);
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (r0 + kGroups * u >= rows) break;
+            const int r = min(r0 + kGroups * u + group, rows - 1);  // idle groups redo the last row
+            t[u] = H == 1 ? r : (int)__umulhi((uint32_t)r, a.h_magic);
+            h[u] = r - t[u] * H;
+            load8<F32>(x, (t0 + t[u]) * a.x_stride + h[u] * kHeadDim + 8 * l, v[u]);
+        }
+        if (r0 == 0) {
+            form_angles(A, t0, tokens, a.rot >> 1, a, freq, pos);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (r0 + kGroups * u >= rows) break;
+            const bool key = h[u] >= a.Hq;
+            const int hh = key ? h[u] - a.Hq : h[u];
+            float g[8];
+            if constexpr (PER_HEAD) {
+                load8<true>(key ? gk : gq, hh * kHeadDim + 8 * l, g);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = key ? gs[1][e] : gs[0][e];
+            }
+            const float inv = inv_rms(v[u], a.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] = v[u][e] * inv * g[e];
+            turn<INTER>(v[u], A, t[u], l, a.rot, 1.f);
+            if (r0 + kGroups * u + group < rows)
+                store8<F32>(key ? k : q, out_row(a, A, t0, t[u], hh, key ? a.Hk : a.Hq) + 8 * l, v[u]);
+        }
     }
 }
 
 // A workgroup takes a run of tokens; an eight-lane group keeps to one head
 // (of up to 32 at a time) so that its part of the gain's gradient stays in
 // registers.  partial: [workgroup][gain row][64].
-template <bool F32, bool INTER>
+template <bool F32, bool INTER, bool PER_HEAD>
 __global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a, const void* __restrict__ x,
                                                      const float* __restrict__ gq, const float* __restrict__ gk,
                                                      const float* __restrict__ freq, const int32_t* __restrict__ pos,
                                                      const float* __restrict__ dq, const float* __restrict__ dk,
                                                      float* __restrict__ dx, float* __restrict__ partial,
                                                      int gain_rows) {
-    __shared__ Angles A;
+    __shared__ Angles both[2];  // of the batch at hand and of the next
     __shared__ float sums[kGroups][kHeadDim];
     const int l = threadIdx.x & 7, group = threadIdx.x >> 3, H = a.Hq + a.Hk;
     const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
@@ -171,42 +215,54 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a, const void* __res
         const bool on = slot < tpar && h < H;
         const int hc = min(h, H - 1);
         const bool key = hc >= a.Hq;
-        const int hh = key ? hc - a.Hq : hc;
+        const int hh = key ? hc - a.Hq : hc, Hx = key ? a.Hk : a.Hq;
+        const float* const dy = key ? dk : dq;
         float g[8], dg[8];
-        load8<true>(key ? gk : gq, (a.per_head ? hh * kHeadDim : 0) + 8 * l, g);
+        load8<true>(key ? gk : gq, (PER_HEAD ? hh * kHeadDim : 0) + 8 * l, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) dg[e] = 0.f;
-        for (int64_t t0 = ta; t0 < tb; t0 += kMaxTokens) {
-            const int tokens = (int)min((int64_t)kMaxTokens, tb - t0);
-            __syncthreads();  // the last batch's angles are read
-            form_angles(A, t0, tokens, a.rot >> 1, a, freq, pos);
-            __syncthreads();
-            for (int s0 = 0; s0 < tokens; s0 += tpar) {
-                const int t = min(s0 + slot, tokens - 1);
-                const bool take = on && s0 + slot < tokens;
-                float v[8], u[8];
-                load8<F32>(x, (t0 + t) * a.x_stride + hc * kHeadDim + 8 * l, v);
-                load8<true>(key ? dk : dq, out_row(a, t0 + t, hh, key ? a.Hk : a.Hq) + 8 * l, u);
-                turn<INTER>(u, A, t, l, a.rot, -1.f);
-                const float inv = inv_rms(v, a.eps);
-                float dot = 0.f;
+        auto batch = [&](int64_t t0) { return (int)min((int64_t)kMaxTokens, tb - t0); };
+        form_angles(both[0], ta, batch(ta), a.rot >> 1, a, freq, pos);
+        __syncthreads();
+        for (int64_t t0 = ta, i0 = 0; t0 < tb; t0 += kMaxTokens, ++i0) {
+            const Angles& A = both[i0 & 1];
+            const int tokens = batch(t0);
+            for (int s0 = 0; s0 < tokens; s0 += tpar * kAtOnce) {
+                float v[kAtOnce][8], u[kAtOnce][8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] *= inv;  // x r
-                    if (take) dg[e] = fmaf(u[e], v[e], dg[e]);
-                    u[e] *= g[e];
-                    dot = fmaf(u[e], v[e], dot);
+                for (int i = 0; i < kAtOnce; ++i) {
+                    const int t = min(s0 + tpar * i + slot, tokens - 1);
+                    load8<F32>(x, (t0 + t) * a.x_stride + hc * kHeadDim + 8 * l, v[i]);
+                    load8<true>(dy, out_row(a, A, t0, t, hh, Hx) + 8 * l, u[i]);
                 }
-                dot = group8_sum(dot) * (1.f / kHeadDim);
+                // the next batch's angles, while this one's rows are on their way
+                if (s0 == 0 && t0 + kMaxTokens < tb)
+                    form_angles(both[(i0 + 1) & 1], t0 + kMaxTokens, batch(t0 + kMaxTokens), a.rot >> 1, a, freq, pos);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = inv * (u[e] - v[e] * dot);
-                if (take) store8<true>(dx, (t0 + t) * a.dx_stride + hc * kHeadDim + 8 * l, u);
+                for (int i = 0; i < kAtOnce; ++i) {
+                    const int t = min(s0 + tpar * i + slot, tokens - 1);
+                    const bool take = on && s0 + tpar * i + slot < tokens;
+                    turn<INTER>(u[i], A, t, l, a.rot, -1.f);
+                    const float inv = inv_rms(v[i], a.eps);
+                    float dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[i][e] *= inv;  // x r
+                        if (take) dg[e] = fmaf(u[i][e], v[i][e], dg[e]);
+                        u[i][e] *= g[e];
+                        dot = fmaf(u[i][e], v[i][e], dot);
+                    }
+                    dot = group8_sum(dot) * (1.f / kHeadDim);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[i][e] = inv * (u[i][e] - v[i][e] * dot);
+                    if (take) store8<true>(dx, (t0 + t) * a.dx_stride + hc * kHeadDim + 8 * l, u[i]);
+                }
             }
+            __syncthreads();  // the next batch's angles are there, this one's read (and the sums of the last heads)
         }
-        __syncthreads();  // sums of the last heads are read
         store8<true>(&sums[group][0], 8 * l, dg);  // zeros where !on
         __syncthreads();
-        if (a.per_head) {
+        if constexpr (PER_HEAD) {
             for (int i = threadIdx.x; i < nh * kHeadDim; i += blockDim.x) {
                 const int hn = i >> 6, d = i & 63;
                 if (h0 + hn >= H) continue;
@@ -220,7 +276,7 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a, const void* __res
                 if ((h0 + s % nh >= a.Hq) == (threadIdx.x >= kHeadDim)) shared_sum += sums[s][d];
         }
     }
-    if (!a.per_head && threadIdx.x < gain_rows * kHeadDim) mine[threadIdx.x] = shared_sum;
+    if (!PER_HEAD && threadIdx.x < gain_rows * kHeadDim) mine[threadIdx.x] = shared_sum;
 }
 
 // One gain row a workgroup: its workgroups' partial sums added in fp64, in
@@ -241,12 +297,15 @@ __global__ __launch_bounds__(1024) void qk_gain_kernel(const float* __restrict__
     }
 }
 
-// Workgroups of the backward: enough for every CU to hold several.
-int64_t bwd_parts(int64_t T) { return std::min<int64_t>((T + kMaxTokens - 1) / kMaxTokens, 1024); }
+// Workgroups of the backward: four a CU, of four tokens at least.
+int64_t bwd_parts(int64_t T) { return std::min<int64_t>((T + 3) / 4, 1024); }
 int gain_rows(const QkShape& s) { return s.per_head ? s.Hq + s.Hk : (s.Hk ? 2 : 1); }
 
 QkArgs args_of(const QkShape& s) {
-    return {s.T, s.L, s.x_stride, s.dx_stride, s.Hq, s.Hk, s.rot, s.per_head, s.eps};
+    // row * ceil(2^32 / H) >> 32 is row / H for rows below 2^22 and H up to 1024
+    const uint64_t H = (uint64_t)s.Hq + s.Hk;
+    const uint32_t magic = H > 1 ? (uint32_t)((((uint64_t)1 << 32) + H - 1) / H) : 0;
+    return {s.T, s.L, s.x_stride, s.dx_stride, s.Hq, s.Hk, s.rot, magic, s.eps};
 }
 
 }  // namespace
@@ -264,10 +323,17 @@ hipError_t launch_qk_fwd(const QkShape& s, bool f32, const void* x, const float*
         kernel<<<(unsigned)((s.T + tokens - 1) / tokens), 256, 0, stream>>>(args_of(s), tokens, x, gq, gk, freq, pos, q,
                                                                            k);
     };
-    if (f32)
-        s.interleaved ? go(qk_fwd_kernel<true, true>) : go(qk_fwd_kernel<true, false>);
-    else
-        s.interleaved ? go(qk_fwd_kernel<false, true>) : go(qk_fwd_kernel<false, false>);
+    if (s.per_head) {
+        if (f32)
+            s.interleaved ? go(qk_fwd_kernel<true, true, true>) : go(qk_fwd_kernel<true, false, true>);
+        else
+            s.interleaved ? go(qk_fwd_kernel<false, true, true>) : go(qk_fwd_kernel<false, false, true>);
+    } else {
+        if (f32)
+            s.interleaved ? go(qk_fwd_kernel<true, true, false>) : go(qk_fwd_kernel<true, false, false>);
+        else
+            s.interleaved ? go(qk_fwd_kernel<false, true, false>) : go(qk_fwd_kernel<false, false, false>);
+    }
     return hipGetLastError();
 }
 
@@ -280,10 +346,17 @@ hipError_t launch_qk_bwd(const QkShape& s, bool f32, const void* x, const float*
     auto go = [&](auto kernel) {
         kernel<<<(unsigned)parts, 256, 0, stream>>>(args_of(s), x, gq, gk, freq, pos, dq, dk, dx, partial, rows);
     };
-    if (f32)
-        s.interleaved ? go(qk_bwd_kernel<true, true>) : go(qk_bwd_kernel<true, false>);
-    else
-        s.interleaved ? go(qk_bwd_kernel<false, true>) : go(qk_bwd_kernel<false, false>);
+    if (s.per_head) {
+        if (f32)
+            s.interleaved ? go(qk_bwd_kernel<true, true, true>) : go(qk_bwd_kernel<true, false, true>);
+        else
+            s.interleaved ? go(qk_bwd_kernel<false, true, true>) : go(qk_bwd_kernel<false, false, true>);
+    } else {
+        if (f32)
+            s.interleaved ? go(qk_bwd_kernel<true, true, false>) : go(qk_bwd_kernel<true, false, false>);
+        else
+            s.interleaved ? go(qk_bwd_kernel<false, true, false>) : go(qk_bwd_kernel<false, false, false>);
+    }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     qk_gain_kernel<<<(unsigned)rows, 1024, 0, stream>>>(partial, (int)parts, rows, s.per_head ? s.Hq : 1, dgq, dgk);
     return hipGetLastError();

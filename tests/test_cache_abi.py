@@ -87,7 +87,7 @@ BAD_CACHE = [(dict(T=0), INVALID), (dict(n_seq=0), INVALID), (dict(H=0), INVALID
              (dict(q_stride=128), INVALID), (dict(k_stride=132), INVALID), (dict(v_stride=64), INVALID),
              (dict(d=128), UNSUPPORTED), (dict(page=8), UNSUPPORTED), (dict(page=48), UNSUPPORTED),
              (dict(page=8192), UNSUPPORTED), (dict(max_pages=1 << 27), UNSUPPORTED), (dict(H=2048), UNSUPPORTED),
-             (dict(n_seq=1 << 20), UNSUPPORTED), (dict(T=1 << 30), UNSUPPORTED), (dict(q_stride=1 << 40), UNSUPPORTED)]
+             (dict(n_seq=(1 << 14) + 1), UNSUPPORTED), (dict(T=1 << 30), UNSUPPORTED), (dict(q_stride=1 << 40), UNSUPPORTED)]
 
 
 def _calls(c, pages, seqs, n=BIG, dtype=1):
