@@ -481,3 +481,95 @@ def test_binding_refusals(gpu):
         cache.lsh_cache_write(c.cfg, pages, seqs, rows.half(), rows.half())
     with pytest.raises(lsh.LshError):
         cache.lsh_cache_attn_fwd(c.cfg, pages, seqs, q, workspace=torch.empty(16, dtype=torch.uint8, device=gpu))
+
+
+@pytest.mark.parametrize("page", [256, 4096])
+def test_attention_large_pages(gpu, page):
+    log("cache attention pages of", page)
+    check_attention(Case("e4m3", True, 2, 2, page, [page + 3, 5, page], [1, 5, 40], fill="nan"), gpu)
+    check_attention(Case("bf16", False, 4, 1, page, [300], [300], fill="nan"), gpu)
+
+
+@pytest.mark.parametrize("type_", TYPES)
+def test_attention_many_heads_on_one(gpu, type_):
+    """More query heads on a key head than a narrow tile has rows, alone and in a batch."""
+    log("cache attention 48 heads on one", type_)
+    check_attention(Case(type_, False, 48, 1, 16, [500], [1]), gpu)
+    check_attention(Case(type_, False, 40, 2, 16, [500, 70, 3], [1, 2, 1]), gpu)
+
+
+def test_rows_before_and_behind_the_sequences(gpu):
+    """Sequences need not begin at row 0 nor end at T: the rows outside stay as they were, on every kernel's path."""
+    for lens, news, T in (([70, 3000], [1, 1], 9), ([500], [200], 260), ([90, 40, 0], [60, 1, 0], 100)):
+        for shared in (True, False):
+            c = Case("e4m3", shared, 2, 2, 16, lens, news, T=T)
+            c.first += 5
+            log("cache attention rows outside", lens, news)
+            check_attention(c, gpu)
+
+
+def test_log_partition_is_optional(gpu):
+    """lse may be NULL in the C call; out is the same."""
+    c = Case("bf16", True, 2, 2, 16, [2000, 50], [1, 40])
+    out, _, (pages, seqs, q) = check_attention(c, gpu)
+    ws = cache.workspace(c.cfg, gpu)
+    out2 = torch.empty_like(out)
+    assert cache.lib().lsh_cache_attn_fwd(c.cfg.ref(), 1, pages.c(), seqs.c(), q.data_ptr(), out2.data_ptr(), None,
+                                          ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out, out2)
+
+
+def test_two_streams_at_once(gpu):
+    """Calls over one pool on two streams, each with its own workspace."""
+    cases = [Case("e4m3", True, 2, 2, 16, [4000, 100], [1, 1], seed=1), Case("e4m3", True, 2, 2, 16, [700], [300], seed=2)]
+    runs = []
+    for c in cases:
+        out, lse, (pages, seqs, q) = check_attention(c, gpu)
+        runs.append((c, out, lse, pages, seqs, q, cache.workspace(c.cfg, gpu), torch.cuda.Stream()))
+    log("cache attention two streams")
+    torch.cuda.synchronize()
+    got = [[] for _ in runs]
+    for _ in range(5):
+        for i, (c, _, _, pages, seqs, q, ws, stream) in enumerate(runs):
+            with torch.cuda.stream(stream):
+                got[i].append(cache.lsh_cache_attn_fwd(c.cfg, pages, seqs, q, workspace=ws))
+    torch.cuda.synchronize()
+    for (_, out, lse, *_), results in zip(runs, got):
+        assert all(torch.equal(out, a) and torch.equal(lse, b) for a, b in results)
+
+
+@pytest.mark.parametrize("type_", TYPES)
+def test_whole_step_captured(gpu, type_):
+    """Write, read and attention in one graph, replayed on new rows, against eager calls."""
+    c = Case(type_, True, 2, 2, 16, [300, 20], [40, 1])
+    seqs = c.seqs(gpu)
+    pools = [cache.Pages.empty(c.cfg, gpu) for _ in range(2)]
+    for p in pools:
+        for t in (p.k, p.v, p.k_scale, p.v_scale, p.k_inv):
+            if t is not None:
+                t.zero_()
+    k, v = (torch.zeros(c.T, 2, 64, device=gpu) for _ in "kv")
+    q = c.q.to(gpu)
+    rk, rv = torch.empty_like(k), torch.empty_like(v)
+    out, lse, ws = torch.empty_like(q), torch.empty(c.T, 2, device=gpu), cache.workspace(c.cfg, gpu)
+
+    def step(pages, rk, rv, out, lse, ws):
+        cache.lsh_cache_write(c.cfg, pages, seqs, k, v)
+        cache.lsh_cache_read(c.cfg, pages, seqs, torch.float32, rk, rv)
+        cache.lsh_cache_attn_fwd(c.cfg, pages, seqs, q, out=out, lse=lse, workspace=ws)
+
+    log("cache step captured", type_)
+    step(pools[0], rk, rv, out, lse, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(pools[0], rk, rv, out, lse, ws)
+    for i in range(3):
+        k.normal_(generator=torch.Generator(gpu).manual_seed(i))
+        v.normal_(generator=torch.Generator(gpu).manual_seed(10 + i))
+        graph.replay()
+        eager = [torch.empty_like(t) for t in (rk, rv, out, lse, ws)]
+        step(pools[1], *eager)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((rk, rv, out, lse), eager))
+        assert torch.equal(pools[0].k, pools[1].k) and torch.equal(pools[0].v, pools[1].v)
