@@ -335,18 +335,21 @@ __device__ __forceinline__ void widen16(u32x4 c, uint32_t byte, bf16x8* x) {
     }
 }
 
+struct NarrowShared {
+    char Vs[4][16 * kTiles * 128];
+    float invs[4][16 * kTiles];  // k_inv of the step's keys
+    f32x4 stats[4][kNarrowRows];
+};
+
 template <CacheType TYPE, bool SHARED>
-__global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
-                                                              const uint16_t* __restrict__ q,
-                                                              uint16_t* __restrict__ out, float* __restrict__ lse) {
+__device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp, const Parts& parts,
+                                            const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
+                                            float* __restrict__ lse, uint32_t block, NarrowShared& S) {
     constexpr int NT = kTiles, kStep = 16 * NT;
-    __shared__ __attribute__((aligned(16))) char Vs[4][kStep * 128];
-    __shared__ __attribute__((aligned(16))) float invs[4][kStep];  // k_inv of the step's keys
-    __shared__ f32x4 stats[4][kNarrowRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int G = a.H / a.Hkv, head = blockIdx.x % (unsigned)a.Hkv;
+    const int G = a.H / a.Hkv, head = block % (unsigned)a.Hkv;
     Item it;
-    if (!find_item(a, sp, (int)(blockIdx.x / (unsigned)a.Hkv), it)) return;
+    if (!find_item(a, sp, (int)(block / (unsigned)a.Hkv), it)) return;
     if (it.tile == 0 && it.part == 0 && head == 0 && tid == 0)
         parts.of_seq[it.seq] = make_int2(it.parts, it.slot);  // slot of tile 0, part 0
     if (it.parts > 1 && it.slot >= parts.slots) return;
@@ -385,7 +388,7 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
     const int per = ((k1 - k0 + 4 * kStep - 1) / (4 * kStep)) * kStep;  // keys a wave
     const int w0 = k0 + wave * per, w1 = min(w0 + per, k1);
     const int steps = w0 < w1 ? (w1 - w0 + kStep - 1) / kStep : 0;
-    char* const V = Vs[wave];
+    char* const V = S.Vs[wave];
 
     constexpr int kRun = 64 / NT;  // steps that the runs of a wave's lanes last
     int runs = steps ? tile_runs(a, it.seq, head, w0 / 16 + lane, w1) : -1, runs_next = -1;
@@ -417,7 +420,7 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
         if (differ) edge0 = min(edge0, key0);
         wave_lds_order();  // the last step's reads of V before this step's writes
         f32x4 z[NT];
-        if (SHARED && lane < kStep) invs[wave][lane] = scale_log2e * inv;
+        if (SHARED && lane < kStep) S.invs[wave][lane] = scale_log2e * inv;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             bf16x8 kop[2];
@@ -446,7 +449,7 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
         wave_lds_order();
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            if constexpr (SHARED) z[t] *= *reinterpret_cast<const f32x4*>(&invs[wave][16 * t + 4 * g]);
+            if constexpr (SHARED) z[t] *= *reinterpret_cast<const f32x4*>(&S.invs[wave][16 * t + 4 * g]);
             if constexpr (EDGE)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -518,10 +521,10 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
 
     // Join the four waves: thread takes row tid / 16 and four dimensions.
     __syncthreads();
-    float* const O = reinterpret_cast<float*>(Vs[wave]);  // [row][64]
+    float* const O = reinterpret_cast<float*>(S.Vs[wave]);  // [row][64]
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(O + n * kHeadDim + 16 * dt + 4 * g) = o[dt];
-    if (g == 0) stats[wave][n] = f32x4{m, l, rounded[0], 0.f};
+    if (g == 0) S.stats[wave][n] = f32x4{m, l, rounded[0], 0.f};
     __syncthreads();
     const int r = tid >> 4, d0 = 4 * (tid & 15);
     if (r0 + r >= it.n_rows) return;
@@ -529,7 +532,7 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
     float top = kNegInf;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        ws[w] = stats[w][r];
+        ws[w] = S.stats[w][r];
         if (ws[w][1] != 0.f) top = fmaxf(top, ws[w][0]);
     }
     f32x4 sum = {}, stat = {top, 0.f, 0.f, 0.f};
@@ -537,7 +540,7 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
     for (int w = 0; w < 4; ++w) {
         if (ws[w][1] == 0.f) continue;  // no keys there
         const float f = __builtin_amdgcn_exp2f(ws[w][0] - top);
-        sum += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(Vs[w]) + r * kHeadDim + d0);
+        sum += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(S.Vs[w]) + r * kHeadDim + d0);
         stat[1] += f * ws[w][1];
         stat[2] += f * ws[w][2];
     }
@@ -565,18 +568,17 @@ struct WideShared {
     uint32_t scales[4][TYPE == kCacheBf16 ? 4 : 64];
 };
 
-template <CacheType TYPE, bool SHARED, int QT, int OCC>
-__global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split sp, Parts parts,
-                                                              const uint16_t* __restrict__ q,
-                                                              uint16_t* __restrict__ out, float* __restrict__ lse,
-                                                              int items, int sets) {
+template <CacheType TYPE, bool SHARED, int QT>
+__device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, const Parts& parts,
+                                          const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
+                                          float* __restrict__ lse, int items, int sets, uint32_t block,
+                                          WideShared<TYPE>& S) {
     constexpr int kRows = 64 * QT;
-    __shared__ __attribute__((aligned(16))) WideShared<TYPE> S;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
     const int G = a.H / a.Hkv;
     // Each XCD keeps to its own heads (or kXcds / sets XCDs share some), whose rows its L2 then serves.
-    const int xcd = (int)(blockIdx.x % kXcds), heads = a.Hkv / sets;
-    const int64_t turn = (int64_t)(blockIdx.x / kXcds) * (kXcds / sets) + xcd / sets;
+    const int xcd = (int)(block % kXcds), heads = a.Hkv / sets;
+    const int64_t turn = (int64_t)(block / kXcds) * (kXcds / sets) + xcd / sets;
     const int head = (int)(turn % heads) * sets + xcd % sets;
     if (turn / heads >= items) return;
     Item it;
@@ -907,6 +909,33 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
     }
 }
 
+// ---- the kernels ----
+
+template <CacheType TYPE, bool SHARED>
+__global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
+                                                                       const uint16_t* __restrict__ q,
+                                                                       uint16_t* __restrict__ out,
+                                                                       float* __restrict__ lse) {
+    __shared__ __attribute__((aligned(16))) NarrowShared S;
+    narrow_tile<TYPE, SHARED>(a, sp, parts, q, out, lse, blockIdx.x, S);
+}
+
+// Chunks, and beside them decoding sequences, in one grid, the chunks' tiles first.
+template <CacheType TYPE, bool SHARED, int QT, int OCC>
+__global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split narrow, Split wide, Parts np, Parts wp,
+                                                              const uint16_t* __restrict__ q,
+                                                              uint16_t* __restrict__ out, float* __restrict__ lse,
+                                                              int items, int sets, uint32_t wide_blocks) {
+    constexpr size_t kBytes = sizeof(WideShared<TYPE>) > sizeof(NarrowShared) ? sizeof(WideShared<TYPE>) : sizeof(NarrowShared);
+    __shared__ __attribute__((aligned(16))) char mem[kBytes];
+    if (blockIdx.x < wide_blocks)
+        wide_tile<TYPE, SHARED, QT>(a, wide, wp, q, out, lse, items, sets, blockIdx.x,
+                                    *reinterpret_cast<WideShared<TYPE>*>(mem));
+    else
+        narrow_tile<TYPE, SHARED>(a, narrow, np, q, out, lse, blockIdx.x - wide_blocks,
+                                  *reinterpret_cast<NarrowShared*>(mem));
+}
+
 // ---- joining split rows ----
 
 // LANES lanes a (token, query head), 16, 64 or 256: a lane takes four
@@ -998,6 +1027,11 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     Plan p{};
     p.narrow = most <= kNarrowRows || a.n_seq > 1;
     p.wide = most > kNarrowRows;
+    // Larger tiles read K and V from LDS less often, but leave fewer of them and
+    // need more parts to fill the chip.  Measured, 256 / 128 / 64 rows a tile
+    // (us): 2K tokens over 32K, 16 heads (2^30 pairs) 337 / 434 / 778; 256 over
+    // 64K (2^28) 111 / 118 / 147; 512 over 4K (2^25) 42 / 32 / 36; 24 over 1K, 8
+    // heads 13.1 / 11.3 / 10.4.
     const int64_t pairs = a.T * a.H * cap;
     p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
     auto a_head = [&](int items) { return (items + a.Hkv - 1) / a.Hkv; };
@@ -1005,6 +1039,13 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     const int shorter = a.n_seq * (int64_t)a.Hkv >= 256 ? 4 * kNarrowStep : kNarrowStep;
     p.n = {kNarrowRows, 0, p.wide ? kNarrowRows : kAll, kNarrowStep, shorter, 4 * kNarrowStep, a_head(256), a_head(2048)};
     p.w = {64 * p.qt, p.narrow ? kNarrowRows : 0, kAll, 64, 64, 128, a_head(128), a_head(p.qt == 1 ? 768 : 512)};
+    // With a tile for every CU only those are split that have twice the keys of
+    // the others, of a single sequence none (16 heads of a 2K prompt: 45 -> 41
+    // us without parts and without the kernel that joins them).
+    if (a.T * a.H >= 256 * p.w.rows) {
+        p.w.few = p.w.target = (int)std::max<int64_t>(rows / p.w.rows / 2, 1);
+        if (a.n_seq == 1) p.w.shorter = p.w.longer = (int)cap;
+    }
     const int64_t seqs = std::min<int64_t>(a.n_seq, a.T);
     size_t off = align256((size_t)a.n_seq * sizeof(int2));
     auto size = [&](const Split& s, int64_t tiles, int64_t& items, size_t& slots) {
@@ -1035,25 +1076,23 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
         return r;
     };
     const Parts np = carve(p.n_slots, p.n), wp = carve(p.w_slots, p.w);
+    int sets = kXcds;
+    while (a.Hkv % sets != 0) sets /= 2;
+    const int64_t turns = p.w_items * (a.Hkv / sets), per = kXcds / sets;
+    const unsigned wide = (unsigned)((turns + per - 1) / per * kXcds), narrow = (unsigned)(p.n_items * a.Hkv);
     if (p.wide) {
-        int sets = kXcds;
-        while (a.Hkv % sets != 0) sets /= 2;
-        const int64_t turns = p.w_items * (a.Hkv / sets), per = kXcds / sets;
-        const unsigned grid = (unsigned)((turns + per - 1) / per * kXcds);
         auto go = [&](auto kernel) {
-            kernel<<<grid, 256, 0, stream>>>(a, p.w, wp, q, out, lse, (int)p.w_items, sets);
+            kernel<<<wide + narrow, 256, 0, stream>>>(a, p.n, p.w, np, wp, q, out, lse, (int)p.w_items, sets, wide);
         };
         switch (p.qt) {
             case 4: go(cache_wide_kernel<TYPE, SHARED, 4, 2>); break;
             case 2: go(cache_wide_kernel<TYPE, SHARED, 2, 2>); break;
             default: go(cache_wide_kernel<TYPE, SHARED, 1, 3>);
         }
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    } else {
+        cache_narrow_kernel<TYPE, SHARED><<<narrow, 256, 0, stream>>>(a, p.n, np, q, out, lse);
     }
-    if (p.narrow) {
-        cache_narrow_kernel<TYPE, SHARED><<<(unsigned)(p.n_items * a.Hkv), 256, 0, stream>>>(a, p.n, np, q, out, lse);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.join) {
         // Few rows have many parts each, many rows few.
         const int64_t rows = a.T * a.H;
