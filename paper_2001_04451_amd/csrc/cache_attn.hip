@@ -1033,7 +1033,10 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     // 64K (2^28) 111 / 118 / 147; 512 over 4K (2^25) 42 / 32 / 36; 24 over 1K, 8
     // heads 13.1 / 11.3 / 10.4.
     const int64_t pairs = a.T * a.H * cap;
-    p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
+    if (cap < 2 * most / G)  // a whole prompt, half of whose pairs are hidden: parts do not even its tiles out, more tiles do
+        p.qt = a.T * a.H >= 512 * 256 ? 4 : 1;  // 16 heads of 8K 205 / 212 / 233, of 4K 127 / 84 / 73, of 2K 51 / 42 / 35
+    else
+        p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
     auto a_head = [&](int items) { return (items + a.Hkv - 1) / a.Hkv; };
     // with a sequence and head for every CU, short parts are not needed, and short caches no join
     const int shorter = a.n_seq * (int64_t)a.Hkv >= 256 ? 4 * kNarrowStep : kNarrowStep;
