@@ -4,9 +4,12 @@
 // values is four lanes.  A block's scale is the smallest power of two that
 // brings its largest magnitude to the type's largest value or below, read off
 // the magnitude's bits; x 2^-e is exact and the conversion rounds once, to
-// nearest even.  A wave takes eight consecutive tokens of one head, so that
-// it writes one run of a page.  HBM-bound; short calls are bound by the chain
-// of loads first -> length -> table -> page.
+// nearest even.  A wave takes eight consecutive tokens and one or four of their
+// rows, so that it writes runs of a page and finds its tokens' slots once.
+// HBM-bound: 16K tokens of 16 heads, fp32 into e2m1, 26 us (5.9 TB/s), read
+// back 28 (5.5); 8 sequences of up to 8K, e4m3 to bf16, 24 us (5.3), against
+// 36, 31 and 34 with one row a wave.  Short calls are bound by the chain of
+// loads first -> length -> table -> page (64 tokens 4.4 us).
 #include "cache_common.h"
 
 namespace lsh {

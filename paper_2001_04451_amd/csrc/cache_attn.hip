@@ -7,19 +7,30 @@
 // these rows and a run of keys; runs are split so that items are alike in
 // length however ragged the batch is, and a second kernel joins the parts of
 // rows that were split.  The split is made by every workgroup for itself from
-// `first` and `length` (find_item), so that nothing is planned on the host and
-// a captured call serves any lengths.
-// Both kernels form S^T = K Q^T and O^T = V^T P^T on the matrix cores with 16
-// rows of queries as the columns (mfma_f32_16x16x32_bf16), so a lane's scores
-// of four keys of two 16-key tiles are, packed to bf16, its operand of the
-// second product, and V^T comes from LDS rows by the transposing read.  Codes
-// are turned to bf16 with their block's scale on the way (exact).
+// `first` and `length` (find_item), or for many sequences by a kernel before
+// (cache_plan_kernel), so that nothing is planned on the host and a captured
+// call serves any lengths.
+// Both kinds of tile form S^T = K Q^T and O^T = V^T P^T on the matrix cores
+// with 16 rows of queries as the columns (mfma_f32_16x16x32_bf16), so a lane's
+// scores of four keys of two 16-key tiles are, packed to bf16, its operand of
+// the second product, and V^T comes from LDS rows by the transposing read.
+// Codes are turned to bf16 with their block's scale on the way (exact).  The
+// weights are rounded to bf16, as the matrix cores take them; the output is
+// divided by the sum of the rounded ones (one more product, with ones), so
+// they sum to one, and the log-partition takes the fp32 sum.
 //   narrow  16 rows (decoding, a few tokens): each of four waves walks its own
 //           keys, K rows straight from memory into operand registers, V rows
 //           through an LDS area of its own; the waves are joined at the end.
-//           Bound by HBM.
+//           Bound by HBM: 64 sequences of up to 16K, 16 heads, e4m3, 124 us
+//           (5.2 TB/s); one of 64K in bf16 45 us (6.0 TB/s), 52 with its join.
+//           Grouped 4-bit caches are bound by the conversions and exp instead
+//           (32 of 32K, 8 query heads a key head: 36 us, 3.9 TB/s).
 //   wide    64 QT rows (chunks): the four waves share blocks of 64 keys staged
-//           in LDS, double-buffered.  Bound by the matrix cores and exp.
+//           in LDS, double-buffered.  Bound by exp and the other vector
+//           instructions, which fill 59% of a SIMD's time, and by how far two
+//           waves overlap them with the matrix cores (37%): 2K tokens over
+//           32K, 16 heads, e4m3, 310 us (0.86 PFLOP/s; a library matrix
+//           product of 8192^3 reaches 1.12 on this card), 328 with its join.
 #include "attn_common.h"
 #include "cache_common.h"
 
@@ -83,49 +94,122 @@ __device__ __forceinline__ float wave_sum(float x) {  // the same in every lane
     return sum_xor32(sum_xor16(x + dpp_f32<kDppMirror>(x)));
 }
 
-// Item number `item` of the split, the same for all lanes; false past the last.
-// A part has at most C >= keys of all tiles / target keys: at most target +
-// tiles items, at most 2 target of them in sequences that are split (a tile
-// of keys > C makes at most 2 keys / C parts).
-__device__ bool find_item(const CacheArgs& a, const Split& sp, int item, Item& it) {
-    const int lane = lane_id();
-    float work = 0.f;  // the same in every workgroup: the same sums in the same order
+// Keys of a part, at most: C >= keys of all tiles / target, so that there are
+// at most target + tiles items, and at most 2 target of them in sequences that
+// are split (a tile of keys > C makes at most 2 keys / C parts).
+__device__ __forceinline__ int part_keys(const Split& sp, float work) {
+    const float few = fminf(fmaxf(work / (float)sp.few, (float)sp.shorter), (float)sp.longer);
+    return (int)fminf(fmaxf(work * 1.0001f / (float)sp.target, few), 1073741824.f) + 1;
+}
+__device__ __forceinline__ int parts_of(int tiles, int keys, int C) {
+    return tiles ? max(1, (int)(((uint32_t)keys + (uint32_t)C - 1u) / (uint32_t)C)) : 0;
+}
+
+// The split of many sequences, made once a call: of each sequence the number of
+// items up to its last, its first slot and its parts a tile.  One workgroup a
+// kind of tile.
+__global__ __launch_bounds__(1024) void cache_plan_kernel(CacheArgs a, Split narrow, Split wide, int4* narrow_plan,
+                                                          int4* wide_plan) {
+    __shared__ float works[16];
+    __shared__ int2 sums[16];
+    const Split sp = blockIdx.x ? wide : narrow;
+    int4* const plan = blockIdx.x ? wide_plan : narrow_plan;
+    if (!plan) return;
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
     int tiles, keys, rows;
-    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        seq_work(a, sp, s0 + lane, tiles, keys, rows);
+    float work = 0.f;
+    for (int s = threadIdx.x; s < a.n_seq; s += 1024) {
+        seq_work(a, sp, s, tiles, keys, rows);
         work += (float)tiles * (float)keys;
     }
     work = wave_sum(work);
-    const float few = fminf(fmaxf(work / (float)sp.few, (float)sp.shorter), (float)sp.longer);
-    const int C = (int)fminf(fmaxf(work * 1.0001f / (float)sp.target, few), 1073741824.f) + 1;
-    int base = 0, slots = 0;
-    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        if (a.n_seq > 64) seq_work(a, sp, s0 + lane, tiles, keys, rows);
-        const int parts = tiles ? max(1, (int)(((uint32_t)keys + (uint32_t)C - 1u) / (uint32_t)C)) : 0;
-        const int items = tiles * parts, split = parts > 1 ? items : 0;
-        const int sum = wave_scan(items), sum2 = wave_scan(split);
-        const uint64_t mine = __ballot(item - base < sum);
-        if (mine) {
-            const int l = __builtin_ctzll(mine);
-            it.seq = s0 + l;
-            const int at = item - base - __builtin_amdgcn_readlane(sum - items, l);
-            it.parts = __builtin_amdgcn_readlane(parts, l);
-            const int back = at / it.parts;  // the last tile, whose rows see the most, first
-            it.part = at - back * it.parts;
-            it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - back;
-            // alike parts, in whole steps
-            it.keys = (__builtin_amdgcn_readlane(keys, l) + it.parts - 1) / it.parts;
-            it.keys = (it.keys + sp.step - 1) / sp.step * sp.step;
-            it.n_rows = __builtin_amdgcn_readlane(rows, l);
-            it.slot = slots + __builtin_amdgcn_readlane(sum2 - split, l) + it.tile * it.parts + it.part;
-            it.first = min(max((int64_t)a.first[it.seq], (int64_t)0), a.T);
-            it.pos0 = (int64_t)a.length[it.seq] - a.first[it.seq + 1] + it.first;
-            return true;
+    if (lane == 0) works[wave] = work;
+    __syncthreads();
+    work = 0.f;
+    for (int w = 0; w < 16; ++w) work += works[w];
+    const int C = part_keys(sp, work);
+    int2 base = make_int2(0, 0);
+    for (int s0 = 0; s0 < a.n_seq; s0 += 1024) {
+        const int s = s0 + (int)threadIdx.x;
+        seq_work(a, sp, s, tiles, keys, rows);
+        const int parts = parts_of(tiles, keys, C), items = tiles * parts, split = parts > 1 ? items : 0;
+        int2 sum = make_int2(wave_scan(items), wave_scan(split));
+        __syncthreads();  // the last round's sums are read
+        if (lane == 63) sums[wave] = sum;
+        __syncthreads();
+        int2 all = make_int2(0, 0);
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) sum.x += sums[w].x, sum.y += sums[w].y;
+            all.x += sums[w].x, all.y += sums[w].y;
         }
-        base += __builtin_amdgcn_readlane(sum, 63);
-        slots += __builtin_amdgcn_readlane(sum2, 63);
+        if (s < a.n_seq) plan[s] = make_int4(base.x + sum.x, base.y + sum.y - split, parts, 0);
+        base.x += all.x, base.y += all.y;
     }
-    return false;
+}
+
+// Item number `item` of the split, the same for all lanes; false past the
+// last.  Without a plan every workgroup adds the sequences up for itself.
+__device__ bool find_item(const CacheArgs& a, const Split& sp, const int4* __restrict__ plan, int item, Item& it) {
+    const int lane = lane_id();
+    int tiles, keys, rows, at, slot;
+    if (plan) {
+        int base = 0, count = a.n_seq;  // the first sequence whose items end behind `item`: 64 at a time
+        for (;;) {
+            const int step = (count + 63) >> 6, end = min((lane + 1) * step, count);
+            const int n = __popcll(__ballot(lane * step < count && plan[base + end - 1].x <= item));
+            if (n * step >= count) return false;
+            base += n * step;
+            count = min(step, count - n * step);
+            if (count == 1) break;
+        }
+        const int4 p = plan[base];
+        seq_work(a, sp, base, tiles, keys, rows);
+        it.seq = base;
+        it.parts = __builtin_amdgcn_readfirstlane(p.z);
+        at = item - __builtin_amdgcn_readfirstlane(p.x - tiles * p.z);
+        slot = __builtin_amdgcn_readfirstlane(p.y);
+        tiles = __builtin_amdgcn_readfirstlane(tiles);
+        keys = __builtin_amdgcn_readfirstlane(keys);
+        rows = __builtin_amdgcn_readfirstlane(rows);
+    } else {
+        float work = 0.f;  // the same in every workgroup: the same sums in the same order
+        for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+            seq_work(a, sp, s0 + lane, tiles, keys, rows);
+            work += (float)tiles * (float)keys;
+        }
+        const int C = part_keys(sp, wave_sum(work));
+        int base = 0, slots = 0, s0 = 0;
+        for (;; s0 += 64) {
+            if (s0 >= a.n_seq) return false;
+            if (a.n_seq > 64) seq_work(a, sp, s0 + lane, tiles, keys, rows);
+            const int parts = parts_of(tiles, keys, C), items = tiles * parts, split = parts > 1 ? items : 0;
+            const int sum = wave_scan(items), sum2 = wave_scan(split);
+            const uint64_t mine = __ballot(item - base < sum);
+            if (mine) {
+                const int l = __builtin_ctzll(mine);
+                it.seq = s0 + l;
+                it.parts = __builtin_amdgcn_readlane(parts, l);
+                at = item - base - __builtin_amdgcn_readlane(sum - items, l);
+                slot = slots + __builtin_amdgcn_readlane(sum2 - split, l);
+                tiles = __builtin_amdgcn_readlane(tiles, l);
+                keys = __builtin_amdgcn_readlane(keys, l);
+                rows = __builtin_amdgcn_readlane(rows, l);
+                break;
+            }
+            base += __builtin_amdgcn_readlane(sum, 63);
+            slots += __builtin_amdgcn_readlane(sum2, 63);
+        }
+    }
+    const int back = at / it.parts;  // the last tile, whose rows see the most, first
+    it.part = at - back * it.parts;
+    it.tile = tiles - 1 - back;
+    it.keys = (keys + it.parts - 1) / it.parts;  // alike parts, in whole steps
+    it.keys = (it.keys + sp.step - 1) / sp.step * sp.step;
+    it.n_rows = rows;
+    it.slot = slot + it.tile * it.parts + it.part;
+    it.first = min(max((int64_t)a.first[it.seq], (int64_t)0), a.T);
+    it.pos0 = (int64_t)a.length[it.seq] - a.first[it.seq + 1] + it.first;
+    return true;
 }
 
 // Row r of the item's sequence and head: query head within the group, token,
@@ -164,9 +248,10 @@ __device__ __forceinline__ int tile_runs(const CacheArgs& a, int seq, int head, 
 // Partial results of split rows, in the workspace.
 struct Parts {
     float* o;       // [slot][Hkv][tile rows][64]: sum of weights times values
-    f32x4* stat;    // [slot][Hkv][tile rows]: maximum (log2), sum of weights, sum of the weights as rounded
+    f32x4* stat;    // [slot][Hkv][tile rows]: offset (log2), sum of weights, sum of the weights as rounded
     int2* of_seq;   // [n_seq]: parts a tile, first slot
     int slots;      // enough for any `first` that does not decrease; the rest of others is left out
+    const int4* plan;  // of cache_plan_kernel, or null
 };
 
 // Value d of a cached row.
@@ -231,8 +316,8 @@ __device__ __forceinline__ bf16x8 blank(bf16x8 vt, uint32_t& found) {
     }
     return as_bf16x8(w);
 }
-// o (dimensions 16 dt + 4 g + e of row `row`, whose query is at q) with the
-// non-finite values of the positions from .. to - 1 that it sees.
+// o (dimensions 16 dt + 4 g + e of a row whose query is at q) with the
+// non-finite values of the positions from .. to - 1 that it sees (rare, and slow).
 template <CacheType TYPE>
 __device__ __forceinline__ void add_odd(const CacheArgs& a, int seq, int head, int from, int to, int limit, int g,
                                         const uint16_t* __restrict__ q, f32x4 (&o)[4]) {
@@ -274,10 +359,12 @@ struct Tag {
     static constexpr bool value = B;
 };
 
-
 // ---- narrow ----
 
-// 16-key tiles that a wave takes a step (its loads under way), and workgroups a CU.
+// 16-key tiles that a wave takes a step (its loads under way), and workgroups
+// a CU.  Two tiles and three workgroups keep the walk out of scratch: 64
+// sequences of e4m3 / one of 64K in bf16 132 / 52 us, with four workgroups 159
+// / 102, with four tiles 157 / 81.
 constexpr int kTiles = 2;
 constexpr int kNarrowOcc = 3;
 constexpr int kNarrowStep = 4 * 16 * kTiles;  // of the four waves
@@ -349,7 +436,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
     const int G = a.H / a.Hkv, head = block % (unsigned)a.Hkv;
     Item it;
-    if (!find_item(a, sp, (int)(block / (unsigned)a.Hkv), it)) return;
+    if (!find_item(a, sp, parts.plan, (int)(block / (unsigned)a.Hkv), it)) return;
     if (it.tile == 0 && it.part == 0 && head == 0 && tid == 0)
         parts.of_seq[it.seq] = make_int2(it.parts, it.slot);  // slot of tile 0, part 0
     if (it.parts > 1 && it.slot >= parts.slots) return;
@@ -582,7 +669,7 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
     const int head = (int)(turn % heads) * sets + xcd % sets;
     if (turn / heads >= items) return;
     Item it;
-    if (!find_item(a, sp, (int)(turn / heads), it)) return;
+    if (!find_item(a, sp, parts.plan, (int)(turn / heads), it)) return;
     if (it.tile == 0 && it.part == 0 && head == 0 && tid == 0)
         parts.of_seq[it.seq] = make_int2(it.parts, it.slot);  // slot of tile 0, part 0
     if (it.parts > 1 && it.slot >= parts.slots) return;
@@ -1013,7 +1100,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narr
 
 // The kernels and splits of a call.
 struct Plan {
-    bool narrow, wide, join;
+    bool narrow, wide, join, planned;
     int qt;
     Split n, w;
     int64_t n_items, w_items;  // a head, at most
@@ -1050,7 +1137,9 @@ Plan plan_of(const CacheArgs& a, int max_new) {
         if (a.n_seq == 1) p.w.shorter = p.w.longer = (int)cap;
     }
     const int64_t seqs = std::min<int64_t>(a.n_seq, a.T);
-    size_t off = align256((size_t)a.n_seq * sizeof(int2));
+    if (!p.wide && seqs * a.Hkv >= 2048) p.n.target = (int)(seqs + 1) / 2;  // decoding, likewise
+    p.planned = a.n_seq > 128;
+    size_t off = align256((size_t)a.n_seq * sizeof(int2)) + (p.planned ? 2 * align256((size_t)a.n_seq * sizeof(int4)) : 0);
     auto size = [&](const Split& s, int64_t tiles, int64_t& items, size_t& slots) {
         const int64_t parts = (cap + s.shorter - 1) / s.shorter;  // of a tile, at most
         items = std::min<int64_t>(s.target, tiles * (parts - 1)) + tiles;
@@ -1068,8 +1157,16 @@ template <CacheType TYPE, bool SHARED>
 hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t* out, float* lse, void* workspace,
                   hipStream_t stream) {
     char* at = static_cast<char*>(workspace) + align256((size_t)a.n_seq * sizeof(int2));
-    auto carve = [&](size_t slots, const Split& s) {
+    auto plan = [&](bool used) {
+        int4* r = used && p.planned ? reinterpret_cast<int4*>(at) : nullptr;
+        if (p.planned) at += align256((size_t)a.n_seq * sizeof(int4));
+        return r;
+    };
+    int4* const n_plan = plan(p.narrow);
+    int4* const w_plan = plan(p.wide);
+    auto carve = [&](size_t slots, const Split& s, const int4* of) {
         Parts r;
+        r.plan = of;
         r.of_seq = static_cast<int2*>(workspace);
         r.slots = (int)slots;
         r.o = reinterpret_cast<float*>(at);
@@ -1078,7 +1175,11 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
         at += align256(slots * a.Hkv * s.rows * sizeof(f32x4));
         return r;
     };
-    const Parts np = carve(p.n_slots, p.n), wp = carve(p.w_slots, p.w);
+    const Parts np = carve(p.n_slots, p.n, n_plan), wp = carve(p.w_slots, p.w, w_plan);
+    if (p.planned) {
+        cache_plan_kernel<<<2, 1024, 0, stream>>>(a, p.n, p.w, n_plan, w_plan);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     int sets = kXcds;
     while (a.Hkv % sets != 0) sets /= 2;
     const int64_t turns = p.w_items * (a.Hkv / sets), per = kXcds / sets;

@@ -195,7 +195,7 @@ def _check(call: str, status: int) -> None:
 def _need(t: torch.Tensor, shape, dtype=None, name="tensor") -> None:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")

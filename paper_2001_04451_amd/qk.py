@@ -106,9 +106,10 @@ def _check_inputs(cfg: QkConfig, x, gain_q, gain_k, freq, pos) -> QkConfig:
     lsh._need(freq, (cfg.rot // 2,), torch.float32, "freq")
     if pos is not None:
         lsh._need(pos, (cfg.T,), torch.int32, "pos")
+    dev = x.device
     for name, t in (("gain_q", gain_q), ("gain_k", gain_k), ("freq", freq), ("pos", pos)):
-        if t is not None and t.device != x.device:
-            raise ValueError(f"{name} is on {t.device}, x on {x.device}")
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, x on {dev}")
     return cfg
 
 
