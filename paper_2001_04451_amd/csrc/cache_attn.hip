@@ -200,15 +200,20 @@ __device__ bool find_item(const CacheArgs& a, const Split& sp, const int4* __res
             slots += __builtin_amdgcn_readlane(sum2, 63);
         }
     }
-    const int back = at / it.parts;  // the last tile, whose rows see the most, first
+    // the same in all lanes: into scalar registers
+    auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    it.seq = scalar(it.seq);
+    it.parts = scalar(it.parts);
+    at = scalar(at);
+    const int back = scalar(at / it.parts);  // the last tile, whose rows see the most, first
     it.part = at - back * it.parts;
-    it.tile = tiles - 1 - back;
-    it.keys = (keys + it.parts - 1) / it.parts;  // alike parts, in whole steps
-    it.keys = (it.keys + sp.step - 1) / sp.step * sp.step;
-    it.n_rows = rows;
-    it.slot = slot + it.tile * it.parts + it.part;
-    it.first = min(max((int64_t)a.first[it.seq], (int64_t)0), a.T);
-    it.pos0 = (int64_t)a.length[it.seq] - a.first[it.seq + 1] + it.first;
+    it.tile = scalar(tiles) - 1 - back;
+    const int keys_part = scalar((keys + it.parts - 1) / it.parts);  // alike parts, in whole steps
+    it.keys = scalar((keys_part + sp.step - 1) / sp.step * sp.step);
+    it.n_rows = scalar(rows);
+    it.slot = scalar(slot) + it.tile * it.parts + it.part;
+    it.first = min(max((int64_t)scalar(a.first[it.seq]), (int64_t)0), a.T);
+    it.pos0 = (int64_t)scalar(a.length[it.seq]) - scalar(a.first[it.seq + 1]) + it.first;
     return true;
 }
 
@@ -225,6 +230,11 @@ __device__ __forceinline__ QueryRow query_row(const CacheArgs& a, const Item& it
     const int64_t n = it.pos0 + q.token + (shared ? 0 : 1);
     q.limit = r < it.n_rows ? (int)min(max(n, (int64_t)0), (int64_t)cache_cap(a)) : 0;
     return q;
+}
+
+// The limit of a row that is the same for all lanes, in a scalar register.
+__device__ __forceinline__ int row_limit(const CacheArgs& a, const Item& it, int r, int G, int shared) {
+    return __builtin_amdgcn_readfirstlane(query_row(a, it, r, G, shared).limit);
 }
 
 // The query of row r (of the last row, past it).
@@ -443,8 +453,8 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     const int r0 = it.tile * kNarrowRows;
     const QueryRow row = query_row(a, it, r0 + n, G, SHARED);
     const int last = min(r0 + kNarrowRows, it.n_rows) - 1;
-    const int most = query_row(a, it, last, G, SHARED).limit;  // of any row of the tile
-    const int least = query_row(a, it, r0, G, SHARED).limit;
+    const int most = row_limit(a, it, last, G, SHARED);  // of any row of the tile
+    const int least = row_limit(a, it, r0, G, SHARED);
     const int k0 = it.part * it.keys, k1 = min(k0 + it.keys, most);
 
     // The queries' operand: the dimensions of K's in the same order.
@@ -674,12 +684,12 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
         parts.of_seq[it.seq] = make_int2(it.parts, it.slot);  // slot of tile 0, part 0
     if (it.parts > 1 && it.slot >= parts.slots) return;
     const int r0 = it.tile * kRows, rw = r0 + 16 * QT * wave;
-    const int most = query_row(a, it, min(r0 + kRows, it.n_rows) - 1, G, SHARED).limit;
+    const int most = row_limit(a, it, min(r0 + kRows, it.n_rows) - 1, G, SHARED);
     const int k0 = it.part * it.keys, k1 = min(k0 + it.keys, most);
-    const bool active = rw < it.n_rows;
+    const bool active = __builtin_amdgcn_readfirstlane(rw) < it.n_rows;
     // what this wave's rows see: all of them the first `least` keys, none more than `mine`
-    const int mine = active ? query_row(a, it, min(rw + 16 * QT, it.n_rows) - 1, G, SHARED).limit : 0;
-    const int least = active ? query_row(a, it, rw, G, SHARED).limit : 0;
+    const int mine = active ? row_limit(a, it, min(rw + 16 * QT, it.n_rows) - 1, G, SHARED) : 0;
+    const int least = active ? row_limit(a, it, rw, G, SHARED) : 0;
     const float scale_log2e = fabsf(a.scale) * kLog2e;  // a negative scale turns the queries round, which is exact
 
     bf16x8 qop[QT][2];
@@ -943,7 +953,7 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
     // First the blocks that all rows of the workgroup see in full, up to the
     // first hole; then the others, whose keys are tested one by one.  Loops of
     // their own: the choice within one cost 30 registers.
-    const int whole = min(blocks, max(query_row(a, it, r0, G, SHARED).limit - k0, 0) / 64);
+    const int whole = min(blocks, max(row_limit(a, it, r0, G, SHARED) - k0, 0) / 64);
     auto walk = [&](auto fast_tag) {
         while (kb < whole && !hole())
             step([&](int b, int) {
