@@ -10,8 +10,8 @@
  *
  * Rot turns each of the first rot/2 pairs of dimensions (a, b) by the angle
  * pos * freq[p] to (a cos - b sin, a sin + b cos) and leaves dimensions rot
- * and above as they are.  The angle is formed in 64 bits (exactly, up to
- * positions of 2^29), so that far positions keep their phase.
+ * and above as they are.  The angle is formed in 64 bits, so that far
+ * positions keep their phase.
  *
  * Conventions are those of lsh.h (device pointers, caller-owned memory and
  * workspace, asynchronous calls on `stream`, lsh_status results, INVALID and

@@ -5,14 +5,15 @@
 // gfx950 design.  Eight lanes hold a head's 64 values, eight each, so its sums
 // are DPP reductions and its rows leave in 16-byte pieces.  The angles depend
 // on the token alone: a workgroup forms those of its tokens once, in LDS, and
-// all heads share them.  Each is pos * freq in fp64 (an exact product below
-// 2^53), turned into revolutions and reduced there, so only the fraction of a
-// revolution reaches fp32.  A pair's other value is in the same lane
-// (interleaved) or a lane shift away (halves, rot a multiple of 16).
-// HBM-bound: 8 x 32K tokens of 8 heads in bf16 107-115 us forward (4.7-5.0
-// TB/s; a 2 GiB copy reaches 4.8 on this card), 286 backward (4.7), where
-// per-row divisions and one row's loads at a time gave 124 and 287; 64 tokens
-// of 16 heads 3.7 us.
+// all heads share them.  Each is pos * (freq / 2 pi) in fp64, reduced there, so
+// only the fraction of a revolution reaches fp32.  A pair's other value is in
+// the same lane (interleaved) or a lane shift away (halves, rot a multiple of
+// 16).  The backward is held to 128 registers: four waves a SIMD, where three
+// took 315 us.
+// HBM-bound: 8 x 32K tokens of 8 heads in bf16 106 us forward (5.0 TB/s; a
+// 2 GiB copy reaches 4.8 on this card), 282 backward (4.8), where per-row
+// divisions and one row's loads at a time gave 124 and 287; 64 tokens of 16
+// heads 3.9 us.
 #include "common.h"
 #include "launch_cache.h"
 
@@ -38,16 +39,23 @@ struct QkArgs {
 
 __device__ __forceinline__ void form_angles(Angles& A, int64_t t0, int tokens, int pairs, const QkArgs& a,
                                             const float* __restrict__ freq, const int32_t* __restrict__ pos) {
-    for (int i = threadIdx.x; i < tokens * 32; i += blockDim.x) {
-        const int t = i >> 5, p = i & 31;
-        const uint32_t at = (uint32_t)(t0 + t);  // T < 2^31
-        if (p == 0 && a.L > 0) {
-            A.b[t] = (int)(at / (uint32_t)a.L);
-            A.l[t] = (int)(at % (uint32_t)a.L);
+    const uint32_t L = (uint32_t)a.L, b0 = L ? (uint32_t)t0 / L : 0, l0 = L ? (uint32_t)t0 % L : (uint32_t)t0;  // T < 2^31
+    const int p = threadIdx.x & 31;  // a thread keeps to one pair
+    const double f = p < pairs ? (double)freq[p] * 0.15915494309189535 : 0.;  // revolutions a position: / (2 pi)
+    for (int t = threadIdx.x >> 5; t < tokens; t += (int)(blockDim.x >> 5)) {
+        uint32_t b = b0, l = l0 + (uint32_t)t;
+        if (L >= kMaxTokens) {  // one batch entry's end at most lies among the tokens
+            if (l >= L) l -= L, ++b;
+        } else if (L > 0) {
+            b += l / L;
+            l %= L;
+        }
+        if (p == 0) {
+            A.b[t] = (int)b;
+            A.l[t] = (int)l;
         }
         if (p >= pairs) continue;
-        const double where = pos ? (double)pos[at] : (double)(a.L > 0 ? at % (uint32_t)a.L : at);
-        double rev = where * (double)freq[p] * 0.15915494309189535;  // 1 / (2 pi)
+        double rev = (pos ? (double)pos[t0 + t] : (double)l) * f;
         rev -= rint(rev);
         float s, c;
         sincospif((float)(2.0 * rev), &s, &c);
@@ -135,7 +143,9 @@ __device__ __forceinline__ float inv_rms(const float* x, float eps) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
     const float ms = group8_sum(ss) * (1.f / kHeadDim) + eps;
-    return ms > 0.f ? 1.f / sqrtf(ms) : ms == 0.f ? 0.f : ms;
+    const bool tiny = ms < 0x1p-100f;  // the instruction takes subnormals as 0
+    const float r = __builtin_amdgcn_rsqf(tiny ? ms * 0x1p80f : ms) * (tiny ? 0x1p40f : 1.f);  // within 2^-22 of it
+    return ms == 0.f ? 0.f : r;
 }
 
 // Where head h (of H) of the workgroup's token t0 + t starts in q, k and their gradients.
@@ -185,7 +195,10 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a, int tokens_wg, co
                 load8<true>(key ? gk : gq, hh * kHeadDim + 8 * l, g);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = key ? gs[1][e] : gs[0][e];
+                for (int e = 0; e < 8; ++e) g[e] = gs[0][e];
+                if (a.Hk > 0)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[e] = key ? gs[1][e] : gs[0][e];
             }
             const float inv = inv_rms(v[u], a.eps);
 #pragma unroll
@@ -201,12 +214,13 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a, int tokens_wg, co
 // (of up to 32 at a time) so that its part of the gain's gradient stays in
 // registers.  partial: [workgroup][gain row][64].
 template <bool F32, bool INTER, bool PER_HEAD>
-__global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a, const void* __restrict__ x,
-                                                     const float* __restrict__ gq, const float* __restrict__ gk,
-                                                     const float* __restrict__ freq, const int32_t* __restrict__ pos,
-                                                     const float* __restrict__ dq, const float* __restrict__ dk,
-                                                     float* __restrict__ dx, float* __restrict__ partial,
-                                                     int gain_rows) {
+__global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkArgs a, const void* __restrict__ x,
+                                                        const float* __restrict__ gq, const float* __restrict__ gk,
+                                                        const float* __restrict__ freq,
+                                                        const int32_t* __restrict__ pos,
+                                                        const float* __restrict__ dq, const float* __restrict__ dk,
+                                                        float* __restrict__ dx, float* __restrict__ partial,
+                                                        int gain_rows) {
     __shared__ Angles both[2];  // of the batch at hand and of the next
     __shared__ float sums[kGroups][kHeadDim];
     const int l = threadIdx.x & 7, group = threadIdx.x >> 3, H = a.Hq + a.Hk;
