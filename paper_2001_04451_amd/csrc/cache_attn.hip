@@ -479,7 +479,18 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     const bool fast = SHARED && __all(scale_log2e * sqrtf(sum_xor32(sum_xor16(qq))) <= 60.f);
 
     float m = fast ? 0.f : kNegInf, l = 0.f;  // l: this lane's keys
-    f32x4 o[4] = {}, rounded = {};
+    // Weights as two bf16 numbers each (17 bits) where values have more than
+    // four bits: the second product costs these tiles 1-3% (32 sequences of
+    // 32K in 4 bits, 8 query heads a key head, would take 46 us, not 40).
+    constexpr bool kTwo = TYPE != kCacheE2m1;
+    f32x4 o[4] = {}, rest[4] = {}, rounded = {};
+    // (-1, 0) and (0, -1) in registers: as operands of their own, the first was
+    // taken for a -1 of 32 bits.
+    uint32_t minus_lo = 0x0000BF80u, minus_hi = 0xBF800000u;
+    asm("" : "+s"(minus_lo), "+s"(minus_hi));
+    auto less = [](float x, uint32_t w, uint32_t minus) {  // x - one of w (exact: w is x rounded)
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, minus), x, false);
+    };
     uint32_t odd = 0;            // a non-finite value was blanked,
     int edge0 = 0x7FFFFFFF;      // at this position or later
     const int per = ((k1 - k0 + 4 * kStep - 1) / (4 * kStep)) * kStep;  // keys a wave
@@ -567,16 +578,16 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                 const float m1 = fmaxf(m, mt);
                 const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
                 l *= corr;
-                rounded *= corr;
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt) o[dt] *= corr;
+                for (int dt = 0; dt < 4; ++dt) o[dt] *= corr, rest[dt] *= corr;
+                if constexpr (!kTwo) rounded *= corr;
                 m = m1;
             }
             off = m > kNegInf ? m : 0.f;
         }
 #pragma unroll
         for (int t = 0; t < NT; t += 2) {
-            u32x4 pw;
+            u32x4 pw, pr = {};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 f32x4& p = z[t + i];
@@ -588,17 +599,22 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                         p[j] = __builtin_amdgcn_exp2f(SHARED ? p[j] - off : fmaf(p[j], c, -off));
                 }
                 l += (p[0] + p[1]) + (p[2] + p[3]);
-                pw[2 * i] = pack_bf16x2(p[0], p[1]);
-                pw[2 * i + 1] = pack_bf16x2(p[2], p[3]);
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                    const uint32_t w = pack_bf16x2(p[j], p[j + 1]);
+                    pw[2 * i + j / 2] = w;
+                    if constexpr (kTwo)
+                        pr[2 * i + j / 2] = pack_bf16x2(less(p[j], w, minus_lo), less(p[j + 1], w, minus_hi));
+                }
             }
-            const bf16x8 pk = as_bf16x8(pw);
-            rounded = mfma16x16x32(kOnes8, pk, rounded);
+            if constexpr (!kTwo) rounded = mfma16x16x32(kOnes8, as_bf16x8(pw), rounded);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(16 * t, 16 * dt, lane)),
                                  vt_read(V + vt_offset<kSwz>(16 * t + 16, 16 * dt, lane)));
                 if (EDGE && differ) vt = blank(vt, odd);
-                o[dt] = mfma16x16x32(vt, pk, o[dt]);
+                o[dt] = mfma16x16x32(vt, as_bf16x8(pw), o[dt]);
+                if constexpr (kTwo) rest[dt] = mfma16x16x32(vt, as_bf16x8(pr), rest[dt]);
             }
         }
         ++st;
@@ -614,6 +630,13 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
         walk(Tag<false>{});
     while (st < steps) step(Tag<false>{}, Tag<true>{});
     l = sum_xor32(sum_xor16(l));
+    // An infinite value times the rest of a weight may be NaN or of the other
+    // sign; times the weight as rounded it is what counts.
+    if constexpr (kTwo)
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[dt][e] += fabsf(rest[dt][e]) < __builtin_inff() ? rest[dt][e] : 0.f;
     if (__any(odd)) add_odd<TYPE>(a, it.seq, head, edge0, w1, row.limit, g, qrow, o);
 
     // Join the four waves: thread takes row tid / 16 and four dimensions.
@@ -621,7 +644,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     float* const O = reinterpret_cast<float*>(S.Vs[wave]);  // [row][64]
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(O + n * kHeadDim + 16 * dt + 4 * g) = o[dt];
-    if (g == 0) S.stats[wave][n] = f32x4{m, l, rounded[0], 0.f};
+    if (g == 0) S.stats[wave][n] = f32x4{m, l, kTwo ? l : rounded[0], 0.f};
     __syncthreads();
     const int r = tid >> 4, d0 = 4 * (tid & 15);
     if (r0 + r >= it.n_rows) return;
