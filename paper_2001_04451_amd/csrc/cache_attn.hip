@@ -17,7 +17,11 @@
 // Codes are turned to bf16 with their block's scale on the way (exact).  The
 // weights are rounded to bf16, as the matrix cores take them; the output is
 // divided by the sum of the rounded ones (one more product, with ones), so
-// they sum to one, and the log-partition takes the fp32 sum.
+// they sum to one, and the log-partition takes the fp32 sum.  Narrow tiles and
+// short calls, which have the matrix cores to spare, add the product with what
+// the rounding left (a second bf16 number a weight), so that the output has
+// little more than the rounding of its own: of 16 heads over 1K keys 0.0017 of
+// its norm off, where the rounded weights alone leave 0.0024.
 //   narrow  16 rows (decoding, a few tokens): each of four waves walks its own
 //           keys, K rows straight from memory into operand registers, V rows
 //           through an LDS area of its own; the waves are joined at the end.
@@ -438,6 +442,26 @@ struct NarrowShared {
     f32x4 stats[4][kNarrowRows];
 };
 
+// What rounding to bf16 leaves of two weights, as bf16 (16 bits of a weight in all).
+struct Minus {
+    uint32_t lo = 0x0000BF80u, hi = 0xBF800000u;  // (-1, 0) and (0, -1)
+    // In registers: as operands of their own, the first was taken for a -1 of 32 bits.
+    __device__ __forceinline__ Minus() { asm("" : "+s"(lo), "+s"(hi)); }
+    __device__ __forceinline__ uint32_t rest(float p0, float p1, uint32_t w) const {  // w: p0 and p1 rounded
+        const bf16x2 w2 = __builtin_bit_cast(bf16x2, w);  // the differences are exact
+        return pack_bf16x2(__builtin_amdgcn_fdot2_f32_bf16(w2, __builtin_bit_cast(bf16x2, lo), p0, false),
+                           __builtin_amdgcn_fdot2_f32_bf16(w2, __builtin_bit_cast(bf16x2, hi), p1, false));
+    }
+};
+// The products with the weights as rounded and with their rests together.  An
+// infinite value times a rest may be NaN or of the other sign; times the
+// weight as rounded it is what counts.
+__device__ __forceinline__ f32x4 with_rest(f32x4 o, f32x4 rest) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += fabsf(rest[e]) < __builtin_inff() ? rest[e] : 0.f;
+    return o;
+}
+
 template <CacheType TYPE, bool SHARED>
 __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp, const Parts& parts,
                                             const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
@@ -484,13 +508,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     // 32K in 4 bits, 8 query heads a key head, would take 46 us, not 40).
     constexpr bool kTwo = TYPE != kCacheE2m1;
     f32x4 o[4] = {}, rest[4] = {}, rounded = {};
-    // (-1, 0) and (0, -1) in registers: as operands of their own, the first was
-    // taken for a -1 of 32 bits.
-    uint32_t minus_lo = 0x0000BF80u, minus_hi = 0xBF800000u;
-    asm("" : "+s"(minus_lo), "+s"(minus_hi));
-    auto less = [](float x, uint32_t w, uint32_t minus) {  // x - one of w (exact: w is x rounded)
-        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, minus), x, false);
-    };
+    const Minus minus;
     uint32_t odd = 0;            // a non-finite value was blanked,
     int edge0 = 0x7FFFFFFF;      // at this position or later
     const int per = ((k1 - k0 + 4 * kStep - 1) / (4 * kStep)) * kStep;  // keys a wave
@@ -603,8 +621,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                 for (int j = 0; j < 4; j += 2) {
                     const uint32_t w = pack_bf16x2(p[j], p[j + 1]);
                     pw[2 * i + j / 2] = w;
-                    if constexpr (kTwo)
-                        pr[2 * i + j / 2] = pack_bf16x2(less(p[j], w, minus_lo), less(p[j + 1], w, minus_hi));
+                    if constexpr (kTwo) pr[2 * i + j / 2] = minus.rest(p[j], p[j + 1], w);
                 }
             }
             if constexpr (!kTwo) rounded = mfma16x16x32(kOnes8, as_bf16x8(pw), rounded);
@@ -630,13 +647,9 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
         walk(Tag<false>{});
     while (st < steps) step(Tag<false>{}, Tag<true>{});
     l = sum_xor32(sum_xor16(l));
-    // An infinite value times the rest of a weight may be NaN or of the other
-    // sign; times the weight as rounded it is what counts.
     if constexpr (kTwo)
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[dt][e] += fabsf(rest[dt][e]) < __builtin_inff() ? rest[dt][e] : 0.f;
+        for (int dt = 0; dt < 4; ++dt) o[dt] = with_rest(o[dt], rest[dt]);
     if (__any(odd)) add_odd<TYPE>(a, it.seq, head, edge0, w1, row.limit, g, qrow, o);
 
     // Join the four waves: thread takes row tid / 16 and four dimensions.
@@ -688,7 +701,11 @@ struct WideShared {
     uint32_t scales[4][TYPE == kCacheBf16 ? 4 : 64];
 };
 
-template <CacheType TYPE, bool SHARED, int QT>
+struct Weights {
+    bf16x8 rounded, rest;  // (Minus)
+};
+
+template <CacheType TYPE, bool SHARED, int QT, bool TWO>
 __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, const Parts& parts,
                                           const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
                                           float* __restrict__ lse, int items, int sets, uint32_t block,
@@ -739,7 +756,9 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
     }
 
     float m[QT], l[QT];
-    f32x4 o[QT][4], rounded[QT];
+    static_assert(!TWO || QT == 1);
+    const Minus minus;
+    f32x4 o[QT][4], rounded[QT], rest[4] = {};
     uint32_t odd = 0;  // a non-finite value was blanked
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
@@ -850,14 +869,17 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
                 const float m1 = fmaxf(m[qt], mt);
                 const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m[qt] - m1) : 1.f;
                 l[qt] *= corr;
-                rounded[qt] *= corr;
+                if constexpr (!TWO) rounded[qt] *= corr;
+                if constexpr (TWO)
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt) rest[dt] *= corr;
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) o[qt][dt] *= corr;
                 m[qt] = m1;
             }
             off = m[qt] > kNegInf ? m[qt] : 0.f;
         }
-        u32x4 pw;
+        u32x4 pw, pr = {};
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x4 p = z[t];
@@ -869,10 +891,21 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
                     p[j] = __builtin_amdgcn_exp2f(FAST ? p[j] : SHARED ? p[j] - off : fmaf(p[j], scale_log2e, -off));
             }
             l[qt] += (p[0] + p[1]) + (p[2] + p[3]);
-            pw[2 * t] = pack_bf16x2(p[0], p[1]);
-            pw[2 * t + 1] = pack_bf16x2(p[2], p[3]);
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const uint32_t w = pack_bf16x2(p[j], p[j + 1]);
+                pw[2 * t + j / 2] = w;
+                if constexpr (TWO) pr[2 * t + j / 2] = minus.rest(p[j], p[j + 1], w);
+            }
         }
-        return as_bf16x8(pw);
+        return Weights{as_bf16x8(pw), as_bf16x8(pr)};
+    };
+    auto count = [&](int qt, const Weights& p) {
+        if constexpr (!TWO) rounded[qt] = mfma16x16x32(kOnes8, p.rounded, rounded[qt]);
+    };
+    auto product = [&](int qt, int dt, bf16x8 vt, const Weights& p) {
+        o[qt][dt] = mfma16x16x32(vt, p.rounded, o[qt][dt]);
+        if constexpr (TWO) rest[dt] = mfma16x16x32(vt, p.rest, rest[dt]);
     };
 
     // A block that the wave's rows see in full, as a pipeline over units of 32
@@ -880,7 +913,8 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
     // take the next one's scores and the last one's values.
     auto attend_whole = [&](int b, auto fast_tag) {
         constexpr int kUnits = 2 * QT;
-        bf16x8 kop[2][2], vt[4], pk[2];
+        bf16x8 kop[2][2], vt[4];
+        Weights pk[2];
         f32x4 cf[2], cf_next[2], z[2][2];
         load_k(b, 0, kop, cf);
         scores(0, kop, z[0]);
@@ -897,9 +931,9 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
             if (u == QT) cf[0] = cf_next[0], cf[1] = cf_next[1];
             auto values = [&] {
                 const int qt = (u - 1) % QT;
-                rounded[qt] = mfma16x16x32(kOnes8, pk[(u - 1) & 1], rounded[qt]);
+                count(qt, pk[(u - 1) & 1]);
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt) o[qt][dt] = mfma16x16x32(vt[dt], pk[(u - 1) & 1], o[qt][dt]);
+                for (int dt = 0; dt < 4; ++dt) product(qt, dt, vt[dt], pk[(u - 1) & 1]);
             };
             if (QT == 1 && u > 0) values();  // a new maximum rescales this very tile's sums
             if constexpr (SHARED) z[u & 1][0] *= cf[0], z[u & 1][1] *= cf[1];
@@ -910,15 +944,16 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
         if constexpr (QT == 1)
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) vt[dt] = load_v(b, 1, dt);
-        rounded[QT - 1] = mfma16x16x32(kOnes8, pk[1], rounded[QT - 1]);
+        count(QT - 1, pk[1]);
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt) o[QT - 1][dt] = mfma16x16x32(vt[dt], pk[1], o[QT - 1][dt]);
+        for (int dt = 0; dt < 4; ++dt) product(QT - 1, dt, vt[dt], pk[1]);
     };
     // Any block: every key is tested against every row.
     auto attend_edge = [&](int b, int key0, uint32_t hole) {
 #pragma unroll 1
         for (int kp = 0; kp < 2; ++kp) {
-            bf16x8 kop[2][2], pk[QT];
+            bf16x8 kop[2][2];
+            Weights pk[QT];
             f32x4 cf[2];
             load_k(b, kp, kop, cf);
 #pragma unroll
@@ -936,13 +971,13 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
                     }
                 }
                 pk[qt] = weights(qt, z, Tag<false>{}, Tag<true>{});
-                rounded[qt] = mfma16x16x32(kOnes8, pk[qt], rounded[qt]);
+                count(qt, pk[qt]);
             }
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 const bf16x8 vt = blank(load_v(b, kp, dt), odd);
 #pragma unroll
-                for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mfma16x16x32(vt, pk[qt], o[qt][dt]);
+                for (int qt = 0; qt < QT; ++qt) product(qt, dt, vt, pk[qt]);
             }
         }
     };
@@ -997,6 +1032,11 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const float sum = sum_xor32(sum_xor16(l[qt])), top = m[qt];
+        if constexpr (TWO) {
+            rounded[qt][0] = sum;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) o[qt][dt] = with_rest(o[qt][dt], rest[dt]);
+        }
         const int r = 16 * QT * wave + 16 * qt + n;
         if (__any(odd))
             add_odd<TYPE>(a, it.seq, head, edge0, k1, least + (int)(past >> (8 * qt) & 255), g,
@@ -1041,7 +1081,8 @@ __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs
 }
 
 // Chunks, and beside them decoding sequences, in one grid, the chunks' tiles first.
-template <CacheType TYPE, bool SHARED, int QT, int OCC>
+// TWO: weights as two numbers, as in narrow tiles.
+template <CacheType TYPE, bool SHARED, int QT, int OCC, bool TWO>
 __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split narrow, Split wide, Parts np, Parts wp,
                                                               const uint16_t* __restrict__ q,
                                                               uint16_t* __restrict__ out, float* __restrict__ lse,
@@ -1049,8 +1090,8 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
     constexpr size_t kBytes = sizeof(WideShared<TYPE>) > sizeof(NarrowShared) ? sizeof(WideShared<TYPE>) : sizeof(NarrowShared);
     __shared__ __attribute__((aligned(16))) char mem[kBytes];
     if (blockIdx.x < wide_blocks)
-        wide_tile<TYPE, SHARED, QT>(a, wide, wp, q, out, lse, items, sets, blockIdx.x,
-                                    *reinterpret_cast<WideShared<TYPE>*>(mem));
+        wide_tile<TYPE, SHARED, QT, TWO>(a, wide, wp, q, out, lse, items, sets, blockIdx.x,
+                                         *reinterpret_cast<WideShared<TYPE>*>(mem));
     else
         narrow_tile<TYPE, SHARED>(a, narrow, np, q, out, lse, blockIdx.x - wide_blocks,
                                   *reinterpret_cast<NarrowShared*>(mem));
@@ -1133,7 +1174,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narr
 
 // The kernels and splits of a call.
 struct Plan {
-    bool narrow, wide, join, planned;
+    bool narrow, wide, two, join, planned;
     int qt;
     Split n, w;
     int64_t n_items, w_items;  // a head, at most
@@ -1157,6 +1198,10 @@ Plan plan_of(const CacheArgs& a, int max_new) {
         p.qt = a.T * a.H >= 512 * 256 ? 4 : 1;  // 16 heads of 8K 205 / 212 / 233, of 4K 127 / 84 / 73, of 2K 51 / 42 / 35
     else
         p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
+    // Short calls wait for memory and for launches, and take their weights as
+    // two numbers for nothing (24 tokens over 1K 10.5 / 10.6 us, 128 over 8K, 4
+    // heads 16.5 / 16.8); prompts would not (16 heads of 4K 71 / 84).
+    p.two = p.qt == 1 && pairs < 1 << 24;
     auto a_head = [&](int items) { return (items + a.Hkv - 1) / a.Hkv; };
     // with a sequence and head for every CU, short parts are not needed, and short caches no join
     const int shorter = a.n_seq * (int64_t)a.Hkv >= 256 ? 4 * kNarrowStep : kNarrowStep;
@@ -1222,9 +1267,13 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
             kernel<<<wide + narrow, 256, 0, stream>>>(a, p.n, p.w, np, wp, q, out, lse, (int)p.w_items, sets, wide);
         };
         switch (p.qt) {
-            case 4: go(cache_wide_kernel<TYPE, SHARED, 4, 2>); break;
-            case 2: go(cache_wide_kernel<TYPE, SHARED, 2, 2>); break;
-            default: go(cache_wide_kernel<TYPE, SHARED, 1, 3>);
+            case 4: go(cache_wide_kernel<TYPE, SHARED, 4, 2, false>); break;
+            case 2: go(cache_wide_kernel<TYPE, SHARED, 2, 2, false>); break;
+            default:
+                if (p.two)
+                    go(cache_wide_kernel<TYPE, SHARED, 1, 3, TYPE != kCacheE2m1>);
+                else
+                    go(cache_wide_kernel<TYPE, SHARED, 1, 3, false>);
         }
     } else {
         cache_narrow_kernel<TYPE, SHARED><<<narrow, 256, 0, stream>>>(a, p.n, np, q, out, lse);

@@ -55,3 +55,31 @@ def test_infinite_values_of_seen_keys(gpu, shared):  # noqa: F811
     want[0, mine, 5], want[0, mine, 9], want[0, mine, 20], want[1, mine, 63] = np.inf, -np.inf, np.nan, np.inf
     assert torch.equal(lse, want_lse)
     torch.testing.assert_close(out, want, rtol=0, atol=0, equal_nan=True)
+
+
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("type_", ["bf16", "e4m3"])
+def test_weights_of_short_chunks_keep_sixteen_bits(gpu, type_, shared):  # noqa: F811
+    """As for few tokens, and infinite values of keys that all rows of a tile see, or some."""
+    c = Case(type_, shared, 4, 4 if shared else 2, 32, [300, 700], [70, 40], seed=22)
+    host, kr, vr = c.host_pages()
+    log("cache attention precision of chunks", type_, shared)
+    out, _ = cache.lsh_cache_attn_fwd(c.cfg, c.pages(host, gpu), c.seqs(gpu), c.q.to(gpu))
+    inv = None if host[4] is None else host[4].astype(np.float64)
+    ref, _, spread, _ = C.attend(c.q.double().numpy(), kr, vr, inv, c.first, c.lens, c.table, c.page, 0.125, c.shared,
+                                 c.cfg.self_mask)
+    dz = 2 * 70 * 2.0 ** -24 * 64 * np.log(2)
+    tol = (2.0 ** -12 + dz) * spread + 2.0 ** -8 * np.abs(ref)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all()
+    if type_ != "bf16":
+        return
+    for s, p, d, x in ((0, 100, 5, np.inf), (0, 250, 9, -np.inf), (1, 3, 11, np.inf), (1, 500, 11, -np.inf)):
+        c.v[c.table[s, p // 32], 1, p % 32, d] = x
+    host, _, _ = c.host_pages()
+    odd, _ = cache.lsh_cache_attn_fwd(c.cfg, c.pages(host, gpu), c.seqs(gpu), c.q.to(gpu))
+    want, G = out.clone(), c.H // c.Hkv
+    mine = slice(G, 2 * G)
+    want[:70, mine, 5], want[70:, mine, 11] = np.inf, np.nan
+    n = 250 - 230 + (1 if shared else 0)  # new tokens that do not see position 250
+    want[n:70, mine, 9] = -np.inf
+    torch.testing.assert_close(odd, want, rtol=0, atol=0, equal_nan=True)
