@@ -25,10 +25,10 @@
 //   narrow  16 rows (decoding, a few tokens): each of four waves walks its own
 //           keys, K rows straight from memory into operand registers, V rows
 //           through an LDS area of its own; the waves are joined at the end.
-//           Bound by HBM: 64 sequences of up to 16K, 16 heads, e4m3, 124 us
-//           (5.2 TB/s); one of 64K in bf16 45 us (6.0 TB/s), 52 with its join.
+//           Bound by HBM: 64 sequences of up to 16K, 16 heads, e4m3, 127 us
+//           (5.1 TB/s); one of 64K in bf16 45 us (6.0 TB/s), 52 with its join.
 //           Grouped 4-bit caches are bound by the conversions and exp instead
-//           (32 of 32K, 8 query heads a key head: 36 us, 3.9 TB/s).
+//           (32 of 32K, 8 query heads a key head: 35 us, 4.1 TB/s).
 //   wide    64 QT rows (chunks): the four waves share blocks of 64 keys staged
 //           in LDS, double-buffered.  Bound by exp and the other vector
 //           instructions, which fill 59% of a SIMD's time, and by how far two
