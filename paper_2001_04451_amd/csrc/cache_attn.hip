@@ -17,8 +17,8 @@
 // Codes are turned to bf16 with their block's scale on the way (exact).  The
 // weights are rounded to bf16, as the matrix cores take them; the output is
 // divided by the sum of the rounded ones (one more product, with ones), so
-// they sum to one, and the log-partition takes the fp32 sum.  Narrow tiles and
-// short calls, which have the matrix cores to spare, add the product with what
+// they sum to one, and the log-partition takes the fp32 sum.  Narrow tiles
+// (two_narrow) and short calls, which have the matrix cores to spare, add the product with what
 // the rounding left (a second bf16 number a weight), so that the output has
 // little more than the rounding of its own: of 16 heads over 1K keys 0.0017 of
 // its norm off, where the rounded weights alone leave 0.0024.
@@ -462,7 +462,7 @@ __device__ __forceinline__ f32x4 with_rest(f32x4 o, f32x4 rest) {
     return o;
 }
 
-template <CacheType TYPE, bool SHARED>
+template <CacheType TYPE, bool SHARED, bool TWO>
 __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp, const Parts& parts,
                                             const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
                                             float* __restrict__ lse, uint32_t block, NarrowShared& S) {
@@ -503,10 +503,6 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     const bool fast = SHARED && __all(scale_log2e * sqrtf(sum_xor32(sum_xor16(qq))) <= 60.f);
 
     float m = fast ? 0.f : kNegInf, l = 0.f;  // l: this lane's keys
-    // Weights as two bf16 numbers each (17 bits) where values have more than
-    // four bits: the second product costs these tiles 1-3% (32 sequences of
-    // 32K in 4 bits, 8 query heads a key head, would take 46 us, not 40).
-    constexpr bool kTwo = TYPE != kCacheE2m1;
     f32x4 o[4] = {}, rest[4] = {}, rounded = {};
     const Minus minus;
     uint32_t odd = 0;            // a non-finite value was blanked,
@@ -598,7 +594,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                 l *= corr;
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) o[dt] *= corr, rest[dt] *= corr;
-                if constexpr (!kTwo) rounded *= corr;
+                if constexpr (!TWO) rounded *= corr;
                 m = m1;
             }
             off = m > kNegInf ? m : 0.f;
@@ -621,17 +617,17 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                 for (int j = 0; j < 4; j += 2) {
                     const uint32_t w = pack_bf16x2(p[j], p[j + 1]);
                     pw[2 * i + j / 2] = w;
-                    if constexpr (kTwo) pr[2 * i + j / 2] = minus.rest(p[j], p[j + 1], w);
+                    if constexpr (TWO) pr[2 * i + j / 2] = minus.rest(p[j], p[j + 1], w);
                 }
             }
-            if constexpr (!kTwo) rounded = mfma16x16x32(kOnes8, as_bf16x8(pw), rounded);
+            if constexpr (!TWO) rounded = mfma16x16x32(kOnes8, as_bf16x8(pw), rounded);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(16 * t, 16 * dt, lane)),
                                  vt_read(V + vt_offset<kSwz>(16 * t + 16, 16 * dt, lane)));
                 if (EDGE && differ) vt = blank(vt, odd);
                 o[dt] = mfma16x16x32(vt, as_bf16x8(pw), o[dt]);
-                if constexpr (kTwo) rest[dt] = mfma16x16x32(vt, as_bf16x8(pr), rest[dt]);
+                if constexpr (TWO) rest[dt] = mfma16x16x32(vt, as_bf16x8(pr), rest[dt]);
             }
         }
         ++st;
@@ -647,7 +643,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
         walk(Tag<false>{});
     while (st < steps) step(Tag<false>{}, Tag<true>{});
     l = sum_xor32(sum_xor16(l));
-    if constexpr (kTwo)
+    if constexpr (TWO)
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) o[dt] = with_rest(o[dt], rest[dt]);
     if (__any(odd)) add_odd<TYPE>(a, it.seq, head, edge0, w1, row.limit, g, qrow, o);
@@ -657,7 +653,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     float* const O = reinterpret_cast<float*>(S.Vs[wave]);  // [row][64]
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(O + n * kHeadDim + 16 * dt + 4 * g) = o[dt];
-    if (g == 0) S.stats[wave][n] = f32x4{m, l, kTwo ? l : rounded[0], 0.f};
+    if (g == 0) S.stats[wave][n] = f32x4{m, l, TWO ? l : rounded[0], 0.f};
     __syncthreads();
     const int r = tid >> 4, d0 = 4 * (tid & 15);
     if (r0 + r >= it.n_rows) return;
@@ -1071,13 +1067,22 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
 
 // ---- the kernels ----
 
-template <CacheType TYPE, bool SHARED>
+// Whether narrow tiles take their weights as two numbers (16 bits): short
+// calls all do (Plan::two), long ones where values have more than four bits.
+// That costs 1-3% there; 32 sequences of 32K in 4 bits, 8 query heads a key
+// head, would take 46 us, not 40.
+template <CacheType TYPE>
+constexpr bool two_narrow(bool is_short) {
+    return is_short || TYPE != kCacheE2m1;
+}
+
+template <CacheType TYPE, bool SHARED, bool TWO>
 __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
                                                                        const uint16_t* __restrict__ q,
                                                                        uint16_t* __restrict__ out,
                                                                        float* __restrict__ lse) {
     __shared__ __attribute__((aligned(16))) NarrowShared S;
-    narrow_tile<TYPE, SHARED>(a, sp, parts, q, out, lse, blockIdx.x, S);
+    narrow_tile<TYPE, SHARED, TWO>(a, sp, parts, q, out, lse, blockIdx.x, S);
 }
 
 // Chunks, and beside them decoding sequences, in one grid, the chunks' tiles first.
@@ -1093,8 +1098,8 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
         wide_tile<TYPE, SHARED, QT, TWO>(a, wide, wp, q, out, lse, items, sets, blockIdx.x,
                                          *reinterpret_cast<WideShared<TYPE>*>(mem));
     else
-        narrow_tile<TYPE, SHARED>(a, narrow, np, q, out, lse, blockIdx.x - wide_blocks,
-                                  *reinterpret_cast<NarrowShared*>(mem));
+        narrow_tile<TYPE, SHARED, two_narrow<TYPE>(TWO)>(a, narrow, np, q, out, lse, blockIdx.x - wide_blocks,
+                                                         *reinterpret_cast<NarrowShared*>(mem));
 }
 
 // ---- joining split rows ----
@@ -1271,12 +1276,16 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
             case 2: go(cache_wide_kernel<TYPE, SHARED, 2, 2, false>); break;
             default:
                 if (p.two)
-                    go(cache_wide_kernel<TYPE, SHARED, 1, 3, TYPE != kCacheE2m1>);
+                    go(cache_wide_kernel<TYPE, SHARED, 1, 3, true>);
                 else
                     go(cache_wide_kernel<TYPE, SHARED, 1, 3, false>);
         }
     } else {
-        cache_narrow_kernel<TYPE, SHARED><<<narrow, 256, 0, stream>>>(a, p.n, np, q, out, lse);
+        auto go = [&](auto kernel) { kernel<<<narrow, 256, 0, stream>>>(a, p.n, np, q, out, lse); };
+        if (p.two)
+            go(cache_narrow_kernel<TYPE, SHARED, true>);
+        else
+            go(cache_narrow_kernel<TYPE, SHARED, two_narrow<TYPE>(false)>);
     }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.join) {

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("shared", [True, False])
-@pytest.mark.parametrize("type_", ["bf16", "e4m3"])
+@pytest.mark.parametrize("type_", ["bf16", "e4m3", "e2m1"])
 def test_weights_of_few_tokens_keep_sixteen_bits(gpu, type_, shared):  # noqa: F811
     """A weight is off by 2^-16 of it at most (what its bf16 rounding leaves, itself at most 2^-8 of it, is rounded to
     bf16 once more); the sums of up to 700 keys take fewer than 700 roundings of 2^-24 to fp32.  Products, sum and
@@ -58,7 +58,7 @@ def test_infinite_values_of_seen_keys(gpu, shared):  # noqa: F811
 
 
 @pytest.mark.parametrize("shared", [True, False])
-@pytest.mark.parametrize("type_", ["bf16", "e4m3"])
+@pytest.mark.parametrize("type_", ["bf16", "e4m3", "e2m1"])
 def test_weights_of_short_chunks_keep_sixteen_bits(gpu, type_, shared):  # noqa: F811
     """As for few tokens, and infinite values of keys that all rows of a tile see, or some."""
     c = Case(type_, shared, 4, 4 if shared else 2, 32, [300, 700], [70, 40], seed=22)
