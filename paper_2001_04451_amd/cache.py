@@ -176,7 +176,7 @@ def _rows(t: torch.Tensor, cfg: CacheConfig, H: int, name: str, stride: int, dev
         return 0
     if t.stride(2) != 1 or (H > 1 and t.stride(1) != cfg.d):
         raise ValueError(f"{name}'s heads must be contiguous")
-    own = t.stride(0) if cfg.T > 1 else 0
+    own = t.stride(0) if cfg.T > 1 else stride  # of a single row any
     if cfg.T > 1 and own < H * cfg.d:  # also 0, one row for all tokens, which the C call would take for packed rows
         raise ValueError(f"{name} has token stride {own}, its rows have {H * cfg.d} elements")
     if stride not in (0, own):

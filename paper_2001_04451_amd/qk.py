@@ -88,7 +88,7 @@ def _token_rows(t: torch.Tensor, T: int, width: int, name: str, stride: int) -> 
         return 0
     if t.stride(1) != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    own = t.stride(0) if T > 1 else 0
+    own = t.stride(0) if T > 1 else stride  # of a single row any
     if T > 1 and own < width:  # also 0, one row for all tokens, which the C call would take for packed rows
         raise ValueError(f"{name} has row stride {own}, its rows have {width} elements")
     if stride not in (0, own):

@@ -67,3 +67,33 @@ def test_rows_that_share_storage_are_refused(many):
         qk.lsh_qk_norm_rotate_bwd(c, many(W), *gains, None, *grads)
     with pytest.raises(ValueError, match="stride"):
         qk.lsh_qk_norm_rotate_bwd(c, on_gpu(T, W), *gains, None, *grads, dx=many(W))
+
+
+def test_one_row_has_any_stride():
+    """With one token nothing lies a stride away: a configuration that names one for its batches takes a single row, which
+    is passed with that stride, and a view's own does not matter."""
+    fused = on_gpu(4, 12 * 64)
+    cfg = cache.CacheConfig(n_seq=1, T=1, H=4, Hkv=4, n_pages=1, max_pages=1, q_stride=768)
+    row = fused[:1, 256:512].unflatten(1, (4, 64))
+    dev = row.device
+    assert cache._rows(row, cfg, 4, "q", cfg.q_stride, dev) == 768
+    assert cache._rows(on_gpu(1, 4, 64), cfg, 4, "q", cfg.q_stride, dev) == 768
+    assert cache._rows(row, cfg, 4, "k", cfg.k_stride, dev) == 0
+    assert qk._token_rows(fused[:1], 1, 256, "x", 768) == 768
+    assert qk._token_rows(fused[:1, :256], 1, 256, "x", 512) == 512
+    assert qk._token_rows(fused[:1], 1, 256, "x", 0) == 0
+
+
+def test_strides_of_many_rows():
+    """Packed rows, views with their own stride, and one that is not what the configuration says."""
+    fused = on_gpu(T, 12 * 64)
+    cfg, *_ = _cache()
+    view, packed = fused[:, 128:256].unflatten(1, (2, 64)), on_gpu(T, 2, 64)
+    dev = view.device
+    assert cache._rows(view, cfg, 2, "k", 0, dev) == cache._rows(view, cfg, 2, "k", 768, dev) == 768
+    assert cache._rows(packed, cfg, 2, "k", 0, dev) == 0 and cache._rows(packed, cfg, 2, "k", 128, dev) == 128
+    assert qk._token_rows(fused, T, 256, "x", 0) == qk._token_rows(fused, T, 256, "x", 768) == 768
+    assert qk._token_rows(on_gpu(T, W), T, W, "x", 0) == 0 and qk._token_rows(on_gpu(T, W), T, W, "x", W) == W
+    for rows in (lambda: cache._rows(view, cfg, 2, "k", 256, dev), lambda: qk._token_rows(fused, T, 256, "x", 256)):
+        with pytest.raises(ValueError, match="the configuration"):
+            rows()
