@@ -237,7 +237,8 @@ def lsh_cache_attn_fwd(cfg: CacheConfig, pages: Pages, seqs: Sequences, q, out=N
     lsh._need(lse, (cfg.T, cfg.H), torch.float32, "lse")
     if workspace is None:
         workspace = torch.empty(max(workspace_bytes(cfg), 256), dtype=torch.uint8, device=dev)
-    for name, t in (("out", out), ("lse", lse), ("workspace", workspace)):
+    lsh._need_workspace(workspace, dev)
+    for name, t in (("out", out), ("lse", lse)):
         if t.device != dev:
             raise ValueError(f"{name} is on {t.device}, the pages on {dev}")
     with lsh.on_device(dev):

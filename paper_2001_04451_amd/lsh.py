@@ -203,6 +203,13 @@ def _need(t: torch.Tensor, shape, dtype=None, name="tensor") -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
+def _need_workspace(t: torch.Tensor, device) -> None:
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"workspace is on {t.device}, the tensors on {device}")
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+
+
 def workspace_bytes(cfg: Config, dtype: torch.dtype, op: int) -> int:
     code = LSH_BF16 if dtype == torch.bfloat16 else LSH_F32
     return int(lib().lsh_workspace_bytes(ctypes.byref(cfg.c()), code, op))

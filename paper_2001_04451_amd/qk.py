@@ -159,6 +159,7 @@ def lsh_qk_norm_rotate_bwd(cfg: QkConfig, x, gain_q, gain_k, freq, pos, dq, dk=N
     dgain_k = _out(dgain_k, cfg.gain_shape(cfg.Hk), torch.float32, x, "dgain_k") if cfg.Hk else None
     if workspace is None:
         workspace = torch.empty(max(qk_workspace_bytes(cfg), 256), dtype=torch.uint8, device=x.device)
+    lsh._need_workspace(workspace, x.device)
     p = lsh._ptr
     with lsh.on_device(x.device):
         lsh._check("lsh_qk_norm_rotate_bwd",

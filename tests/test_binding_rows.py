@@ -97,3 +97,19 @@ def test_strides_of_many_rows():
     for rows in (lambda: cache._rows(view, cfg, 2, "k", 256, dev), lambda: qk._token_rows(fused, T, 256, "x", 256)):
         with pytest.raises(ValueError, match="the configuration"):
             rows()
+
+
+def test_workspaces_are_device_memory():
+    """A workspace on the host, on another device than the tensors, or of less storage than elements never reaches the library."""
+    cfg, pages, seqs = _cache()
+    q = on_gpu(T, H, 64, dtype=torch.bfloat16)
+    c = qk.QkConfig(T=T, Hq=2, Hk=1)
+    args = (c, on_gpu(T, W), on_gpu(64), on_gpu(64), on_gpu(32), None, on_gpu(T, 2, 64), on_gpu(T, 1, 64))
+    large = 1 << 20
+    host = torch.zeros(large, dtype=torch.uint8)
+    elsewhere = torch.zeros(large, dtype=torch.uint8, device="meta").as_subclass(OnGpu)
+    for bad in (host, elsewhere, on_gpu(1, dtype=torch.uint8).expand(large), on_gpu(large, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            cache.lsh_cache_attn_fwd(cfg, pages, seqs, q, workspace=bad)
+        with pytest.raises(ValueError, match="workspace"):
+            qk.lsh_qk_norm_rotate_bwd(*args, workspace=bad)
