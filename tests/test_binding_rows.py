@@ -102,14 +102,14 @@ def test_strides_of_many_rows():
 def test_workspaces_are_device_memory():
     """A workspace on the host, on another device than the tensors, or of less storage than elements never reaches the library."""
     cfg, pages, seqs = _cache()
-    q = on_gpu(T, H, 64, dtype=torch.bfloat16)
+    q, out, lse = on_gpu(T, H, 64, dtype=torch.bfloat16), on_gpu(T, H, 64, dtype=torch.bfloat16), on_gpu(T, H)
     c = qk.QkConfig(T=T, Hq=2, Hk=1)
-    args = (c, on_gpu(T, W), on_gpu(64), on_gpu(64), on_gpu(32), None, on_gpu(T, 2, 64), on_gpu(T, 1, 64))
+    args = (c, on_gpu(T, W), on_gpu(64), on_gpu(64), on_gpu(32), None, on_gpu(T, 2, 64), on_gpu(T, 1, 64), on_gpu(T, W))
     large = 1 << 20
     host = torch.zeros(large, dtype=torch.uint8)
     elsewhere = torch.zeros(large, dtype=torch.uint8, device="meta").as_subclass(OnGpu)
     for bad in (host, elsewhere, on_gpu(1, dtype=torch.uint8).expand(large), on_gpu(large, dtype=torch.uint8)[::2]):
         with pytest.raises(ValueError, match="workspace"):
-            cache.lsh_cache_attn_fwd(cfg, pages, seqs, q, workspace=bad)
+            cache.lsh_cache_attn_fwd(cfg, pages, seqs, q, out=out, lse=lse, workspace=bad)
         with pytest.raises(ValueError, match="workspace"):
             qk.lsh_qk_norm_rotate_bwd(*args, workspace=bad)
