@@ -149,14 +149,15 @@ class Sequences:
     table: torch.Tensor
 
     def check(self, cfg: CacheConfig, device) -> None:
-        if self.__dict__.get("_checked") is cfg:
+        checked = self.__dict__.get("_checked")
+        if checked is not None and checked[0] is cfg and checked[1] == device:
             return
         for name, shape in (("first", (cfg.n_seq + 1,)), ("length", (cfg.n_seq,)), ("table", (cfg.n_seq, cfg.max_pages))):
             t = getattr(self, name)
             lsh._need(t, shape, torch.int32, name)
             if t.device != device:
                 raise ValueError(f"{name} is on {t.device}, the pages on {device}")
-        object.__setattr__(self, "_checked", cfg)
+        object.__setattr__(self, "_checked", (cfg, device))
 
     def c(self) -> CacheSeqsC:
         return CacheSeqsC(lsh._ptr(self.first), lsh._ptr(self.length), lsh._ptr(self.table))

@@ -113,3 +113,12 @@ def test_workspaces_are_device_memory():
             cache.lsh_cache_attn_fwd(cfg, pages, seqs, q, out=out, lse=lse, workspace=bad)
         with pytest.raises(ValueError, match="workspace"):
             qk.lsh_qk_norm_rotate_bwd(*args, workspace=bad)
+
+
+def test_sequences_are_checked_for_each_device():
+    """One set of sequences and one configuration, over pools of two devices."""
+    cfg, _, seqs = _cache()
+    seqs.check(cfg, torch.device("cpu"))
+    with pytest.raises(ValueError, match="first is on cpu"):
+        seqs.check(cfg, torch.device("cuda:1"))
+    seqs.check(cfg, torch.device("cpu"))
