@@ -44,7 +44,10 @@
  * multiples of 8), out and lse are packed.  Pointers are 16-byte aligned.
  * Supported: d = 64, page a power of two from 16 to 4096,
  * max_pages * page <= 2^30, n_pages * Hkv * page < 2^34, H <= 1024,
- * n_seq <= 2^14, T * H < 2^31 (LSH_ERR_UNSUPPORTED otherwise).
+ * n_seq <= 2^14, T * H < 2^31 (LSH_ERR_UNSUPPORTED otherwise).  A launch has
+ * fewer than 2^32 threads, and a call that needs more is unsupported too: to
+ * write or read, T * Hkv up to 2^28 is always taken; for the attention,
+ * T * H up to 2^27 with n_seq * Hkv up to 2^21.
  */
 #ifndef LSH_CACHE_H
 #define LSH_CACHE_H
@@ -84,7 +87,7 @@ typedef struct lsh_cache_seqs {
     const int32_t *first, *length, *table;
 } lsh_cache_seqs;
 
-/* Bytes of workspace lsh_cache_attn_fwd needs (0 for an invalid configuration). */
+/* Bytes of workspace lsh_cache_attn_fwd needs (0 for a configuration that it does not take). */
 size_t lsh_cache_workspace_bytes(const lsh_cache_config *cfg);
 
 /* The new tokens' rows into the cache: k and v [T][Hkv][64] in dtype (with

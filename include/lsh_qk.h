@@ -30,7 +30,8 @@
  * Sums of squares are formed in fp32: rows with 2^-60 < |x_d| < 2^60 for
  * their largest x_d are exact to fp32 rounding.  A zero row with eps = 0
  * gives zeros.  Supported: d = 64, rot a multiple of 16 up to 64,
- * Hq + Hk <= 1024, T * (Hq + Hk) < 2^31 (LSH_ERR_UNSUPPORTED otherwise).
+ * Hq + Hk <= 1024, T * (Hq + Hk) < 2^31, T <= 2^28 - 16 (LSH_ERR_UNSUPPORTED
+ * otherwise).
  */
 #ifndef LSH_QK_H
 #define LSH_QK_H

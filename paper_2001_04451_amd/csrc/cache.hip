@@ -226,9 +226,10 @@ hipError_t by_type(CacheType type, bool f32, Go go) {
 // Rows a wave: four, whose loads are under way together, where that leaves
 // enough waves to fill the chip.
 bool four_rows(const CacheArgs& a) { return (a.T + 7) / 8 * a.Hkv >= 4096; }
-unsigned row_grid(const CacheArgs& a, int per) {
-    return (unsigned)(((a.T + 7) / 8 * ((2 * a.Hkv + per - 1) / per) + 3) / 4);
+int64_t row_blocks(const CacheArgs& a, int per) {
+    return ((a.T + 7) / 8 * ((2 * a.Hkv + per - 1) / per) + 3) / 4;
 }
+unsigned row_grid(const CacheArgs& a, int per) { return (unsigned)row_blocks(a, per); }
 
 struct GoWrite {
     const CacheArgs& a;
@@ -256,6 +257,8 @@ struct GoRead {
 };
 
 }  // namespace
+
+bool cache_rows_fit(const CacheArgs& a) { return row_blocks(a, four_rows(a) ? 4 : 1) <= kMaxWorkgroups; }
 
 hipError_t launch_cache_write(const CacheArgs& a, CacheType type, bool f32, const void* k, const void* v,
                               hipStream_t stream) {

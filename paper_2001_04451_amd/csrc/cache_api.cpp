@@ -75,7 +75,8 @@ extern "C" {
 
 size_t lsh_cache_workspace_bytes(const lsh_cache_config* cfg) {
     lsh::CacheArgs a;
-    return check_cache(cfg, &a) == LSH_OK ? lsh::cache_attn_workspace_bytes(a, cfg->max_new) : 0;
+    if (check_cache(cfg, &a) != LSH_OK || !lsh::cache_attn_fits(a, cfg->max_new)) return 0;
+    return lsh::cache_attn_workspace_bytes(a, cfg->max_new);
 }
 
 int lsh_cache_write(const lsh_cache_config* cfg, lsh_dtype dtype, const lsh_cache_pages* pages,
@@ -84,6 +85,7 @@ int lsh_cache_write(const lsh_cache_config* cfg, lsh_dtype dtype, const lsh_cach
     LSH_TRY(check_cache(cfg, &a));
     LSH_TRY(check_dtype(dtype));
     LSH_TRY(check_buffers(cfg, pages, seqs, &a));
+    if (!lsh::cache_rows_fit(a)) return LSH_ERR_UNSUPPORTED;
     if (!k || !v || !all_aligned(k, v)) return LSH_ERR_INVALID;
     return status_of(
         lsh::launch_cache_write(a, type_of(cfg), dtype == LSH_F32, k, v, static_cast<hipStream_t>(stream)));
@@ -95,6 +97,7 @@ int lsh_cache_read(const lsh_cache_config* cfg, lsh_dtype dtype, const lsh_cache
     LSH_TRY(check_cache(cfg, &a));
     LSH_TRY(check_dtype(dtype));
     LSH_TRY(check_buffers(cfg, pages, seqs, &a));
+    if (!lsh::cache_rows_fit(a)) return LSH_ERR_UNSUPPORTED;
     if ((!k && !v) || !all_aligned(k, v)) return LSH_ERR_INVALID;
     return status_of(
         lsh::launch_cache_read(a, type_of(cfg), dtype == LSH_F32, k, v, static_cast<hipStream_t>(stream)));
@@ -106,6 +109,7 @@ int lsh_cache_attn_fwd(const lsh_cache_config* cfg, lsh_dtype dtype, const lsh_c
     lsh::CacheArgs a;
     LSH_TRY(check_cache(cfg, &a));
     LSH_TRY(check_dtype(dtype));
+    if (!lsh::cache_attn_fits(a, cfg->max_new)) return LSH_ERR_UNSUPPORTED;
     if (dtype != LSH_BF16) return LSH_ERR_UNSUPPORTED;
     if (cfg->shared_qk && !(cfg->self_mask >= kMinSelfMask)) return LSH_ERR_UNSUPPORTED;
     LSH_TRY(check_buffers(cfg, pages, seqs, &a));

@@ -1184,6 +1184,8 @@ struct Plan {
     Split n, w;
     int64_t n_items, w_items;  // a head, at most
     size_t n_slots, w_slots, bytes;
+    int sets, lanes;              // of wide_tile; of the join, a row
+    int64_t n_wg, w_wg, join_wg;  // workgroups
 };
 
 Plan plan_of(const CacheArgs& a, int max_new) {
@@ -1233,6 +1235,13 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     if (p.wide) size(p.w, rows / p.w.rows + seqs, p.w_items, p.w_slots);
     p.join = p.n_slots + p.w_slots > 0;
     p.bytes = off;
+    p.sets = kXcds;
+    while (a.Hkv % p.sets != 0) p.sets /= 2;
+    const int64_t turns = p.w_items * (a.Hkv / p.sets), per = kXcds / p.sets;
+    p.w_wg = (turns + per - 1) / per * kXcds, p.n_wg = p.n_items * a.Hkv;
+    // Few rows have many parts each, many rows few.
+    p.lanes = a.T * a.H <= 1024 ? 256 : a.T * a.H <= 16384 ? 64 : 16;
+    p.join_wg = p.join ? (a.T * a.H * p.lanes + 255) / 256 : 0;
     return p;
 }
 
@@ -1263,13 +1272,10 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
         cache_plan_kernel<<<2, 1024, 0, stream>>>(a, p.n, p.w, n_plan, w_plan);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    int sets = kXcds;
-    while (a.Hkv % sets != 0) sets /= 2;
-    const int64_t turns = p.w_items * (a.Hkv / sets), per = kXcds / sets;
-    const unsigned wide = (unsigned)((turns + per - 1) / per * kXcds), narrow = (unsigned)(p.n_items * a.Hkv);
+    const unsigned wide = (unsigned)p.w_wg, narrow = (unsigned)p.n_wg;
     if (p.wide) {
         auto go = [&](auto kernel) {
-            kernel<<<wide + narrow, 256, 0, stream>>>(a, p.n, p.w, np, wp, q, out, lse, (int)p.w_items, sets, wide);
+            kernel<<<wide + narrow, 256, 0, stream>>>(a, p.n, p.w, np, wp, q, out, lse, (int)p.w_items, p.sets, wide);
         };
         switch (p.qt) {
             case 4: go(cache_wide_kernel<TYPE, SHARED, 4, 2, false>); break;
@@ -1289,22 +1295,24 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
     }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.join) {
-        // Few rows have many parts each, many rows few.
-        const int64_t rows = a.T * a.H;
-        auto go = [&](auto kernel, int lanes) {
-            kernel<<<(unsigned)((rows * lanes + 255) / 256), 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
+        auto go = [&](auto kernel) {
+            kernel<<<(unsigned)p.join_wg, 256, 0, stream>>>(a, p.n, p.w, p.wide, np, wp, q, out, lse);
         };
-        if (rows <= 1024)
-            go(cache_join_kernel<TYPE, 256>, 256);
-        else if (rows <= 16384)
-            go(cache_join_kernel<TYPE, 64>, 64);
-        else
-            go(cache_join_kernel<TYPE, 16>, 16);
+        switch (p.lanes) {
+            case 256: go(cache_join_kernel<TYPE, 256>); break;
+            case 64: go(cache_join_kernel<TYPE, 64>); break;
+            default: go(cache_join_kernel<TYPE, 16>);
+        }
     }
     return hipGetLastError();
 }
 
 }  // namespace
+
+bool cache_attn_fits(const CacheArgs& a, int max_new) {
+    const Plan p = plan_of(a, max_new);
+    return p.w_wg + p.n_wg <= kMaxWorkgroups && p.join_wg <= kMaxWorkgroups;
+}
 
 size_t cache_attn_workspace_bytes(const CacheArgs& a, int max_new) { return plan_of(a, max_new).bytes; }
 

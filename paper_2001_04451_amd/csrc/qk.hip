@@ -328,6 +328,8 @@ QkArgs args_of(const QkShape& s) {
 
 }  // namespace
 
+bool qk_fits(const QkShape& s) { return (s.T + kMaxTokens - 1) / kMaxTokens <= kMaxWorkgroups; }
+
 size_t qk_workspace_bytes(const QkShape& s) {
     return align256((size_t)bwd_parts(s.T) * gain_rows(s) * kHeadDim * sizeof(float));
 }

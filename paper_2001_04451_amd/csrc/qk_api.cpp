@@ -38,7 +38,7 @@ int check_qk(const lsh_qk_config* c, lsh::QkShape* s) {
     if (c->x_stride > (int64_t)1 << 31 || c->dx_stride > (int64_t)1 << 31) return LSH_ERR_UNSUPPORTED;
     *s = {c->T,  c->L,   c->x_stride ? c->x_stride : packed, c->dx_stride ? c->dx_stride : packed, c->Hq,
           c->Hk, c->rot, c->interleaved != 0,               c->gain_per_head != 0,               c->eps};
-    return LSH_OK;
+    return lsh::qk_fits(*s) ? LSH_OK : LSH_ERR_UNSUPPORTED;
 }
 
 int check_dtype(int dtype) { return dtype == LSH_F32 || dtype == LSH_BF16 ? LSH_OK : LSH_ERR_INVALID; }
