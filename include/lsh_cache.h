@@ -113,10 +113,11 @@ int lsh_cache_read(const lsh_cache_config *cfg, lsh_dtype dtype, const lsh_cache
  *   workspace >= lsh_cache_workspace_bytes(cfg); its contents are free
  * The values of a key that some token of the call may not see never reach
  * that token, whatever they are, nor do slots past a sequence's end.
- * With shared_qk, k_inv has to be what lsh_cache_write stores: weights are
- * taken without a running maximum where keys of length one bound the logits
- * (they are then within 2^-60 and 2^60, so values are meant to be within
- * 2^-60 and 2^60 too: fp32 sums of their products hold those).
+ * Values of up to 2^60 in magnitude never overflow the fp32 sums of weights
+ * times values, however many keys there are; larger finite ones may.  With
+ * shared_qk, k_inv has to be what lsh_cache_write stores: weights are taken
+ * without a running maximum where keys of length one bound the logits
+ * (scale log2(e) |q| <= 30; values below 2^-60 lose bits there).
  * bf16 only. */
 int lsh_cache_attn_fwd(const lsh_cache_config *cfg, lsh_dtype dtype, const lsh_cache_pages *pages,
                        const lsh_cache_seqs *seqs, const void *q, void *out, float *lse, void *workspace,

@@ -51,6 +51,10 @@ constexpr float kNegInf = -__builtin_inff();
 // sums far within fp32, and neither the four lanes of a query nor the sums so
 // far need to be brought into line at every step.
 constexpr float kSlack = 16.f;
+// No running maximum is taken where normalised keys keep every logit (log2)
+// within this: weights are within 2^-30 and 2^30 then, and fp32 holds the sums
+// of 2^30 of them times values of up to 2^60.
+constexpr float kFree = 30.f;
 
 // How the keys are split: rows in (lo, hi] belong to this kernel, in tiles of
 // `rows`; parts are multiples of `step` keys.  Up to `target` items a head,
@@ -499,8 +503,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
         qop[i] = as_bf16x8(x);
     }
     const float scale_log2e = fabsf(a.scale) * kLog2e;
-    // No running maximum where normalised keys keep every logit within 2^-60 and 2^60 of one.
-    const bool fast = SHARED && __all(scale_log2e * sqrtf(sum_xor32(sum_xor16(qq))) <= 60.f);
+    const bool fast = SHARED && __all(scale_log2e * sqrtf(sum_xor32(sum_xor16(qq))) <= kFree);
 
     float m = fast ? 0.f : kNegInf, l = 0.f;  // l: this lane's keys
     f32x4 o[4] = {}, rest[4] = {}, rounded = {};
@@ -978,9 +981,8 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
         }
     };
 
-    // No running maximum where every logit of the workgroup is within 2^-60 and
-    // 2^60 of one: normalised keys bound it by the query's length.
-    const bool fast = SHARED && __syncthreads_and(scale_log2e * sqrtf(biggest) <= 60.f);
+    // for the whole workgroup: normalised keys bound a logit by the query's length
+    const bool fast = SHARED && __syncthreads_and(scale_log2e * sqrtf(biggest) <= kFree);
     if (fast)
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) m[qt] = 0.f;
