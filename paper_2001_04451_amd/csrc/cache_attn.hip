@@ -49,7 +49,9 @@ constexpr float kNegInf = -__builtin_inff();
 // The offset that weights are taken against follows the running maximum only
 // when that has risen by more than this (in log2): weights stay below 2^16,
 // sums far within fp32, and neither the four lanes of a query nor the sums so
-// far need to be brought into line at every step.
+// far need to be brought into line at every step.  Each row's offset moves by
+// that row's maximum alone, so that keys hidden from it do not touch even its
+// rounding.
 constexpr float kSlack = 16.f;
 // No running maximum is taken where normalised keys keep every logit (log2)
 // within this: weights are within 2^-30 and 2^30 then, and fp32 holds the sums
@@ -592,7 +594,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
             if constexpr (!SHARED) mt = mt > kNegInf ? mt * c : mt;
             if (__any(mt > m + kSlack)) {
                 mt = max_xor32(max_xor16(mt));
-                const float m1 = fmaxf(m, mt);
+                const float m1 = mt > m + kSlack ? mt : m;  // for each row by itself (kSlack)
                 const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
                 l *= corr;
 #pragma unroll
@@ -865,7 +867,7 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
             if constexpr (!SHARED) mt = mt > kNegInf ? mt * scale_log2e : mt;
             if (__any(mt > m[qt] + kSlack)) {
                 mt = max_xor32(max_xor16(mt));
-                const float m1 = fmaxf(m[qt], mt);
+                const float m1 = mt > m[qt] + kSlack ? mt : m[qt];  // for each row by itself (kSlack)
                 const float corr = m1 > kNegInf ? __builtin_amdgcn_exp2f(m[qt] - m1) : 1.f;
                 l[qt] *= corr;
                 if constexpr (!TWO) rounded[qt] *= corr;
