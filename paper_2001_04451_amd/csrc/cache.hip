@@ -43,8 +43,7 @@ __device__ __forceinline__ Place place_of(const CacheArgs& a, int per) {
     r.slot = -1;
     r.mine = false;
     if (t0 >= a.T) return r;
-    int s = max(0, seq_of(a.first, a.n_seq, t0));
-    while (s + 1 < a.n_seq && a.first[s + 1] <= r.t) ++s;
+    const int s = seq_from(a.first, a.n_seq, max(0, seq_of(a.first, a.n_seq, t0)), r.t);
     const int64_t end = a.first[s + 1];
     r.mine = r.t < a.T && a.first[s] <= r.t && r.t < end;
     if (r.mine) r.slot = slot_of(a, s, a.length[s] - end + r.t, 0);

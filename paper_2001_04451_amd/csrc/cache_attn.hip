@@ -1125,8 +1125,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, Split narr
     // rows leave whole (with LANES = 256 the workgroup)
     if (t0 >= a.T) return;
     int s = max(seq_of(a.first, a.n_seq, t0), 0);
-    if (LANES == 16)
-        while (s + 1 < a.n_seq && a.first[s + 1] <= t) ++s;
+    if (LANES == 16) s = seq_from(a.first, a.n_seq, s, t);
     if (t >= a.T || t < a.first[s] || t >= a.first[s + 1]) return;
     const int64_t f0 = max((int64_t)a.first[s], (int64_t)0), f1 = min((int64_t)a.first[s + 1], a.T);
     const int rows = (int)(f1 - f0) * G;

@@ -28,6 +28,17 @@ __device__ __forceinline__ int seq_of(const int32_t* __restrict__ first, int n_s
     }
 }
 
+// The same for a row of each lane's own, t, not before the one whose sequence is
+// s: in steps that double and then halve, so that sequences without new tokens
+// between them cost a few loads and not one each.
+__device__ __forceinline__ int seq_from(const int32_t* __restrict__ first, int n_seq, int s, int64_t t) {
+    int step = 1;
+    for (; s + step < n_seq && first[s + step] <= t; step *= 2) s += step;
+    for (step /= 2; step > 0; step /= 2)
+        if (s + step < n_seq && first[s + step] <= t) s += step;
+    return s;
+}
+
 // Index of a position's slot, (page * Hkv + head) * page size + place, or -1.
 __device__ __forceinline__ int64_t slot_of(const CacheArgs& a, int seq, int64_t pos, int head) {
     const int64_t p = pos >> a.page_log2;
