@@ -17,18 +17,21 @@
 // Codes are turned to bf16 with their block's scale on the way (exact).  The
 // weights are rounded to bf16, as the matrix cores take them; the output is
 // divided by the sum of the rounded ones (one more product, with ones), so
-// they sum to one, and the log-partition takes the fp32 sum.  Narrow tiles
-// (two_narrow) and short calls, which have the matrix cores to spare, add the product with what
-// the rounding left (a second bf16 number a weight), so that the output has
-// little more than the rounding of its own: of 16 heads over 1K keys 0.0017 of
-// its norm off, where the rounded weights alone leave 0.0024.
+// they sum to one, and the log-partition takes the fp32 sum.  Tiles of 16 and
+// 64 rows, but for large prompts (Plan::two), add the product with what the
+// rounding left (a second bf16 number a weight), so that the output has little
+// more than the rounding of its own: of 16 heads over 1K keys 0.0017 of its
+// norm off, where the rounded weights alone leave 0.0024.  In tiles of 128 rows
+// that would cost 2-12% (512 tokens over 4K, 16 heads 30.5 / 34 us), in those
+// of 256 the registers that the accumulators of a second product need.
 //   narrow  16 rows (decoding, a few tokens): each of four waves walks its own
 //           keys, K rows straight from memory into operand registers, V rows
 //           through an LDS area of its own; the waves are joined at the end.
 //           Bound by HBM: 64 sequences of up to 16K, 16 heads, e4m3, 127 us
 //           (5.1 TB/s); one of 64K in bf16 45 us (6.0 TB/s), 52 with its join.
 //           Grouped 4-bit caches are bound by the conversions and exp instead
-//           (32 of 32K, 8 query heads a key head: 35 us, 4.1 TB/s).
+//           (32 of 32K, 8 query heads a key head: 46 us with the join; with one
+//           number a weight 40).
 //   wide    64 QT rows (chunks): the four waves share blocks of 64 keys staged
 //           in LDS, double-buffered.  Bound by exp and the other vector
 //           instructions, which fill 59% of a SIMD's time, and by how far two
@@ -468,7 +471,7 @@ __device__ __forceinline__ f32x4 with_rest(f32x4 o, f32x4 rest) {
     return o;
 }
 
-template <CacheType TYPE, bool SHARED, bool TWO>
+template <CacheType TYPE, bool SHARED>
 __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp, const Parts& parts,
                                             const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
                                             float* __restrict__ lse, uint32_t block, NarrowShared& S) {
@@ -508,7 +511,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     const bool fast = SHARED && __all(scale_log2e * sqrtf(sum_xor32(sum_xor16(qq))) <= kFree);
 
     float m = fast ? 0.f : kNegInf, l = 0.f;  // l: this lane's keys
-    f32x4 o[4] = {}, rest[4] = {}, rounded = {};
+    f32x4 o[4] = {}, rest[4] = {};
     const Minus minus;
     uint32_t odd = 0;            // a non-finite value was blanked,
     int edge0 = 0x7FFFFFFF;      // at this position or later
@@ -599,14 +602,13 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                 l *= corr;
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) o[dt] *= corr, rest[dt] *= corr;
-                if constexpr (!TWO) rounded *= corr;
                 m = m1;
             }
             off = m > kNegInf ? m : 0.f;
         }
 #pragma unroll
         for (int t = 0; t < NT; t += 2) {
-            u32x4 pw, pr = {};
+            u32x4 pw, pr;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 f32x4& p = z[t + i];
@@ -622,17 +624,16 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
                 for (int j = 0; j < 4; j += 2) {
                     const uint32_t w = pack_bf16x2(p[j], p[j + 1]);
                     pw[2 * i + j / 2] = w;
-                    if constexpr (TWO) pr[2 * i + j / 2] = minus.rest(p[j], p[j + 1], w);
+                    pr[2 * i + j / 2] = minus.rest(p[j], p[j + 1], w);
                 }
             }
-            if constexpr (!TWO) rounded = mfma16x16x32(kOnes8, as_bf16x8(pw), rounded);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 bf16x8 vt = cat4(vt_read(V + vt_offset<kSwz>(16 * t, 16 * dt, lane)),
                                  vt_read(V + vt_offset<kSwz>(16 * t + 16, 16 * dt, lane)));
                 if (EDGE && differ) vt = blank(vt, odd);
                 o[dt] = mfma16x16x32(vt, as_bf16x8(pw), o[dt]);
-                if constexpr (TWO) rest[dt] = mfma16x16x32(vt, as_bf16x8(pr), rest[dt]);
+                rest[dt] = mfma16x16x32(vt, as_bf16x8(pr), rest[dt]);
             }
         }
         ++st;
@@ -648,9 +649,8 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
         walk(Tag<false>{});
     while (st < steps) step(Tag<false>{}, Tag<true>{});
     l = sum_xor32(sum_xor16(l));
-    if constexpr (TWO)
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt) o[dt] = with_rest(o[dt], rest[dt]);
+    for (int dt = 0; dt < 4; ++dt) o[dt] = with_rest(o[dt], rest[dt]);
     if (__any(odd)) add_odd<TYPE>(a, it.seq, head, edge0, w1, row.limit, g, qrow, o);
 
     // Join the four waves: thread takes row tid / 16 and four dimensions.
@@ -658,7 +658,7 @@ __device__ __forceinline__ void narrow_tile(const CacheArgs& a, const Split& sp,
     float* const O = reinterpret_cast<float*>(S.Vs[wave]);  // [row][64]
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(O + n * kHeadDim + 16 * dt + 4 * g) = o[dt];
-    if (g == 0) S.stats[wave][n] = f32x4{m, l, TWO ? l : rounded[0], 0.f};
+    if (g == 0) S.stats[wave][n] = f32x4{m, l, l, 0.f};
     __syncthreads();
     const int r = tid >> 4, d0 = 4 * (tid & 15);
     if (r0 + r >= it.n_rows) return;
@@ -1071,26 +1071,17 @@ __device__ __forceinline__ void wide_tile(const CacheArgs& a, const Split& sp, c
 
 // ---- the kernels ----
 
-// Whether narrow tiles take their weights as two numbers (16 bits): short
-// calls all do (Plan::two), long ones where values have more than four bits.
-// That costs 1-3% there; 32 sequences of 32K in 4 bits, 8 query heads a key
-// head, would take 46 us, not 40.
-template <CacheType TYPE>
-constexpr bool two_narrow(bool is_short) {
-    return is_short || TYPE != kCacheE2m1;
-}
-
-template <CacheType TYPE, bool SHARED, bool TWO>
+template <CacheType TYPE, bool SHARED>
 __global__ __launch_bounds__(256, kNarrowOcc) void cache_narrow_kernel(CacheArgs a, Split sp, Parts parts,
                                                                        const uint16_t* __restrict__ q,
                                                                        uint16_t* __restrict__ out,
                                                                        float* __restrict__ lse) {
     __shared__ __attribute__((aligned(16))) NarrowShared S;
-    narrow_tile<TYPE, SHARED, TWO>(a, sp, parts, q, out, lse, blockIdx.x, S);
+    narrow_tile<TYPE, SHARED>(a, sp, parts, q, out, lse, blockIdx.x, S);
 }
 
 // Chunks, and beside them decoding sequences, in one grid, the chunks' tiles first.
-// TWO: weights as two numbers, as in narrow tiles.
+// TWO: weights as two numbers, as narrow tiles have them.
 template <CacheType TYPE, bool SHARED, int QT, int OCC, bool TWO>
 __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split narrow, Split wide, Parts np, Parts wp,
                                                               const uint16_t* __restrict__ q,
@@ -1102,7 +1093,7 @@ __global__ __launch_bounds__(256, OCC) void cache_wide_kernel(CacheArgs a, Split
         wide_tile<TYPE, SHARED, QT, TWO>(a, wide, wp, q, out, lse, items, sets, blockIdx.x,
                                          *reinterpret_cast<WideShared<TYPE>*>(mem));
     else
-        narrow_tile<TYPE, SHARED, two_narrow<TYPE>(TWO)>(a, narrow, np, q, out, lse, blockIdx.x - wide_blocks,
+        narrow_tile<TYPE, SHARED>(a, narrow, np, q, out, lse, blockIdx.x - wide_blocks,
                                                          *reinterpret_cast<NarrowShared*>(mem));
 }
 
@@ -1204,14 +1195,17 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     // 64K (2^28) 111 / 118 / 147; 512 over 4K (2^25) 42 / 32 / 36; 24 over 1K, 8
     // heads 13.1 / 11.3 / 10.4.
     const int64_t pairs = a.T * a.H * cap;
-    if (cap < 2 * most / G)  // a whole prompt, half of whose pairs are hidden: parts do not even its tiles out, more tiles do
+    const bool prompt = cap < 2 * most / G;
+    if (prompt)  // a whole prompt, half of whose pairs are hidden: parts do not even its tiles out, more tiles do
         p.qt = a.T * a.H >= 512 * 256 ? 4 : 1;  // 16 heads of 8K 205 / 212 / 233, of 4K 127 / 84 / 73, of 2K 51 / 42 / 35
     else
         p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
-    // Short calls wait for memory and for launches, and take their weights as
-    // two numbers for nothing (24 tokens over 1K 10.5 / 10.6 us, 128 over 8K, 4
-    // heads 16.5 / 16.8); prompts would not (16 heads of 4K 71 / 84).
-    p.two = p.qt == 1 && pairs < 1 << 24;
+    // Weights as one number / as two in tiles of 64 rows (us): chunks wait for
+    // memory (24 tokens over 1K, 8 heads 10.4 / 10.6; 48 over 16K, 16 heads 24.4
+    // / 25.0; 64 over 64K 56.1 / 57.0) and small prompts for launches (512 tokens
+    // of 16 heads 19.4 / 20.0; 1000 28.7 / 29.6), but larger ones for the matrix
+    // cores (1024 19.1 / 20.9; 2048 32.4 / 35.6; 4096 71 / 84).
+    p.two = p.qt == 1 && !(prompt && pairs >= 1 << 24);
     auto a_head = [&](int items) { return (items + a.Hkv - 1) / a.Hkv; };
     // with a sequence and head for every CU, short parts are not needed, and short caches no join
     const int shorter = a.n_seq * (int64_t)a.Hkv >= 256 ? 4 * kNarrowStep : kNarrowStep;
@@ -1290,11 +1284,7 @@ hipError_t launch(const CacheArgs& a, const Plan& p, const uint16_t* q, uint16_t
                     go(cache_wide_kernel<TYPE, SHARED, 1, 3, false>);
         }
     } else {
-        auto go = [&](auto kernel) { kernel<<<narrow, 256, 0, stream>>>(a, p.n, np, q, out, lse); };
-        if (p.two)
-            go(cache_narrow_kernel<TYPE, SHARED, true>);
-        else
-            go(cache_narrow_kernel<TYPE, SHARED, two_narrow<TYPE>(false)>);
+        cache_narrow_kernel<TYPE, SHARED><<<narrow, 256, 0, stream>>>(a, p.n, np, q, out, lse);
     }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.join) {

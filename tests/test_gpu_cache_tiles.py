@@ -243,6 +243,45 @@ def test_prompts_in_tiles_of_64(gpu, lens, type_):  # noqa: F811
     check_sampled(c, gpu, np.unique(np.concatenate([edges, c.rng.integers(0, c.T, 40)])))
 
 
+def large_prompt(c):
+    """The case with a table of 2^24 pairs, less than twice as wide as its new tokens: tiles of 64 rows, one number a weight."""
+    width = -(-(1 << 24) // (c.T * c.H * c.page))
+    c.table = np.concatenate([c.table, np.full((len(c.lens), max(0, width - c.most)), c.n_pages, np.int32)], 1)
+    c.most = max(c.most, width)
+    c.cfg = replace(c.cfg, max_pages=c.most)
+    assert c.most * c.page < 2 * c.T and c.T * c.H < 1 << 17
+    return c
+
+
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("type_", TYPES)
+def test_prompts_in_tiles_of_64_hide_what_follows(gpu, type_, shared):  # noqa: F811
+    """Holes, NaN in hidden rows, and infinities that some rows see; the rows that do not see them keep their bits."""
+    def run(bad):
+        c = Case(type_, shared, 64, 64 if shared else 32, 16, [100, 420], [60, 400], seed=44, fill="nan")
+        c.table[1, 9] = -1
+        for s, p in bad.items():
+            at = c.table[s, p // 16], p % 16
+            c.v[at[0], 1, at[1], 40] = np.inf
+        host, _, _ = c.host_pages()
+        large_prompt(c)
+        return c, *cache.lsh_cache_attn_fwd(c.cfg, c.pages(host, gpu), c.seqs(gpu), c.q.to(gpu))
+
+    bad = {0: 75, 1: 301}  # position of the bad row in each sequence
+    log("cache prompts of 64 rows a tile, bad rows", type_, shared)
+    (c, out, lse), (_, want, want_lse) = run(bad), run({})
+    heads = slice(1, 2) if shared else slice(2, 4)
+    assert torch.equal(lse, want_lse)
+    for s, p in bad.items():
+        n = p - (c.lens[s] - c.news[s]) + (1 if shared else 0)  # new tokens that do not see it
+        wrong = want[c.first[s] + n:c.first[s + 1], heads]  # a block of codes with an infinity reads as NaN
+        wrong[..., slice(40, 41) if type_ == "bf16" else slice(32, 64)] = np.inf if type_ == "bf16" else np.nan
+    torch.testing.assert_close(out, want, rtol=0, atol=0, equal_nan=True)
+    c = Case(type_, shared, 64, 64 if shared else 32, 16, [100, 420], [60, 400], seed=44, fill="nan")
+    c.table[1, 9] = -1
+    check_sampled(large_prompt(c), gpu, np.unique(np.concatenate([[0, 59, 60, 203, 204, 220, 459], c.rng.integers(0, 460, 40)])))
+
+
 # ---- decoding ----
 
 
