@@ -97,8 +97,11 @@ int lsh_cache_write(const lsh_cache_config *cfg, lsh_dtype dtype, const lsh_cach
 
 /* The rows the cache stands for, of each sequence's last first[s+1]-first[s]
  * positions (whole sequences where that is length[s]): k and v [T][Hkv][64]
- * in dtype, rounded once; with shared_qk, k has unit length.  k or v may be
- * NULL. */
+ * in dtype; k or v may be NULL.  With shared_qk, k has unit length (the stored
+ * row times k_inv in fp32, rounded to dtype); the query rows themselves, as
+ * stored, are what a configuration without shared_qk reads from the same pages.
+ * The LSH attention over a context takes those, transposed to lsh.h's
+ * [B][H][L][64]. */
 int lsh_cache_read(const lsh_cache_config *cfg, lsh_dtype dtype, const lsh_cache_pages *pages,
                    const lsh_cache_seqs *seqs, void *k, void *v, void *stream);
 
@@ -113,6 +116,14 @@ int lsh_cache_read(const lsh_cache_config *cfg, lsh_dtype dtype, const lsh_cache
  *   workspace >= lsh_cache_workspace_bytes(cfg); its contents are free
  * The values of a key that some token of the call may not see never reach
  * that token, whatever they are, nor do slots past a sequence's end.
+ * Kernels are chosen by T, H, Hkv, n_seq, max_new and the table's width
+ * max_pages * page (not by what `length` holds, which the host does not see): a
+ * table much wider than its sequences gives short calls the kernels of long
+ * ones.  Weights enter the products with 16 bits; with 8 (bf16) in calls of
+ * T * H * max_pages * page >= 2^24 or T * H >= 2^17 in which a sequence may have
+ * more than 64 rows (new tokens times H / Hkv) or that are whole prompts.  So a
+ * row's last bits may change with the table's width and with the other rows of
+ * its call.
  * Values of up to 2^60 in magnitude never overflow the fp32 sums of weights
  * times values, however many keys there are; larger finite ones may.  With
  * shared_qk, k_inv has to be what lsh_cache_write stores: weights are taken
