@@ -36,8 +36,8 @@
 //           in LDS, double-buffered.  Bound by exp and the other vector
 //           instructions, which fill 59% of a SIMD's time, and by how far two
 //           waves overlap them with the matrix cores (37%): 2K tokens over
-//           32K, 16 heads, e4m3, 310 us (0.86 PFLOP/s; a library matrix
-//           product of 8192^3 reaches 1.12 on this card), 328 with its join.
+//           32K, 16 heads, e4m3, 329 us with its join (0.81 PFLOP/s; a library
+//           matrix product of 8192^3 reaches 1.12 on this card).
 #include "attn_common.h"
 #include "cache_common.h"
 
@@ -1191,13 +1191,13 @@ Plan plan_of(const CacheArgs& a, int max_new) {
     p.wide = most > kNarrowRows;
     // Larger tiles read K and V from LDS less often, but leave fewer of them and
     // need more parts to fill the chip.  Measured, 256 / 128 / 64 rows a tile
-    // (us): 2K tokens over 32K, 16 heads (2^30 pairs) 337 / 434 / 778; 256 over
-    // 64K (2^28) 111 / 118 / 147; 512 over 4K (2^25) 42 / 32 / 36; 24 over 1K, 8
-    // heads 13.1 / 11.3 / 10.4.
+    // (us): 2K tokens over 32K, 16 heads (2^30 pairs) 331 / 581 / 680; 256 over
+    // 64K (2^28) 116 / 122 / 166; 512 over 4K (2^25) 40 / 31 / 38; 24 over 1K, 8
+    // heads 13.2 / 11.4 / 10.7.
     const int64_t pairs = a.T * a.H * cap;
     const bool prompt = cap < 2 * most / G;
     if (prompt)  // a whole prompt, half of whose pairs are hidden: parts do not even its tiles out, more tiles do
-        p.qt = a.T * a.H >= 512 * 256 ? 4 : 1;  // 16 heads of 8K 205 / 212 / 233, of 4K 127 / 84 / 73, of 2K 51 / 42 / 35
+        p.qt = a.T * a.H >= 512 * 256 ? 4 : 1;  // 16 heads of 8K 206 / 207 / 233, of 4K 107 / 78 / 76, of 2K 51 / 41 / 35
     else
         p.qt = most > 128 && pairs >= 1 << 27 ? 4 : most > 64 && pairs >= 1 << 24 ? 2 : 1;
     // Weights as one number / as two in tiles of 64 rows (us): chunks wait for

@@ -10,10 +10,10 @@
 // the same lane (interleaved) or a lane shift away (halves, rot a multiple of
 // 16).  The backward is held to 128 registers: four waves a SIMD, where three
 // took 315 us.
-// HBM-bound: 8 x 32K tokens of 8 heads in bf16 106 us forward (5.0 TB/s; a
-// 2 GiB copy reaches 4.8 on this card), 282 backward (4.8), where per-row
-// divisions and one row's loads at a time gave 124 and 287; 64 tokens of 16
-// heads 3.9 us.
+// HBM-bound: 8 x 32K tokens of 8 heads in bf16 107 us forward (5.0 TB/s; a
+// 2 GiB copy reaches 4.8 on this card), 282 backward with the 7 of its second
+// kernel (4.9 in the first); with per-row divisions and one row's loads at a
+// time both took 5-15% more.  64 tokens of 16 heads 3.9 us.
 #include "common.h"
 #include "launch_cache.h"
 
