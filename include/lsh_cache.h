@@ -36,7 +36,7 @@
  * [0, T), and a position that is negative, past the table, or on a page
  * outside [0, n_pages) has no slot.  A token without a slot is not written,
  * reads as zeros and is no one's key.  Rows of q, k, v, out outside all
- * sequences are neither read nor written.  Two tokens of a call must not
+ * sequences are neither used nor written.  Two tokens of a call must not
  * share a slot in lsh_cache_write.
  *
  * Conventions are those of lsh.h.  Rows of q, k and v are [T][H or Hkv][64]
