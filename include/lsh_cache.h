@@ -37,7 +37,7 @@
  * outside [0, n_pages) has no slot.  A token without a slot is not written,
  * reads as zeros and is no one's key.  Rows of q, k, v, out outside all
  * sequences are neither used nor written.  Two tokens of a call must not
- * share a slot in lsh_cache_write.
+ * share a slot in lsh_cache_write or lsh_cache_append.
  *
  * Conventions are those of lsh.h.  Rows of q, k and v are [T][H or Hkv][64]
  * with q_stride, k_stride, v_stride elements from token to token (0: packed;
@@ -46,13 +46,14 @@
  * max_pages * page <= 2^30, n_pages * Hkv * page < 2^34, H <= 1024,
  * n_seq <= 2^14, T * H < 2^31 (LSH_ERR_UNSUPPORTED otherwise).  A launch has
  * fewer than 2^32 threads, and a call that needs more is unsupported too: to
- * write or read, T * Hkv up to 2^28 is always taken; for the attention,
+ * write or read, T * Hkv up to 2^28 is always taken, to append T up to 2^28 - 16; for the attention,
  * T * H up to 2^27 with n_seq * Hkv up to 2^21.
  */
 #ifndef LSH_CACHE_H
 #define LSH_CACHE_H
 
 #include "lsh.h"
+#include "lsh_qk.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -94,6 +95,27 @@ size_t lsh_cache_workspace_bytes(const lsh_cache_config *cfg);
  * shared_qk, k is given the query rows). */
 int lsh_cache_write(const lsh_cache_config *cfg, lsh_dtype dtype, const lsh_cache_pages *pages,
                     const lsh_cache_seqs *seqs, const void *k, const void *v, void *stream);
+
+/* A projection's rows of the new tokens, normed per head and rotated to their
+ * positions on the way: the queries out, keys and values into the cache; one
+ * call for lsh_qk_norm_rotate_fwd and lsh_cache_write, without positions from
+ * the caller.
+ *   qk    T, Hq and d as cfg's T, H and d; Hk = Hkv, with shared_qk 0; L = 0;
+ *         x_stride, rot, interleaved, gain_per_head and eps as in lsh_qk.h
+ *         (dx_stride is not used)
+ *   x     [T][x_stride] in dtype: a row holds H query heads, Hk key heads and
+ *         Hkv value heads of 64; x_stride 0 (packed) or at least that
+ *   gain_q, gain_k  as in lsh_qk.h, gain_k NULL with shared_qk; both NULL for
+ *         no norm: the heads are only rotated
+ *   freq  [rot / 2], may be NULL for rot = 0
+ *   q     [T][H][64] bf16 with cfg->q_stride (what lsh_cache_attn_fwd takes);
+ *         rows of tokens of no sequence are not written
+ * A token is rotated by its position length - n + i, also where it has no slot
+ * (its keys and values are then not written).  Keys are rounded once, from fp32
+ * to the cache's type (with shared_qk and bf16 pages, to the bits of q). */
+int lsh_cache_append(const lsh_cache_config *cfg, const lsh_qk_config *qk, lsh_dtype dtype,
+                     const lsh_cache_pages *pages, const lsh_cache_seqs *seqs, const void *x, const float *gain_q,
+                     const float *gain_k, const float *freq, void *q, void *stream);
 
 /* The rows the cache stands for, of each sequence's last first[s+1]-first[s]
  * positions (whole sequences where that is length[s]): k and v [T][Hkv][64]

@@ -2,7 +2,7 @@
 rows and attention of new tokens over it.
 
 ``Pages`` holds the pool, ``Sequences`` says which rows are whose;
-``lsh_cache_write``, ``lsh_cache_read`` and ``lsh_cache_attn_fwd`` check shapes
+``lsh_cache_write``, ``lsh_cache_append``, ``lsh_cache_read`` and ``lsh_cache_attn_fwd`` check shapes
 and dtypes, call the C entry point on torch's current stream of the tensors'
 device and raise ``lsh.LshError`` on a non-zero status.
 """
@@ -14,10 +14,11 @@ from dataclasses import dataclass, replace
 
 import torch
 
-from . import lsh
+from . import lsh, qk as _qk
 
 # Every symbol include/lsh_cache.h declares.
-EXPORTED = ("lsh_cache_workspace_bytes", "lsh_cache_write", "lsh_cache_read", "lsh_cache_attn_fwd")
+EXPORTED = ("lsh_cache_workspace_bytes", "lsh_cache_write", "lsh_cache_append", "lsh_cache_read",
+            "lsh_cache_attn_fwd")
 TYPES = {"bf16": 0, "e4m3": 1, "e2m1": 2}
 ROW_BYTES = {"bf16": 128, "e4m3": 64, "e2m1": 32}
 
@@ -50,7 +51,8 @@ def lib() -> ctypes.CDLL:
         L.lsh_cache_workspace_bytes.argtypes, L.lsh_cache_workspace_bytes.restype = [C], ctypes.c_size_t
         L.lsh_cache_write.argtypes = L.lsh_cache_read.argtypes = head + [P, P, P]
         L.lsh_cache_attn_fwd.argtypes = head + [P, P, P, P, ctypes.c_size_t, P]
-        for fn in (L.lsh_cache_write, L.lsh_cache_read, L.lsh_cache_attn_fwd):
+        L.lsh_cache_append.argtypes = [C, ctypes.POINTER(_qk.QkConfigC)] + head[1:] + [P] * 6
+        for fn in (L.lsh_cache_write, L.lsh_cache_append, L.lsh_cache_read, L.lsh_cache_attn_fwd):
             fn.restype = I
         _lib = L
     return _lib
@@ -205,6 +207,42 @@ def lsh_cache_write(cfg: CacheConfig, pages: Pages, seqs: Sequences, k, v) -> No
         lsh._check("lsh_cache_write",
                    lib().lsh_cache_write(cfg.ref(), lsh._dtype_code(k), ctypes.byref(pages.c()),
                                          ctypes.byref(seqs.c()), lsh._ptr(k), lsh._ptr(v), lsh._stream(dev)))
+
+
+def lsh_cache_append(cfg: CacheConfig, qk: _qk.QkConfig, pages: Pages, seqs: Sequences, x, gain_q=None, gain_k=None,
+                     freq=None, q=None):
+    """The queries [T, H, 64] bf16 of a projection's rows x [T, (H + Hk + Hkv) * 64 or more], whose keys and values go
+    into the cache: query and key heads normed (with gains) and rotated to their positions (lsh_cache_append).  Rows of
+    q outside all sequences are left as they are."""
+    pages.check(cfg)
+    dev = pages.k.device
+    seqs.check(cfg, dev)
+    Hk = 0 if cfg.shared_qk else cfg.Hkv
+    if (qk.T, qk.Hq, qk.Hk, qk.L) != (cfg.T, cfg.H, Hk, 0):
+        raise ValueError(f"qk has T, Hq, Hk, L = {(qk.T, qk.Hq, qk.Hk, qk.L)}, expected {(cfg.T, cfg.H, Hk, 0)}")
+    stride = _qk._token_rows(x, cfg.T, (cfg.H + Hk + cfg.Hkv) * cfg.d, "x", qk.x_stride)
+    if stride != qk.x_stride:
+        qk = replace(qk, x_stride=stride)
+    if (gain_k is not None) != (gain_q is not None and Hk > 0):
+        raise ValueError("gain_k goes with gain_q and with keys of their own")
+    for name, t, shape, dtype in (("gain_q", gain_q, qk.gain_shape(cfg.H), torch.float32),
+                                  ("gain_k", gain_k, qk.gain_shape(Hk), torch.float32),
+                                  ("freq", freq, (qk.rot // 2,), torch.float32)):
+        if t is not None:
+            lsh._need(t, shape, dtype, name)
+            if t.device != dev:
+                raise ValueError(f"{name} is on {t.device}, the pages on {dev}")
+    if x.device != dev:
+        raise ValueError(f"x is on {x.device}, the pages on {dev}")
+    if q is None:
+        q = torch.empty((cfg.T, cfg.H, cfg.d), dtype=torch.bfloat16, device=dev)
+    cfg = cfg.strides(q_stride=_rows(q, cfg, cfg.H, "q", cfg.q_stride, dev, torch.bfloat16))
+    with lsh.on_device(dev):
+        lsh._check("lsh_cache_append",
+                   lib().lsh_cache_append(cfg.ref(), qk.ref(), lsh._dtype_code(x), ctypes.byref(pages.c()),
+                                          ctypes.byref(seqs.c()), lsh._ptr(x), lsh._ptr(gain_q), lsh._ptr(gain_k),
+                                          lsh._ptr(freq), lsh._ptr(q), lsh._stream(dev)))
+    return q
 
 
 def lsh_cache_read(cfg: CacheConfig, pages: Pages, seqs: Sequences, dtype: torch.dtype, k=None, v=None):

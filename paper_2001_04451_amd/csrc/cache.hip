@@ -11,6 +11,7 @@
 // 36, 31 and 34 with one row a wave.  Short calls are bound by the chain of
 // loads first -> length -> table -> page (64 tokens 4.4 us).
 #include "cache_common.h"
+#include "qk_common.h"
 
 namespace lsh {
 namespace {
@@ -48,24 +49,6 @@ __device__ __forceinline__ Place place_of(const CacheArgs& a, int per) {
     r.mine = r.t < a.T && a.first[s] <= r.t && r.t < end;
     if (r.mine) r.slot = slot_of(a, s, a.length[s] - end + r.t, 0);
     return r;
-}
-
-// Eight values of a row of fp32 or bf16.
-template <bool F32>
-__device__ __forceinline__ void load8(const void* base, int64_t at, float* x) {
-    if constexpr (F32) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
-        const f32x4 lo = p[0], hi = p[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = lo[e], x[4 + e] = hi[e];
-    } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = __uint_as_float(w[e] << 16);
-            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-        }
-    }
 }
 
 template <CacheType TYPE>
@@ -212,6 +195,84 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a, void* __re
     }
 }
 
+// A projection's rows, normed and rotated on the way (lsh_cache_append): queries
+// out, keys and values into the cache.  A workgroup takes up to sixteen
+// consecutive tokens: finds their slots once, forms the angles of their positions
+// once (as the per-head norm does), and walks over their rows with the tokens
+// innermost, so that a wave's eight rows are of one head and leave as a run of a
+// page.  Keys go from fp32 to their codes in one rounding.
+struct AppendArgs {
+    int64_t x_stride;
+    int Hk, rot, norm, per_head, tokens_log2;  // Hk: key heads in a row, 0 for shared keys
+    float eps;
+};
+
+constexpr int kAppendAtOnce = 2;  // rows of a group whose loads are under way
+
+template <CacheType TYPE, bool F32, bool INTER>
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheArgs a, AppendArgs p, const void* __restrict__ x,
+                                                           const float* __restrict__ gq, const float* __restrict__ gk,
+                                                           const float* __restrict__ freq, uint16_t* __restrict__ q) {
+    __shared__ Angles A;
+    __shared__ int64_t pos[kMaxTokens], slot[kMaxTokens];
+    __shared__ int mine[kMaxTokens];
+    const int64_t t0 = (int64_t)blockIdx.x << p.tokens_log2;
+    const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
+    const int rows = (a.H + p.Hk + a.Hkv) << p.tokens_log2;
+    for (int r0 = 0; r0 < rows; r0 += 32 * kAppendAtOnce) {
+        float v[kAppendAtOnce][8];
+#pragma unroll
+        for (int u = 0; u < kAppendAtOnce; ++u) {
+            if (r0 + 32 * u >= rows) break;
+            const int r = min(r0 + 32 * u + group, rows - 1), h = r >> p.tokens_log2;
+            const int64_t t = min(t0 + (r - (h << p.tokens_log2)), a.T - 1);
+            load8<F32>(x, t * p.x_stride + h * kHeadDim + 8 * l, v[u]);
+        }
+        if (r0 == 0) {  // while the first rows are on their way
+            if (threadIdx.x < 64) {
+                const int s0 = max(0, seq_of(a.first, a.n_seq, t0));
+                const int64_t t = t0 + threadIdx.x;
+                if (threadIdx.x < 1u << p.tokens_log2) {
+                    const int s = seq_from(a.first, a.n_seq, s0, t);
+                    const int64_t end = a.first[s + 1], at = a.length[s] - end + t;
+                    const bool own = t < a.T && a.first[s] <= t && t < end;
+                    mine[threadIdx.x] = own;
+                    pos[threadIdx.x] = at;
+                    slot[threadIdx.x] = own ? slot_of(a, s, at, 0) : -1;
+                }
+            }
+            __syncthreads();
+            const int pair = threadIdx.x & 31;
+            if (pair < p.rot >> 1) {
+                const double f = revolutions(freq[pair]);
+                for (int t = threadIdx.x >> 5; t < 1 << p.tokens_log2; t += 8) form_angle(A, t, pair, (double)pos[t], f);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < kAppendAtOnce; ++u) {
+            if (r0 + 32 * u >= rows) break;
+            const int at = r0 + 32 * u + group, r = min(at, rows - 1), h = r >> p.tokens_log2;
+            const int t = r - (h << p.tokens_log2);
+            const bool on = at < rows && mine[t], value = h >= a.H + p.Hk, key = !value && h >= a.H;
+            const int head = value ? h - a.H - p.Hk : (key ? h - a.H : h);
+            if (!value) {
+                if (p.norm) {
+                    float g[8];
+                    load8<true>(key ? gk : gq, (p.per_head ? head * kHeadDim : 0) + 8 * l, g);
+                    const float inv = inv_rms(v[u], p.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[u][e] = v[u][e] * inv * g[e];
+                }
+                turn<INTER>(v[u], A, t, l, p.rot, 1.f);
+                if (!key && on) store8<false>(q, (t0 + t) * a.q_stride + head * kHeadDim + 8 * l, v[u]);
+            }
+            if (value || key || a.shared)
+                write_row<TYPE>(a, on && slot[t] >= 0 ? slot[t] + ((int64_t)head << a.page_log2) : -1, value, v[u]);
+        }
+    }
+}
+
 template <typename Go>
 hipError_t by_type(CacheType type, bool f32, Go go) {
     switch (type) {
@@ -255,6 +316,24 @@ struct GoRead {
     }
 };
 
+struct GoAppend {
+    const CacheArgs& a;
+    const AppendArgs& p;
+    bool interleaved;
+    const void* x;
+    const float *gq, *gk, *freq;
+    uint16_t* q;
+    hipStream_t stream;
+    template <CacheType TYPE, bool F32>
+    void operator()() const {
+        const unsigned grid = (unsigned)((a.T + (1 << p.tokens_log2) - 1) >> p.tokens_log2);
+        if (interleaved)
+            cache_append_kernel<TYPE, F32, true><<<grid, 256, 0, stream>>>(a, p, x, gq, gk, freq, q);
+        else
+            cache_append_kernel<TYPE, F32, false><<<grid, 256, 0, stream>>>(a, p, x, gq, gk, freq, q);
+    }
+};
+
 }  // namespace
 
 bool cache_rows_fit(const CacheArgs& a) { return row_blocks(a, four_rows(a) ? 4 : 1) <= kMaxWorkgroups; }
@@ -266,6 +345,14 @@ hipError_t launch_cache_write(const CacheArgs& a, CacheType type, bool f32, cons
 
 hipError_t launch_cache_read(const CacheArgs& a, CacheType type, bool f32, void* k, void* v, hipStream_t stream) {
     return by_type(type, f32, GoRead{a, k, v, stream});
+}
+
+hipError_t launch_cache_append(const CacheArgs& a, const QkShape& s, CacheType type, bool f32, const void* x,
+                               const float* gq, const float* gk, const float* freq, uint16_t* q, hipStream_t stream) {
+    AppendArgs p{s.x_stride, s.Hk, s.rot, gq != nullptr, s.per_head, 4, s.eps};
+    // as many tokens a workgroup (sharing its angles) as leave four workgroups a CU
+    while (p.tokens_log2 > 0 && (a.T >> p.tokens_log2) < 1024) --p.tokens_log2;
+    return by_type(type, f32, GoAppend{a, p, s.interleaved != 0, x, gq, gk, freq, q, stream});
 }
 
 }  // namespace lsh

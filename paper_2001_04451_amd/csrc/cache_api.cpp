@@ -65,6 +65,21 @@ int check_buffers(const lsh_cache_config* c, const lsh_cache_pages* p, const lsh
     return LSH_OK;
 }
 
+// The norm and rotation of an append: the cache's heads, in the row's order.
+int check_append(const lsh_cache_config* c, const lsh_qk_config* k, lsh::QkShape* s) {
+    if (!k || k->T != c->T || k->L != 0 || k->Hq != c->H || k->Hk != (c->shared_qk ? 0 : c->Hkv) || k->d != c->d)
+        return LSH_ERR_INVALID;
+    if (k->rot < 0 || k->rot > k->d || k->rot % 2 != 0) return LSH_ERR_INVALID;
+    if (!std::isfinite(k->eps) || k->eps < 0.f) return LSH_ERR_INVALID;
+    if (k->rot % 16 != 0) return LSH_ERR_UNSUPPORTED;
+    const int64_t packed = ((int64_t)k->Hq + k->Hk + c->Hkv) * k->d;
+    if (!stride_ok(k->x_stride, packed)) return LSH_ERR_INVALID;
+    if (k->x_stride > (int64_t)1 << 31 || c->T > ((int64_t)1 << 28) - 16) return LSH_ERR_UNSUPPORTED;
+    *s = {c->T, 0, k->x_stride ? k->x_stride : packed, 0, k->Hq, k->Hk, k->rot, k->interleaved != 0,
+          k->gain_per_head != 0, k->eps};
+    return LSH_OK;
+}
+
 int check_dtype(int dtype) { return dtype == LSH_F32 || dtype == LSH_BF16 ? LSH_OK : LSH_ERR_INVALID; }
 
 lsh::CacheType type_of(const lsh_cache_config* c) { return static_cast<lsh::CacheType>(c->type); }
@@ -89,6 +104,22 @@ int lsh_cache_write(const lsh_cache_config* cfg, lsh_dtype dtype, const lsh_cach
     if (!k || !v || !all_aligned(k, v)) return LSH_ERR_INVALID;
     return status_of(
         lsh::launch_cache_write(a, type_of(cfg), dtype == LSH_F32, k, v, static_cast<hipStream_t>(stream)));
+}
+
+int lsh_cache_append(const lsh_cache_config* cfg, const lsh_qk_config* qk, lsh_dtype dtype,
+                     const lsh_cache_pages* pages, const lsh_cache_seqs* seqs, const void* x, const float* gain_q,
+                     const float* gain_k, const float* freq, void* q, void* stream) {
+    lsh::CacheArgs a;
+    lsh::QkShape s;
+    LSH_TRY(check_cache(cfg, &a));
+    LSH_TRY(check_append(cfg, qk, &s));
+    LSH_TRY(check_dtype(dtype));
+    LSH_TRY(check_buffers(cfg, pages, seqs, &a));
+    if (!x || !q || (s.rot > 0 && !freq) || !all_aligned(x, q, gain_q, gain_k)) return LSH_ERR_INVALID;
+    // gains for all turned heads or for none
+    if (s.Hk > 0 ? !gain_q != !gain_k : gain_k != nullptr) return LSH_ERR_INVALID;
+    return status_of(lsh::launch_cache_append(a, s, type_of(cfg), dtype == LSH_F32, x, gain_q, gain_k, freq,
+                                              static_cast<uint16_t*>(q), static_cast<hipStream_t>(stream)));
 }
 
 int lsh_cache_read(const lsh_cache_config* cfg, lsh_dtype dtype, const lsh_cache_pages* pages,

@@ -134,6 +134,37 @@ __device__ __forceinline__ float group8_max(float x) {
     return fmaxf(x, dpp_f32<kDppHalfMirror>(x));
 }
 
+// Eight consecutive values of fp32 or bf16 from 16-byte aligned memory, and to it.
+template <bool F32>
+__device__ __forceinline__ void load8(const void* base, int64_t at, float* x) {
+    if constexpr (F32) {
+        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
+        const f32x4 lo = p[0], hi = p[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = lo[e], x[4 + e] = hi[e];
+    } else {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(w[e] << 16);
+            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        }
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void store8(void* base, int64_t at, const float* x) {
+    if constexpr (F32) {
+        f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(base) + at);
+        p[0] = f32x4{x[0], x[1], x[2], x[3]};
+        p[1] = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(base) + at) = w;
+    }
+}
+
 __device__ __forceinline__ float wave_max(float x) {
     for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
     return x;

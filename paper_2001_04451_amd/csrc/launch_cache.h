@@ -46,6 +46,9 @@ bool cache_rows_fit(const CacheArgs& a);  // the grid of a write or a read
 hipError_t launch_cache_write(const CacheArgs& a, CacheType type, bool f32, const void* k, const void* v,
                               hipStream_t stream);
 hipError_t launch_cache_read(const CacheArgs& a, CacheType type, bool f32, void* k, void* v, hipStream_t stream);
+// Rows of s.Hk key heads (none with shared keys) between the H query and the Hkv value heads.
+hipError_t launch_cache_append(const CacheArgs& a, const QkShape& s, CacheType type, bool f32, const void* x,
+                               const float* gq, const float* gk, const float* freq, uint16_t* q, hipStream_t stream);
 
 bool cache_attn_fits(const CacheArgs& a, int max_new);
 size_t cache_attn_workspace_bytes(const CacheArgs& a, int max_new);

@@ -1,0 +1,48 @@
+// Launchers behind lsh_w4.h.  Arguments are already validated (w4_api.cpp);
+// every launcher only enqueues work on `stream`.
+#pragma once
+
+#include "launch_cache.h"
+
+namespace lsh {
+
+// Packed weights: tiles of 16 outputs x 128 inputs, a row of tiles after the
+// other.  A tile's codes are 64 x 16 bytes, piece l those of output l % 16: for
+// i of 0 .. 3 a word with inputs 32 i + 8 (l / 16) .. + 7, the operand of lane l
+// for one 16 x 16 x 32 product, so that a wave's load is 1 KB without gaps.
+// Its scales are [16][per_tile] (per_tile = 128 / group), its zero points
+// likewise.  Outputs past N and inputs past K hold codes of 0 and scales of 0.
+struct W4Shape {
+    int N, K, e2m1, group, zeros;
+    int64_t tiles_n, tiles_k;  // ceil(N / 16), ceil(K / 128)
+    __host__ __device__ int per_tile() const { return 128 / group; }
+    __host__ __device__ size_t scale_bytes() const { return e2m1 ? 1 : 2; }
+    __host__ __device__ size_t codes_size() const { return (size_t)(tiles_n * tiles_k) * 1024; }
+    __host__ __device__ size_t scales_size() const {
+        return ((size_t)(tiles_n * tiles_k) * 16 * per_tile() * scale_bytes() + 255) & ~(size_t)255;
+    }
+    size_t zeros_size() const { return zeros ? align256((size_t)(tiles_n * tiles_k) * 16 * per_tile()) : 0; }
+    size_t bytes() const { return codes_size() + scales_size() + zeros_size(); }
+};
+
+struct W4Call {
+    int64_t M, a_stride;
+    const uint16_t* a;
+    const char* packed;
+    const float *bias, *resid;
+    float sign;
+    int relu;
+    float* out_f32;
+    uint16_t* out_bf16;
+};
+
+hipError_t launch_w4_quantize(const W4Shape& s, bool f32, const void* w, char* packed, hipStream_t stream);
+hipError_t launch_w4_pack(const W4Shape& s, const uint8_t* codes, const void* scales, const uint8_t* zeros,
+                          char* packed, hipStream_t stream);
+hipError_t launch_w4_unpack(const W4Shape& s, bool f32, const char* packed, void* w, hipStream_t stream);
+
+bool w4_fits(const W4Shape& s, int64_t M);
+size_t w4_workspace_bytes(const W4Shape& s, int64_t M);
+hipError_t launch_linear_w4(const W4Shape& s, const W4Call& c, void* workspace, hipStream_t stream);
+
+}  // namespace lsh

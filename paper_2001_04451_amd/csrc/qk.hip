@@ -14,21 +14,14 @@
 // 2 GiB copy reaches 4.8 on this card), 282 backward with the 7 of its second
 // kernel (4.9 in the first); with per-row divisions and one row's loads at a
 // time both took 5-15% more.  64 tokens of 16 heads 3.9 us.
-#include "common.h"
 #include "launch_cache.h"
+#include "qk_common.h"
 
 namespace lsh {
 namespace {
 
-constexpr int kMaxTokens = 16;  // whose angles a workgroup holds at a time
 constexpr int kGroups = 32;     // eight-lane groups of a workgroup
 constexpr int kAtOnce = 2;      // rows of a group whose loads are under way
-
-struct Angles {
-    float c[kMaxTokens][32];
-    float s[kMaxTokens][32];
-    int b[kMaxTokens], l[kMaxTokens];  // batch entry and position in it (L > 0)
-};
 
 struct QkArgs {
     int64_t T, L, x_stride, dx_stride;
@@ -41,7 +34,7 @@ __device__ __forceinline__ void form_angles(Angles& A, int64_t t0, int tokens, i
                                             const float* __restrict__ freq, const int32_t* __restrict__ pos) {
     const uint32_t L = (uint32_t)a.L, b0 = L ? (uint32_t)t0 / L : 0, l0 = L ? (uint32_t)t0 % L : (uint32_t)t0;  // T < 2^31
     const int p = threadIdx.x & 31;  // a thread keeps to one pair
-    const double f = p < pairs ? (double)freq[p] * 0.15915494309189535 : 0.;  // revolutions a position: / (2 pi)
+    const double f = p < pairs ? revolutions(freq[p]) : 0.;
     for (int t = threadIdx.x >> 5; t < tokens; t += (int)(blockDim.x >> 5)) {
         uint32_t b = b0, l = l0 + (uint32_t)t;
         if (L >= kMaxTokens) {  // one batch entry's end at most lies among the tokens
@@ -55,97 +48,8 @@ __device__ __forceinline__ void form_angles(Angles& A, int64_t t0, int tokens, i
             A.l[t] = (int)l;
         }
         if (p >= pairs) continue;
-        double rev = (pos ? (double)pos[t0 + t] : (double)l) * f;
-        rev -= rint(rev);
-        float s, c;
-        sincospif((float)(2.0 * rev), &s, &c);
-        A.c[t][p] = c;
-        A.s[t][p] = s;
+        form_angle(A, t, p, pos ? (double)pos[t0 + t] : (double)l, f);
     }
-}
-
-// Eight values of a row.
-template <bool F32>
-__device__ __forceinline__ void load8(const void* base, int64_t at, float* x) {
-    if constexpr (F32) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
-        const f32x4 lo = p[0], hi = p[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = lo[e], x[4 + e] = hi[e];
-    } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = __uint_as_float(w[e] << 16);
-            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-        }
-    }
-}
-template <bool F32>
-__device__ __forceinline__ void store8(void* base, int64_t at, const float* x) {
-    if constexpr (F32) {
-        f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(base) + at);
-        p[0] = f32x4{x[0], x[1], x[2], x[3]};
-        p[1] = f32x4{x[4], x[5], x[6], x[7]};
-    } else {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(base) + at) = w;
-    }
-}
-
-// A lane's eight dimensions (8 l ..) turned by the angles of token t (by their
-// negatives for sign = -1).  All eight lanes of the group take part.
-template <bool INTER>
-__device__ __forceinline__ void turn(float* y, const Angles& A, int t, int l, int rot, float sign) {
-    if constexpr (INTER) {
-        if (8 * l >= rot) return;
-        const f32x4 c = *reinterpret_cast<const f32x4*>(&A.c[t][4 * l]);
-        const f32x4 s = *reinterpret_cast<const f32x4*>(&A.s[t][4 * l]);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const float a = y[2 * p], b = y[2 * p + 1], sn = sign * s[p];
-            y[2 * p] = a * c[p] - b * sn;
-            y[2 * p + 1] = a * sn + b * c[p];
-        }
-    } else {
-        const int hl = rot >> 4;  // lanes in half of the turned dimensions
-        const bool low = l < hl, in = l < 2 * hl;
-        float z[8];
-        if (hl == 4) {  // lane l ^ 4: the banks of four lanes trade places by moves within their row
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int x = __float_as_int(y[e]);
-                const int up = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xF, 0x5, false);  // banks 0, 2: from l + 4
-                z[e] = __int_as_float(__builtin_amdgcn_update_dpp(up, x, 0x114, 0xF, 0xA, false));  // 1, 3: from l - 4
-            }
-        } else if (hl == 2) {  // lane l ^ 2
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = dpp_f32<kDppXor2>(y[e]);
-        } else {
-            const int other = (threadIdx.x & 63) + (in ? (low ? hl : -hl) : 0);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other);
-        }
-        if (!in) return;
-        const int p0 = 8 * (low ? l : l - hl);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float sn = low ? -sign * A.s[t][p0 + e] : sign * A.s[t][p0 + e];
-            y[e] = y[e] * A.c[t][p0 + e] + z[e] * sn;
-        }
-    }
-}
-
-__device__ __forceinline__ float inv_rms(const float* x, float eps) {
-    float ss = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-    const float ms = group8_sum(ss) * (1.f / kHeadDim) + eps;
-    const bool tiny = ms < 0x1p-100f;  // the instruction takes subnormals as 0
-    const float r = __builtin_amdgcn_rsqf(tiny ? ms * 0x1p80f : ms) * (tiny ? 0x1p40f : 1.f);  // within 2^-22 of it
-    return ms == 0.f ? 0.f : r;
 }
 
 // Where head h (of H) of the workgroup's token t0 + t starts in q, k and their gradients.
