@@ -40,7 +40,7 @@
  *   bias     [N] fp32 or NULL
  *   resid    [M][N] fp32 or NULL, out_f32 [M][N] fp32, out_bf16 [M][N] bf16
  * Every pointer is 16-byte aligned, packed 256.  Supported: K a multiple of
- * 32 up to 2^17, N up to 2^22, M N < 2^31, M <= 2^24, a_stride <= 2^31
+ * 32 up to 2^17, N up to 2^22, N K < 2^35, M N < 2^31, M <= 2^21, a_stride <= 2^31
  * (LSH_ERR_UNSUPPORTED otherwise).
  */
 #ifndef LSH_W4_H

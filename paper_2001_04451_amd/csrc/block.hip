@@ -111,21 +111,6 @@ struct GemmArgs {
     uint16_t* out_bf16;     // kOutReluBf16: [M][N]; kOutHeads: [B][H][L][64]
 };
 
-// Raw buffer descriptor (word 3: raw, untyped 32-bit data).
-__device__ __forceinline__ u32x4 raw_buffer(const void* p, uint64_t bytes) {
-    const uint64_t a = (uint64_t)p;
-    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), bytes >= 0xFFFFFFFFull ? 0xFFFFFFFFu : (uint32_t)bytes, 0x00020000u};
-}
-
-// 16 bytes per lane from the buffer at byte v_off + s_off straight to LDS at
-// lds + 16 * lane.  Inline assembly, so that the compiler neither orders LDS
-// reads behind it nor waits for it: the kernel counts its own loads.
-__device__ __forceinline__ void buffer_to_lds(u32x4 buf, uint32_t v_off, uint32_t s_off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(v_off), "s"(buf),
-                 "s"(s_off), "s"(lds)
-                 : "memory", "m0");
-}
-
 // Shape of one product kernel: a workgroup of four waves computes a TM x TN
 // tile of C, each wave a quarter of TM / 2 x TN / 2 as 16 x 16 products.  A and
 // W pass through LDS in stages of KB k-values, STAGES of them in flight.

@@ -10,8 +10,9 @@ namespace lsh {
 // other.  A tile's codes are 64 x 16 bytes, piece l those of output l % 16: for
 // i of 0 .. 3 a word with inputs 32 i + 8 (l / 16) .. + 7, the operand of lane l
 // for one 16 x 16 x 32 product, so that a wave's load is 1 KB without gaps.
-// Its scales are [16][per_tile] (per_tile = 128 / group), its zero points
-// likewise.  Outputs past N and inputs past K hold codes of 0 and scales of 0.
+// Its INT4 scales and zero points are [per_tile][16] (per_tile = 128 / group),
+// its E2M1 scales [16][4].  Outputs past N and inputs past K hold codes of 0 and
+// scales of 0.
 struct W4Shape {
     int N, K, e2m1, group, zeros;
     int64_t tiles_n, tiles_k;  // ceil(N / 16), ceil(K / 128)
@@ -21,7 +22,9 @@ struct W4Shape {
     __host__ __device__ size_t scales_size() const {
         return ((size_t)(tiles_n * tiles_k) * 16 * per_tile() * scale_bytes() + 255) & ~(size_t)255;
     }
-    size_t zeros_size() const { return zeros ? align256((size_t)(tiles_n * tiles_k) * 16 * per_tile()) : 0; }
+    __host__ __device__ size_t zeros_size() const {
+        return zeros ? ((size_t)(tiles_n * tiles_k) * 16 * per_tile() + 255) & ~(size_t)255 : 0;
+    }
     size_t bytes() const { return codes_size() + scales_size() + zeros_size(); }
 };
 
@@ -41,7 +44,6 @@ hipError_t launch_w4_pack(const W4Shape& s, const uint8_t* codes, const void* sc
                           char* packed, hipStream_t stream);
 hipError_t launch_w4_unpack(const W4Shape& s, bool f32, const char* packed, void* w, hipStream_t stream);
 
-bool w4_fits(const W4Shape& s, int64_t M);
 size_t w4_workspace_bytes(const W4Shape& s, int64_t M);
 hipError_t launch_linear_w4(const W4Shape& s, const W4Call& c, void* workspace, hipStream_t stream);
 

@@ -8,8 +8,10 @@
 // itself; the group's sum of products is scaled afterwards in fp32,
 //   s (sum a c - z sum a),
 // with sum a from a product with ones, which lands where the sum of a c does.
-#include "common.h"
+#include "attn_common.h"
 #include "launch_w4.h"
+
+#include <type_traits>
 
 namespace lsh {
 namespace {
@@ -46,103 +48,364 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Scales (as fp32) and zero points of a lane's output in one tile.
-template <int PT>
-struct Scales {
-    float s[PT], z[PT];
-    __device__ __forceinline__ void load(const W4Args& g, int64_t tile, int n) {
-        const int64_t at = (tile * 16 + n) * PT;
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(g.scales) + at;
-#pragma unroll
-        for (int i = 0; i < PT; ++i) s[i] = bf16_bits_to_f32(p[i]);
-#pragma unroll
-        for (int i = 0; i < PT; ++i) z[i] = g.zeros ? (float)g.zeros[at + i] : 8.f;
+__device__ __forceinline__ bf16x8 all_of(uint32_t bf16) {
+    const uint32_t p = bf16 | bf16 << 16;
+    return from_pairs(p, p, p, p);
+}
+constexpr f32x4 kNone = {0.f, 0.f, 0.f, 0.f};
+
+// A lane's piece of a tile's codes; with E2M1 the scale bytes of its output.
+template <bool E2M1>
+struct Codes {
+    u32x4 w;
+    uint32_t bytes;
+    __device__ __forceinline__ void load(const W4Args& g, int64_t tile, int lane) {
+        w = *reinterpret_cast<const u32x4*>(g.codes + tile * 1024 + 16 * lane);
+        if constexpr (E2M1) bytes = *reinterpret_cast<const uint32_t*>(g.scales + tile * 64 + 4 * (lane & 15));
+    }
+    // Step i's eight weights, scaled (E2M1) or as codes.
+    __device__ __forceinline__ bf16x8 step(int i) const {
+        if constexpr (E2M1)
+            return e2m1_values(w[i], (bytes >> (8 * i)) & 255u);
+        else
+            return int4_codes(w[i]);
     }
 };
 
-__device__ __forceinline__ void put(const W4Args& g, int64_t m, int n, float v) {
-    if (m >= g.c.M || n >= g.s.N) return;
-    const int64_t at = m * g.s.N + n;
-    if (g.c.bias) v += g.c.bias[n];
-    if (g.c.out_f32)
-        g.c.out_f32[at] = fmaf(g.c.sign, v, g.c.resid ? g.c.resid[at] : 0.f);
-    else
-        g.c.out_bf16[at] = (uint16_t)f32_to_bf16_bits(g.c.relu && v < 0.f ? 0.f : v);
+// INT4's scales and zero points.  Products take the weights first, so that a lane
+// ends up with outputs 4 q .. + 3 of row l % 16 (q = l / 16): the scales of these.
+__device__ __forceinline__ f32x4 four_bf16(uint2 s) {
+    return f32x4{__uint_as_float(s.x << 16), __uint_as_float(s.x & 0xFFFF0000u), __uint_as_float(s.y << 16),
+                 __uint_as_float(s.y & 0xFFFF0000u)};
+}
+__device__ __forceinline__ f32x4 four_bytes(uint32_t z) {
+    return f32x4{(float)(z & 255u), (float)((z >> 8) & 255u), (float)((z >> 16) & 255u), (float)(z >> 24)};
+}
+template <bool ZEROS, int PT>
+struct Scales {
+    uint2 s[PT];
+    uint32_t z[PT];
+    __device__ __forceinline__ void load(const W4Args& g, int64_t tile, int lane) {
+#pragma unroll
+        for (int p = 0; p < PT; ++p) {
+            s[p] = *reinterpret_cast<const uint2*>(g.scales + (tile * PT + p) * 32 + 8 * (lane >> 4));
+            if constexpr (ZEROS) z[p] = *reinterpret_cast<const uint32_t*>(g.zeros + (tile * PT + p) * 16 + 4 * (lane >> 4));
+        }
+    }
+    __device__ __forceinline__ f32x4 scale(int p) const { return four_bf16(s[p]); }
+    __device__ __forceinline__ f32x4 zero(int p) const {
+        if constexpr (ZEROS) return four_bytes(z[p]);
+        return f32x4{8.f, 8.f, 8.f, 8.f};
+    }
+};
+
+// Four outputs n .. n + 3 of row m.
+__device__ __forceinline__ void put4(const W4Args& g, int64_t m, int n, f32x4 v) {
+    const int N = g.s.N;
+    if (m >= g.c.M || n >= N) return;
+    const int64_t at = m * N + n;
+    if ((N & 3) == 0) {  // then n + 3 < N and the four are aligned
+        if (g.c.bias) v += *reinterpret_cast<const f32x4*>(g.c.bias + n);
+        if (g.c.out_f32) {
+            f32x4 r = g.c.resid ? *reinterpret_cast<const f32x4*>(g.c.resid + at) : kNone;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = fmaf(g.c.sign, v[e], r[e]);
+            *reinterpret_cast<f32x4*>(g.c.out_f32 + at) = r;
+        } else {
+            if (g.c.relu)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+            *reinterpret_cast<uint2*>(g.c.out_bf16 + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (n + e >= N) break;
+        float x = v[e] + (g.c.bias ? g.c.bias[n + e] : 0.f);
+        if (g.c.out_f32)
+            g.c.out_f32[at + e] = fmaf(g.c.sign, x, g.c.resid ? g.c.resid[at + e] : 0.f);
+        else
+            g.c.out_bf16[at + e] = (uint16_t)f32_to_bf16_bits(g.c.relu && x < 0.f ? 0.f : x);
+    }
 }
 
-constexpr int kWaves = 8;
-
-// A workgroup takes 16 outputs of 16 MT rows; its waves take the tiles of 128
-// inputs in turn and add up in LDS.
-template <bool E2M1, int PT, int MT>
-__global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Args g) {
-    __shared__ float sums[kWaves][MT][16][16];  // [wave][row tile][row][output]
-    const int lane = lane_id(), wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
+// ---------------------------------------------------------------------------
+// Few rows.  A workgroup takes 16 outputs of 16 MT rows; its waves take the
+// tiles of 128 inputs in turn, AHEAD of them on their way, and add up in LDS.
+template <bool E2M1, bool ZEROS, int PT, int MT>
+__global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
+    extern __shared__ __attribute__((aligned(16))) float sums[];  // [wave][row tile][row][output]
+    constexpr int AHEAD = MT == 1 ? (PT == 4 && !E2M1 ? 2 : 4) : (MT == 2 ? 2 : 1);
+    const int lane = lane_id(), wave = threadIdx.x >> 6, waves = blockDim.x >> 6, q = lane >> 4;
     const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
     const int tiles_k = (int)g.s.tiles_k;
     const int64_t row_tile = (int64_t)blockIdx.x * tiles_k;
     const uint16_t* x[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = g.c.a + min(m0 + 16 * t + n, g.c.M - 1) * g.c.a_stride + 8 * q;
-    const bf16x8 ones = from_pairs(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < MT; ++t) x[t] = g.c.a + min(m0 + 16 * t + (lane & 15), g.c.M - 1) * g.c.a_stride + 8 * q;
+    struct Block {
+        Codes<E2M1> w;
+        Scales<ZEROS, E2M1 ? 0 : PT> s;
+        bf16x8 x[MT][4];
+    } blocks[AHEAD];
+    auto load = [&](Block& b, int k) {
+        b.w.load(g, row_tile + k, lane);
+        b.s.load(g, row_tile + k, lane);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                b.x[t][i] = 128 * k + 32 * i < g.s.K ? *reinterpret_cast<const bf16x8*>(x[t] + 128 * k + 32 * i) : all_of(0);
+    };
     f32x4 acc[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = none;
-    for (int b = wave; b < tiles_k; b += kWaves) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(g.codes + (row_tile + b) * 1024 + 16 * lane);
-        const int steps = min(4, (g.s.K - 128 * b) / 32);
+    for (int t = 0; t < MT; ++t) acc[t] = kNone;
+    // inputs past K: codes of 0 and rows of 0 add nothing
+    auto add = [&](const Block& b) {
         if constexpr (E2M1) {
-            const uint32_t bytes = *reinterpret_cast<const uint32_t*>(g.scales + ((row_tile + b) * 16 + n) * 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (i >= steps) break;
-                const bf16x8 v = e2m1_values(w[i], (bytes >> (8 * i)) & 255u);
+                const bf16x8 v = b.w.step(i);
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    acc[t] = mfma16(*reinterpret_cast<const bf16x8*>(x[t] + 128 * b + 32 * i), v, acc[t]);
+                for (int t = 0; t < MT; ++t) acc[t] = mfma16(v, b.x[t][i], acc[t]);
             }
         } else {
-            Scales<PT> sc;
-            sc.load(g, row_tile + b, n);
+            const bf16x8 ones = all_of(0x3F80u);
 #pragma unroll
             for (int p = 0; p < PT; ++p) {
-                constexpr int kSteps = 4 / PT;
                 f32x4 part[MT], sum[MT];
 #pragma unroll
-                for (int t = 0; t < MT; ++t) part[t] = sum[t] = none;
+                for (int t = 0; t < MT; ++t) part[t] = sum[t] = kNone;
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) {
-                    const int i = p * kSteps + j;
-                    if (i >= steps) break;
-                    const bf16x8 v = int4_codes(w[i]);
+                for (int i = p * (4 / PT); i < (p + 1) * (4 / PT); ++i) {
+                    const bf16x8 v = b.w.step(i);
 #pragma unroll
                     for (int t = 0; t < MT; ++t) {
-                        const bf16x8 xv = *reinterpret_cast<const bf16x8*>(x[t] + 128 * b + 32 * i);
-                        part[t] = mfma16(xv, v, part[t]);
-                        sum[t] = mfma16(xv, ones, sum[t]);
+                        part[t] = mfma16(v, b.x[t][i], part[t]);
+                        sum[t] = mfma16(ones, b.x[t][i], sum[t]);
                     }
                 }
+                const f32x4 s = b.s.scale(p), z = b.s.zero(p);
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[t][e] = fmaf(sc.s[p], fmaf(-sc.z[p], sum[t][e], part[t][e]), acc[t][e]);
+                    for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(s[e], fmaf(-z[e], sum[t][e], part[t][e]), acc[t][e]);
+                if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);  // no group's products before the last one's: spills
             }
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (wave + u * waves < tiles_k) load(blocks[u], wave + u * waves);
+    for (int k = wave; k < tiles_k; k += AHEAD * waves) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (k + u * waves >= tiles_k) break;
+            add(blocks[u]);
+            if (k + (u + AHEAD) * waves < tiles_k) load(blocks[u], k + (u + AHEAD) * waves);
         }
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sums[wave][t][4 * q + e][n] = acc[t][e];
+        *reinterpret_cast<f32x4*>(sums + ((wave * MT + t) * 16 + (lane & 15)) * 16 + 4 * q) = acc[t];
     __syncthreads();
-    for (int i = threadIdx.x; i < MT * 256; i += 64 * kWaves) {
-        const int t = i >> 8, r = (i >> 4) & 15, c = i & 15;
-        float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += sums[w][t][r][c];
-        put(g, m0 + 16 * t + r, (int)(blockIdx.x * 16) + c, v);
+    for (int i = threadIdx.x; i < MT * 64; i += blockDim.x) {
+        const int row = i >> 2, c = 4 * (i & 3);  // of 16 MT rows
+        if (m0 + row >= g.c.M) break;
+        f32x4 v = *reinterpret_cast<const f32x4*>(sums + row * 16 + c);
+        for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * MT * 16 + row) * 16 + c);
+        put4(g, m0 + row, (int)(blockIdx.x * 16) + c, v);
     }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows.  A workgroup of 2 x 2 waves computes 32 MI rows x 32 NI outputs, a
+// wave a quarter.  Rows pass through LDS in two stages of 128 inputs, copied
+// there by buffer loads; the weights go from memory to the registers of the
+// waves that use them, a stage ahead, and are widened there.
+template <int MI, int NI>
+struct Wide {
+    static constexpr int TM = 32 * MI, TN = 32 * NI;
+    static constexpr int kRowBytes = TM * 256;          // two halves of 64 inputs, rows of 128 bytes each
+    static constexpr int kStage = kRowBytes + 2 * 1024;  // and INT4's scales and zero points
+    static constexpr int kCopies = TM / 16;    // of 1 KB, a wave and stage
+    static constexpr size_t kLds = 2 * kStage;
+};
+
+// raw_buffer() in scalar registers.
+__device__ __forceinline__ u32x4 buffer_of(const void* p, uint64_t bytes) {
+    u32x4 b = raw_buffer(p, bytes);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = __builtin_amdgcn_readfirstlane(b[i]);
+    return b;
+}
+
+template <bool E2M1, bool ZEROS, int PT, int MI, int NI>
+__global__ __launch_bounds__(256, 2) void w4_wide_kernel(W4Args g) {
+    using S = Wide<MI, NI>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+    const int wm = wave & 1, wn = wave >> 1, tiles_k = (int)g.s.tiles_k;
+    // Tile of this workgroup (workgroup b runs on XCD b % 8): an XCD takes a run of
+    // the walk along the rows, so that its rows and weights meet in its L2.
+    const int nm = (int)((g.c.M + S::TM - 1) / S::TM), nn = (g.s.N + S::TN - 1) / S::TN;
+    int tm, tn;
+    {
+        const int tiles = nm * nn, xcd = (int)(blockIdx.x % 8);
+        const int i = xcd * (tiles / 8) + min(xcd, tiles % 8) + (int)(blockIdx.x / 8);
+        tn = i / nm;
+        tm = i - tn * nm;
+    }
+    const int64_t m0 = (int64_t)tm * S::TM;
+    const int n0 = tn * S::TN;
+    const uint16_t* const base = g.c.a + m0 * g.c.a_stride;
+    const u32x4 buf = buffer_of(base, ((uint64_t)(g.c.M - 1 - m0) * g.c.a_stride + g.s.K) * 2);
+    // Copies: lane l fills slot l % 8 of row l / 8 of eight rows; piece p of row r is
+    // in slot p ^ (r & 7) (operand reads meet all banks).  Rows past M repeat the last.
+    uint32_t off[S::kCopies];
+#pragma unroll
+    for (int j = 0; j < S::kCopies; ++j) {
+        const int run = wave * S::kCopies + j, half = run / (S::TM / 8), r = 8 * (run % (S::TM / 8)) + (lane >> 3);
+        const int64_t row = min((int64_t)r, g.c.M - 1 - m0);
+        off[j] = (uint32_t)(row * g.c.a_stride * 2) + 128u * half + 16u * ((lane & 7) ^ (r & 7));
+    }
+    const uint32_t lds0 = lds_addr(smem);
+    auto copy = [&](int k) {
+        const uint32_t to = lds0 + (k & 1) * S::kStage + wave * S::kCopies * 1024;
+#pragma unroll
+        for (int j = 0; j < S::kCopies; ++j) buffer_to_lds(buf, off[j], (uint32_t)k * 256u, to + j * 1024);
+    };
+    int64_t tile[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+        tile[i] = min((int64_t)(n0 / 16 + wn * NI + i), g.s.tiles_n - 1) * tiles_k;
+    // INT4: the workgroup's scales, 32 PT bytes a tile, and zero points, 16 PT, one
+    // copy each; lanes past the last tile repeat it.
+    const int64_t tile0 = n0 / 16;
+    const int st = min(lane / (2 * PT), 2 * NI - 1), zt = min(lane / PT, 2 * NI - 1);
+    const uint32_t scale_off =
+        (uint32_t)(min(tile0 + st, g.s.tiles_n - 1) * tiles_k * (32 * PT)) + 16 * (lane % (2 * PT));
+    const uint32_t zero_off = (uint32_t)(min(tile0 + zt, g.s.tiles_n - 1) * tiles_k * (16 * PT)) + 16 * (lane % PT);
+    const u32x4 scale_buf = buffer_of(g.scales, g.s.scales_size());
+    const u32x4 zero_buf = buffer_of(g.zeros, ZEROS ? g.s.zeros_size() : 0);
+    auto copy_scales = [&](int k) {
+        const uint32_t to = lds0 + (k & 1) * S::kStage + S::kRowBytes;
+        if (!E2M1 && wave == 0) buffer_to_lds(scale_buf, scale_off, (uint32_t)k * (32 * PT), to);
+        if (ZEROS && wave == 1) buffer_to_lds(zero_buf, zero_off, (uint32_t)k * (16 * PT), to + 1024);
+    };
+    auto scale = [&](int k, int i, int p) {
+        const uint2 s = *reinterpret_cast<const uint2*>(smem + (k & 1) * S::kStage + S::kRowBytes +
+                                                        ((wn * NI + i) * PT + p) * 32 + 8 * q);
+        return four_bf16(s);
+    };
+    auto zero = [&](int k, int i, int p) {
+        return four_bytes(*reinterpret_cast<const uint32_t*>(smem + (k & 1) * S::kStage + S::kRowBytes + 1024 +
+                                                             ((wn * NI + i) * PT + p) * 16 + 4 * q));
+    };
+    Codes<E2M1> cur[NI], next[NI];
+    auto load = [&](Codes<E2M1>* w, int k) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) w[i].load(g, tile[i] + k, lane);
+    };
+    // rows 16 t + l % 16 of the wave's, piece 4 (i % 2) + q of half i / 2
+    const uint32_t row = wm * (S::TM / 2) + (lane & 15);
+    auto rows = [&](int k, int i, int t) {
+        const uint32_t at = (k & 1) * S::kStage + (i >> 1) * (S::TM * 128) + (row + 16 * t) * 128 +
+                            16 * ((4 * (i & 1) + q) ^ (row & 7));
+        return *reinterpret_cast<const bf16x8*>(smem + at);
+    };
+    f32x4 acc[NI][MI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int t = 0; t < MI; ++t) acc[i][t] = kNone;
+    constexpr int kSteps = E2M1 ? 1 : 4 / PT;  // products of 32 inputs between two scalings
+    // `last`: the tile may end inside; steps past K take rows of zeros (their codes are 0)
+    auto add = [&](int k, auto last) {
+#pragma unroll
+        for (int p = 0; p < 4 / kSteps; ++p) {
+            bf16x8 x[kSteps][MI];
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                for (int t = 0; t < MI; ++t) {
+                    x[j][t] = rows(k, p * kSteps + j, t);
+                    if (decltype(last)::value && 128 * k + 32 * (p * kSteps + j) >= g.s.K) x[j][t] = all_of(0);
+                }
+            if constexpr (E2M1) {
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const bf16x8 v = cur[i].step(p);
+#pragma unroll
+                    for (int t = 0; t < MI; ++t) acc[i][t] = mfma16(v, x[0][t], acc[i][t]);
+                }
+            } else {
+                const bf16x8 ones = all_of(ZEROS ? 0x3F80u : 0xC100u);  // 1 or -8
+                f32x4 sum[MI];
+#pragma unroll
+                for (int t = 0; t < MI; ++t) sum[t] = kNone;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) {
+#pragma unroll
+                    for (int t = 0; t < MI; ++t) sum[t] = mfma16(ones, x[j][t], sum[t]);
+                }
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    f32x4 part[MI];
+                    const f32x4 s = scale(k, i, p);
+                    if constexpr (ZEROS) {
+                        const f32x4 z = zero(k, i, p);
+#pragma unroll
+                        for (int t = 0; t < MI; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) part[t][e] = -z[e] * sum[t][e];
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < MI; ++t) part[t] = sum[t];
+                    }
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j) {
+                            const bf16x8 v = cur[i].step(p * kSteps + j);
+#pragma unroll
+                        for (int t = 0; t < MI; ++t) part[t] = mfma16(v, x[j][t], part[t]);
+                    }
+#pragma unroll
+                    for (int t = 0; t < MI; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(s[e], part[t][e], acc[i][t][e]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+    };
+    auto arrived = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    copy(0);
+    copy_scales(0);
+    load(cur, 0);
+    arrived();
+    for (int k = 0; k < tiles_k; ++k) {
+        if (k + 1 < tiles_k) {
+            copy(k + 1);
+            copy_scales(k + 1);
+            load(next, k + 1);
+        }
+        if (k + 1 < tiles_k)
+            add(k, std::false_type{});
+        else
+            add(k, std::true_type{});
+        arrived();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) cur[i] = next[i];
+    }
+#pragma unroll
+    for (int t = 0; t < MI; ++t)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+            put4(g, m0 + row + 16 * t, n0 + 16 * (wn * NI + i) + 4 * q, acc[i][t]);
 }
 
 // ---------------------------------------------------------------------------
@@ -166,6 +429,10 @@ __device__ __forceinline__ Spot spot_of(const W4Shape& s) {
     p.pair = r;
     p.in = p.n < s.N && p.k < s.K;
     return p;
+}
+// Where a tile's scale (and zero point) of output r's group j lies.
+__device__ __forceinline__ int scale_place(const W4Shape& s, int r, int j) {
+    return s.e2m1 ? r * s.per_tile() + j : j * 16 + r;
 }
 __device__ __forceinline__ uint32_t word_of(const uint32_t* code, bool e2m1) {
     uint32_t w = 0;
@@ -230,7 +497,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(W4Shape s, const void*
     lo = group_fold(lo, lanes, [](float a, float b) { return fminf(a, b); });
     hi = group_fold(hi, lanes, [](float a, float b) { return fmaxf(a, b); });
     bad = group_fold(bad, lanes, [](float a, float b) { return fmaxf(a, b); });
-    const int j = threadIdx.x & 15, per = s.per_tile(), at = ((int)p.pair) * per + j / lanes;
+    const int j = threadIdx.x & 15, per = s.per_tile(), at = scale_place(s, p.pair, j / lanes);
     char* const scales = packed + s.codes_size() + p.tile * (16 * per * (int64_t)s.scale_bytes());
     uint8_t* const zeros = reinterpret_cast<uint8_t*>(packed + s.codes_size() + s.scales_size()) + p.tile * 16 * per;
     uint32_t code[8];
@@ -285,7 +552,8 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(W4Shape s, const uint8_t* 
     if (j < per) {
         const int groups = (s.K + s.group - 1) / s.group, k = p.k - 8 * j + j * s.group;  // the group's first input
         const bool in = p.n < s.N && k < s.K;
-        const int64_t from = in ? (int64_t)p.n * groups + k / s.group : 0, to = (p.tile * 16 + p.pair) * per + j;
+        const int64_t from = in ? (int64_t)p.n * groups + k / s.group : 0;
+        const int64_t to = p.tile * 16 * per + scale_place(s, p.pair, j);
         char* const sc = packed + s.codes_size();
         if (s.e2m1)
             sc[to] = in ? static_cast<const char*>(scales)[from] : 0;
@@ -304,7 +572,7 @@ __global__ __launch_bounds__(256) void w4_unpack_kernel(W4Shape s, const char* _
     if (!p.in) return;
     const uint32_t w = reinterpret_cast<const uint32_t*>(packed + p.tile * 1024)[p.word];
     const int j = threadIdx.x & 15, per = s.per_tile();
-    const int64_t at = (p.tile * 16 + p.pair) * per + j / (s.group / 8);
+    const int64_t at = p.tile * 16 * per + scale_place(s, p.pair, j / (s.group / 8));
     const char* const sc = packed + s.codes_size();
     float v[8];
     if (s.e2m1) {
@@ -335,16 +603,18 @@ __global__ __launch_bounds__(256) void w4_unpack_kernel(W4Shape s, const char* _
     }
 }
 
-template <int MT, typename Go>
+template <typename Go>
 void by_weights(const W4Shape& s, Go go) {
+    using std::integral_constant;
+    auto with = [&](auto pt) { s.zeros ? go(std::false_type{}, std::true_type{}, pt) : go(std::false_type{}, std::false_type{}, pt); };
     if (s.e2m1)
-        go(w4_rows_kernel<true, 4, MT>);
+        go(std::true_type{}, std::false_type{}, integral_constant<int, 4>{});
     else if (s.group == 32)
-        go(w4_rows_kernel<false, 4, MT>);
+        with(integral_constant<int, 4>{});
     else if (s.group == 64)
-        go(w4_rows_kernel<false, 2, MT>);
+        with(integral_constant<int, 2>{});
     else
-        go(w4_rows_kernel<false, 1, MT>);
+        with(integral_constant<int, 1>{});
 }
 
 unsigned tiles(const W4Shape& s) { return (unsigned)(s.tiles_n * s.tiles_k); }
@@ -373,25 +643,51 @@ hipError_t launch_w4_unpack(const W4Shape& s, bool f32, const char* packed, void
     return hipGetLastError();
 }
 
-bool w4_fits(const W4Shape& s, int64_t M) { return s.tiles_n < (int64_t)1 << 22 && (M + 63) / 64 < 65536; }
+namespace {
+
+// Rows from which the wide kernel takes over; its offsets within a tile are 32 bits.
+bool takes_wide(const W4Shape&, int64_t M, int64_t a_stride) { return M > 64 && a_stride < 1 << 24; }
+
+template <bool E2M1, bool ZEROS, int PT, int MT>
+void launch_rows(const W4Args& g, hipStream_t stream) {
+    const int waves = g.s.tiles_k >= 8 ? 8 : 4;
+    const dim3 grid((unsigned)g.s.tiles_n, (unsigned)((g.c.M + 16 * MT - 1) / (16 * MT)));
+    w4_rows_kernel<E2M1, ZEROS, PT, MT><<<grid, 64 * waves, (size_t)waves * MT * 1024, stream>>>(g);
+}
+
+template <bool E2M1, bool ZEROS, int PT, int MI, int NI>
+void launch_wide(const W4Args& g, hipStream_t stream) {
+    using S = Wide<MI, NI>;
+    auto* k = &w4_wide_kernel<E2M1, ZEROS, PT, MI, NI>;
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
+    const int64_t tiles = ((g.c.M + S::TM - 1) / S::TM) * ((g.s.N + S::TN - 1) / S::TN);
+    k<<<(unsigned)tiles, 256, S::kLds, stream>>>(g);
+}
+
+}  // namespace
 
 size_t w4_workspace_bytes(const W4Shape&, int64_t) { return 0; }
 
 hipError_t launch_linear_w4(const W4Shape& s, const W4Call& c, void*, hipStream_t stream) {
     const W4Args g{s, c, c.packed, c.packed + s.codes_size(),
                    s.zeros ? reinterpret_cast<const uint8_t*>(c.packed + s.codes_size() + s.scales_size()) : nullptr};
-    auto go = [&](int mt) {
-        return [&g, mt, stream](auto kernel) {
-            const dim3 grid((unsigned)g.s.tiles_n, (unsigned)((g.c.M + 16 * mt - 1) / (16 * mt)));
-            kernel<<<grid, 64 * kWaves, 0, stream>>>(g);
-        };
-    };
-    if (c.M <= 16)
-        by_weights<1>(s, go(1));
-    else if (c.M <= 32)
-        by_weights<2>(s, go(2));
-    else
-        by_weights<4>(s, go(4));
+    by_weights(s, [&](auto e2m1, auto zeros, auto pt) {
+        constexpr bool E2M1 = decltype(e2m1)::value, ZEROS = decltype(zeros)::value;
+        constexpr int PT = decltype(pt)::value;
+        if (takes_wide(s, c.M, c.a_stride)) {
+            auto tiles = [&](int t, int u) { return ((c.M + t - 1) / t) * ((s.N + u - 1) / u); };
+            if (tiles(128, 128) >= 256)
+                launch_wide<E2M1, ZEROS, PT, 4, 4>(g, stream);
+            else
+                launch_wide<E2M1, ZEROS, PT, 2, 2>(g, stream);
+        } else if (c.M <= 16) {
+            launch_rows<E2M1, ZEROS, PT, 1>(g, stream);
+        } else if (c.M <= 32) {
+            launch_rows<E2M1, ZEROS, PT, 2>(g, stream);
+        } else {
+            launch_rows<E2M1, ZEROS, PT, 4>(g, stream);
+        }
+    });
     return hipGetLastError();
 }
 
