@@ -225,18 +225,20 @@ def lsh_cache_append(cfg: CacheConfig, qk: _qk.QkConfig, pages: Pages, seqs: Seq
         qk = replace(qk, x_stride=stride)
     if (gain_k is not None) != (gain_q is not None and Hk > 0):
         raise ValueError("gain_k goes with gain_q and with keys of their own")
-    for name, t, shape, dtype in (("gain_q", gain_q, qk.gain_shape(cfg.H), torch.float32),
-                                  ("gain_k", gain_k, qk.gain_shape(Hk), torch.float32),
-                                  ("freq", freq, (qk.rot // 2,), torch.float32)):
+    for name, t, shape in (("gain_q", gain_q, qk.gain_shape(cfg.H)), ("gain_k", gain_k, qk.gain_shape(Hk)),
+                           ("freq", freq, (qk.rot // 2,))):
         if t is not None:
-            lsh._need(t, shape, dtype, name)
+            lsh._need(t, shape, torch.float32, name)
             if t.device != dev:
                 raise ValueError(f"{name} is on {t.device}, the pages on {dev}")
     if x.device != dev:
         raise ValueError(f"x is on {x.device}, the pages on {dev}")
     if q is None:
-        q = torch.empty((cfg.T, cfg.H, cfg.d), dtype=torch.bfloat16, device=dev)
-    cfg = cfg.strides(q_stride=_rows(q, cfg, cfg.H, "q", cfg.q_stride, dev, torch.bfloat16))
+        q, own = x.new_empty((cfg.T, cfg.H, cfg.d), dtype=torch.bfloat16), 0
+    else:
+        own = _rows(q, cfg, cfg.H, "q", cfg.q_stride, dev, torch.bfloat16)
+    if own != cfg.q_stride:
+        cfg = replace(cfg, q_stride=own)
     with lsh.on_device(dev):
         lsh._check("lsh_cache_append",
                    lib().lsh_cache_append(cfg.ref(), qk.ref(), lsh._dtype_code(x), ctypes.byref(pages.c()),

@@ -132,43 +132,76 @@ __device__ __forceinline__ void put4(const W4Args& g, int64_t m, int n, f32x4 v)
 
 // ---------------------------------------------------------------------------
 // Few rows.  A workgroup takes 16 outputs of 16 MT rows; its waves take the
-// tiles of 128 inputs in turn, AHEAD of them on their way, and add up in LDS.
-template <bool E2M1, bool ZEROS, int PT, int MT>
+// tiles of 128 inputs in turn, the codes of AHEAD of them on their way, and add
+// up in LDS.  Where the rows are short (STAGED) they pass through LDS once, while
+// the first codes are on their way; else a wave loads them tile by tile.
+constexpr size_t kStaged = 34 * 1024;  // bytes of rows, at most
+__host__ __device__ constexpr int64_t staged_stride(int K) { return K + 32; }  // rows start 16 banks apart
+
+template <bool E2M1, bool ZEROS, int PT, int MT, bool STAGED>
 __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
-    extern __shared__ __attribute__((aligned(16))) float sums[];  // [wave][row tile][row][output]
-    constexpr int AHEAD = MT == 1 ? (PT == 4 && !E2M1 ? 2 : 4) : (MT == 2 ? 2 : 1);
-    const int lane = lane_id(), wave = threadIdx.x >> 6, waves = blockDim.x >> 6, q = lane >> 4;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float* const sums = reinterpret_cast<float*>(smem);  // [wave][row tile][row][output]
+    constexpr int AHEAD = !E2M1 && PT == 4 ? 2 : 4;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int q = lane >> 4, K = g.s.K;
     const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int tiles_k = (int)g.s.tiles_k;
+    const int tiles_k = (int)g.s.tiles_k, whole = K / 128;
     const int64_t row_tile = (int64_t)blockIdx.x * tiles_k;
-    const uint16_t* x[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = g.c.a + min(m0 + 16 * t + (lane & 15), g.c.M - 1) * g.c.a_stride + 8 * q;
     struct Block {
         Codes<E2M1> w;
         Scales<ZEROS, E2M1 ? 0 : PT> s;
-        bf16x8 x[MT][4];
     } blocks[AHEAD];
     auto load = [&](Block& b, int k) {
         b.w.load(g, row_tile + k, lane);
         b.s.load(g, row_tile + k, lane);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                b.x[t][i] = 128 * k + 32 * i < g.s.K ? *reinterpret_cast<const bf16x8*>(x[t] + 128 * k + 32 * i) : all_of(0);
     };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (wave + u * waves < whole) load(blocks[u], wave + u * waves);
+    // Rows past M are not loaded: what their lanes hold meets their own results alone.
+    const uint16_t* x[MT];
+    bool there[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t m = m0 + 16 * t + (lane & 15);
+        there[t] = m < g.c.M;
+        if constexpr (STAGED)
+            x[t] = reinterpret_cast<const uint16_t*>(smem) + (16 * t + (lane & 15)) * staged_stride(K) + 8 * q;
+        else
+            x[t] = g.c.a + m * g.c.a_stride + 8 * q;
+    }
+    if constexpr (STAGED) {
+        const int rows = (int)min((int64_t)16 * MT, g.c.M - m0), pieces = K / 8;
+        for (int r = 0; r < rows; ++r)
+            for (int p = threadIdx.x; p < pieces; p += blockDim.x)
+                *reinterpret_cast<u32x4*>(smem + 2 * (r * staged_stride(K) + 8 * p)) =
+                    *reinterpret_cast<const u32x4*>(g.c.a + (m0 + r) * g.c.a_stride + 8 * p);
+        __syncthreads();
+    }
     f32x4 acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = kNone;
-    // inputs past K: codes of 0 and rows of 0 add nothing
-    auto add = [&](const Block& b) {
+    // `last`: a tile that ends inside; steps past K take rows of zeros (their codes are 0)
+    auto add = [&](const Block& b, int k, auto last) {
+        bf16x8 xv[4][MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if (there[t])
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!decltype(last)::value || 128 * k + 32 * i < K)
+                        xv[i][t] = *reinterpret_cast<const bf16x8*>(x[t] + 128 * k + 32 * i);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (decltype(last)::value && 128 * k + 32 * i >= K) xv[i][t] = all_of(0);
+        }
         if constexpr (E2M1) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bf16x8 v = b.w.step(i);
 #pragma unroll
-                for (int t = 0; t < MT; ++t) acc[t] = mfma16(v, b.x[t][i], acc[t]);
+                for (int t = 0; t < MT; ++t) acc[t] = mfma16(v, xv[i][t], acc[t]);
             }
         } else {
             const bf16x8 ones = all_of(0x3F80u);
@@ -182,8 +215,8 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
                     const bf16x8 v = b.w.step(i);
 #pragma unroll
                     for (int t = 0; t < MT; ++t) {
-                        part[t] = mfma16(v, b.x[t][i], part[t]);
-                        sum[t] = mfma16(ones, b.x[t][i], sum[t]);
+                        part[t] = mfma16(v, xv[i][t], part[t]);
+                        sum[t] = mfma16(ones, xv[i][t], sum[t]);
                     }
                 }
                 const f32x4 s = b.s.scale(p), z = b.s.zero(p);
@@ -195,17 +228,20 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
             }
         }
     };
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-        if (wave + u * waves < tiles_k) load(blocks[u], wave + u * waves);
-    for (int k = wave; k < tiles_k; k += AHEAD * waves) {
+    for (int k = wave; k < whole; k += AHEAD * waves) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (k + u * waves >= tiles_k) break;
-            add(blocks[u]);
-            if (k + (u + AHEAD) * waves < tiles_k) load(blocks[u], k + (u + AHEAD) * waves);
+            const int at = k + u * waves;
+            if (at >= whole) break;
+            add(blocks[u], at, std::false_type{});
+            if (at + AHEAD * waves < whole) load(blocks[u], at + AHEAD * waves);
         }
     }
+    if (whole < tiles_k && wave == whole % waves) {
+        load(blocks[0], whole);
+        add(blocks[0], whole, std::true_type{});
+    }
+    if constexpr (STAGED) __syncthreads();  // the rows have been read
 #pragma unroll
     for (int t = 0; t < MT; ++t)
         *reinterpret_cast<f32x4*>(sums + ((wave * MT + t) * 16 + (lane & 15)) * 16 + 4 * q) = acc[t];
@@ -652,7 +688,16 @@ template <bool E2M1, bool ZEROS, int PT, int MT>
 void launch_rows(const W4Args& g, hipStream_t stream) {
     const int waves = g.s.tiles_k >= 8 ? 8 : 4;
     const dim3 grid((unsigned)g.s.tiles_n, (unsigned)((g.c.M + 16 * MT - 1) / (16 * MT)));
-    w4_rows_kernel<E2M1, ZEROS, PT, MT><<<grid, 64 * waves, (size_t)waves * MT * 1024, stream>>>(g);
+    const size_t sums = (size_t)waves * MT * 1024;
+    if constexpr (MT == 1) {
+        // 16 rows and their padding, or as many as there are
+        const size_t rows = (size_t)g.c.M * staged_stride(g.s.K) * 2;
+        if (rows <= kStaged) {
+            w4_rows_kernel<E2M1, ZEROS, PT, MT, true><<<grid, 64 * waves, std::max(rows, sums), stream>>>(g);
+            return;
+        }
+    }
+    w4_rows_kernel<E2M1, ZEROS, PT, MT, false><<<grid, 64 * waves, sums, stream>>>(g);
 }
 
 template <bool E2M1, bool ZEROS, int PT, int MI, int NI>

@@ -152,8 +152,9 @@ def _inputs(cfg: ResidualConfig, f, gate, weights, like):
         own["gate_stride"] = _rows(gate, cfg, "gate", cfg.gate_stride)
         if gate.dtype != f.dtype or gate.device != dev:
             raise ValueError(f"gate is {gate.dtype} on {gate.device}, f {f.dtype} on {dev}")
-    own = {k: v for k, v in own.items() if v != getattr(cfg, k)}
-    return (replace(cfg, **own) if own else cfg), code, dev
+    if own.get("f_stride") != cfg.f_stride or own.get("gate_stride", cfg.gate_stride) != cfg.gate_stride:
+        cfg = replace(cfg, **own)
+    return cfg, code, dev
 
 
 def _take(t, shape, dtype, dev, name, make=True):
@@ -180,7 +181,7 @@ def lsh_residual_norm_fwd(cfg: ResidualConfig, x, f, gate, weights: ResidualWeig
     if code is None:
         code = lsh._dtype_code(torch.empty(0, dtype=own))
     x = _take(x, shape, torch.float32, dev, "x", False)
-    y = _take(y, shape, torch.float32, dev, "y")
+    y = x.new_empty(shape) if y is None and x is not None else _take(y, shape, torch.float32, dev, "y")
     if z is not None and not cfg.pre:
         raise ValueError("z goes with pre")
     z = _take(z, shape, own, dev, "z") if cfg.pre else None

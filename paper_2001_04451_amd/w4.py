@@ -97,9 +97,10 @@ def _packed(cfg: W4Config, packed, device) -> torch.Tensor:
         return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
     if packed.dtype != torch.uint8 or packed.dim() != 1 or packed.numel() < n:
         raise ValueError(f"packed has {packed.numel()} elements of {packed.dtype}, expected {n} of uint8 or more")
-    lsh._need(packed, packed.shape, torch.uint8, "packed")
     if packed.device != device:
         raise ValueError(f"packed is on {packed.device}, the tensors on {device}")
+    if not packed.is_cuda or not packed.is_contiguous():
+        raise ValueError("packed must be contiguous memory of a GPU")
     return packed
 
 
@@ -153,19 +154,31 @@ def _row_stride(a, K: int) -> int:
     """Elements between the rows of a [M, K] (0: packed)."""
     if not a.is_cuda:
         raise ValueError("a must be a GPU tensor")
-    if a.dim() != 2 or a.shape[1] != K or a.shape[0] < 1:
-        raise ValueError(f"a has shape {tuple(a.shape)}, expected (1 or more, {K})")
+    shape = a.shape
+    if len(shape) != 2 or shape[1] != K or shape[0] < 1:
+        raise ValueError(f"a has shape {tuple(shape)}, expected (1 or more, {K})")
     if a.dtype != torch.bfloat16:
         raise ValueError(f"a has dtype {a.dtype}, expected torch.bfloat16")
     if a.is_contiguous():
         return 0
+    own = a.stride(0)
     if a.stride(1) != 1:
         raise ValueError("a's rows must be contiguous")
-    if a.shape[0] == 1:  # of a single row any
+    if shape[0] == 1:  # of a single row any
         return 0
-    if a.stride(0) < K:  # also 0, one row for all, which the C call would take for packed rows
-        raise ValueError(f"a has row stride {a.stride(0)}, its rows have {K} elements")
-    return a.stride(0)
+    if own < K:  # also 0, one row for all, which the C call would take for packed rows
+        raise ValueError(f"a has row stride {own}, its rows have {K} elements")
+    return own
+
+
+def _beside(t, shape, dtype, dev, name) -> int | None:
+    """The address of t, contiguous and on a's device."""
+    if t is None:
+        return None
+    lsh._need(t, shape, dtype, name)
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, a on {dev}")
+    return t.data_ptr()
 
 
 def lsh_linear_w4(cfg: W4Config, a, packed, bias=None, resid=None, sign: float = 1.0, relu: bool = False,
@@ -173,30 +186,26 @@ def lsh_linear_w4(cfg: W4Config, a, packed, bias=None, resid=None, sign: float =
     """resid + sign (a W^T + bias) in fp32, or with dtype bfloat16 bf16(a W^T + bias), relu before the rounding
     with ``relu`` (lsh_linear_w4).  a [M, K] bf16, its rows at any stride that is a multiple of 8."""
     stride = _row_stride(a, cfg.K)
-    M, dev = a.shape[0], a.device
+    dev, shape = a.device, (a.shape[0], cfg.N)
     packed = _packed(cfg, packed, dev)
-    if dtype not in (torch.float32, torch.bfloat16):
+    f32 = dtype == torch.float32
+    if not f32 and dtype != torch.bfloat16:
         raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
     if out is None:
-        out = torch.empty((M, cfg.N), dtype=dtype, device=dev)
+        out = a.new_empty(shape, dtype=dtype)
+        to = out.data_ptr()
     else:
-        lsh._need(out, (M, cfg.N), dtype, "out")
-    if bias is not None:
-        lsh._need(bias, (cfg.N,), torch.float32, "bias")
-    if resid is not None:
-        lsh._need(resid, (M, cfg.N), torch.float32, "resid")
+        to = _beside(out, shape, dtype, dev, "out")
+    bias = _beside(bias, (cfg.N,), torch.float32, dev, "bias")
+    resid = _beside(resid, shape, torch.float32, dev, "resid")
     if workspace is None:
-        n = workspace_bytes(cfg, M)
+        n = workspace_bytes(cfg, shape[0])
         workspace = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     else:
         lsh._need_workspace(workspace, dev)
-    for name, t in (("out", out), ("bias", bias), ("resid", resid)):
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, a on {dev}")
-    p, f32 = lsh._ptr, dtype == torch.float32
     with lsh.on_device(dev):
         lsh._check("lsh_linear_w4",
-                   lib().lsh_linear_w4(cfg.ref(), M, p(a), stride, p(packed), p(bias), p(resid), sign,
-                                       int(bool(relu)), p(out) if f32 else None, None if f32 else p(out),
-                                       p(workspace), 0 if workspace is None else workspace.numel(), lsh._stream(dev)))
+                   lib().lsh_linear_w4(cfg.ref(), shape[0], a.data_ptr(), stride, packed.data_ptr(), bias, resid, sign,
+                                       bool(relu), to if f32 else None, None if f32 else to, lsh._ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), lsh._stream(dev)))
     return out
