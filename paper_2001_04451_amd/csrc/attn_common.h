@@ -146,6 +146,23 @@ __device__ __forceinline__ void buffer_to_lds(u32x4 buf, uint32_t v_off, uint32_
                  : "memory", "m0");
 }
 
+// Until at most N of the wave's loads are in flight and its LDS reads are
+// done (as the builtin, so that the compiler knows of the latter).
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64, "vmcnt has six bits");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+    asm volatile("" ::: "memory");
+}
+
+// Workgroup barrier alone (no wait for copies in flight); no LDS access moves
+// across it.
+__device__ __forceinline__ void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ void copy4_to_lds(const void* src, const void* lds_base) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_addr(lds_base))
                  : "memory", "m0");

@@ -134,29 +134,12 @@ struct GemmShape {
     static __device__ __forceinline__ int slot(int row, int p) { return p ^ (row & 7); }
 };
 
-// Until at most N of the wave's loads are in flight and its LDS reads are
-// done (as the builtin, so that the compiler knows of the latter).
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    static_assert(N < 64, "vmcnt has six bits");
-    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
-    asm volatile("" ::: "memory");
-}
-
 // acc += a b, in place in the accumulation registers.  Inline assembly ties
 // the result to the accumulator's registers: with the builtin the allocator
 // gives results other registers than their addends and moves them back (350
 // moves beside the 128 products of two stages at 256 accumulators a lane).
 __device__ __forceinline__ void mfma_into(f32x4& acc, bf16x8 a, bf16x8 b) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
-}
-
-// Workgroup barrier alone (no wait for copies in flight); no LDS access moves
-// across it.
-__device__ __forceinline__ void barrier() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
 }
 
 template <class S, int IN, int OUT>

@@ -10,8 +10,8 @@ namespace lsh {
 // other.  A tile's codes are 64 x 16 bytes, piece l those of output l % 16: for
 // i of 0 .. 3 a word with inputs 32 i + 8 (l / 16) .. + 7, the operand of lane l
 // for one 16 x 16 x 32 product, so that a wave's load is 1 KB without gaps.
-// Its INT4 scales and zero points are [per_tile][16] (per_tile = 128 / group),
-// its E2M1 scales [16][4].  Outputs past N and inputs past K hold codes of 0 and
+// Its INT4 scales and zero points are [4][per_tile][4], those of outputs 4 q ..
+// + 3 next to each other (per_tile = 128 / group), its E2M1 scales [16][4].  Outputs past N and inputs past K hold codes of 0 and
 // scales of 0.
 struct W4Shape {
     int N, K, e2m1, group, zeros;

@@ -81,22 +81,41 @@ __device__ __forceinline__ f32x4 four_bf16(uint2 s) {
 __device__ __forceinline__ f32x4 four_bytes(uint32_t z) {
     return f32x4{(float)(z & 255u), (float)((z >> 8) & 255u), (float)((z >> 16) & 255u), (float)(z >> 24)};
 }
-template <bool ZEROS, int PT>
-struct Scales {
-    uint2 s[PT];
-    uint32_t z[PT];
-    __device__ __forceinline__ void load(const W4Args& g, int64_t tile, int lane) {
+template <int BYTES>
+struct Bytes {  // from memory aligned to them, or to 16
+    uint32_t w[BYTES / 4];
+    __device__ __forceinline__ void load(const void* p) {
+        if constexpr (BYTES % 16 == 0) {
 #pragma unroll
-        for (int p = 0; p < PT; ++p) {
-            s[p] = *reinterpret_cast<const uint2*>(g.scales + (tile * PT + p) * 32 + 8 * (lane >> 4));
-            if constexpr (ZEROS) z[p] = *reinterpret_cast<const uint32_t*>(g.zeros + (tile * PT + p) * 16 + 4 * (lane >> 4));
+            for (int i = 0; i < BYTES / 16; ++i) {
+                const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
+            }
+        } else if constexpr (BYTES == 8) {
+            const uint2 v = *static_cast<const uint2*>(p);
+            w[0] = v.x, w[1] = v.y;
+        } else {
+            w[0] = *static_cast<const uint32_t*>(p);
         }
     }
-    __device__ __forceinline__ f32x4 scale(int p) const { return four_bf16(s[p]); }
+};
+template <bool ZEROS, int PT>
+struct Scales {
+    Bytes<8 * PT> s;
+    Bytes<ZEROS ? 4 * PT : 0> z;
+    __device__ __forceinline__ void load(const W4Args& g, int64_t tile, int lane) {
+        s.load(g.scales + (tile * 4 + (lane >> 4)) * (8 * PT));
+        if constexpr (ZEROS) z.load(g.zeros + (tile * 4 + (lane >> 4)) * (4 * PT));
+    }
+    __device__ __forceinline__ f32x4 scale(int p) const { return four_bf16(make_uint2(s.w[2 * p], s.w[2 * p + 1])); }
     __device__ __forceinline__ f32x4 zero(int p) const {
-        if constexpr (ZEROS) return four_bytes(z[p]);
+        if constexpr (ZEROS) return four_bytes(z.w[p]);
         return f32x4{8.f, 8.f, 8.f, 8.f};
     }
+};
+struct NoScales {
+    __device__ __forceinline__ void load(const W4Args&, int64_t, int) {}
 };
 
 // Four outputs n .. n + 3 of row m.
@@ -138,23 +157,28 @@ __device__ __forceinline__ void put4(const W4Args& g, int64_t m, int n, f32x4 v)
 constexpr size_t kStaged = 34 * 1024;  // bytes of rows, at most
 __host__ __device__ constexpr int64_t staged_stride(int K) { return K + 32; }  // rows start 16 banks apart
 
-template <bool E2M1, bool ZEROS, int PT, int MT, bool STAGED>
+template <bool E2M1, bool ZEROS, int PT, int MT, int NT, bool STAGED>
 __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    float* const sums = reinterpret_cast<float*>(smem);  // [wave][row tile][row][output]
-    constexpr int AHEAD = !E2M1 && PT == 4 ? 2 : 4;
+    float* const sums = reinterpret_cast<float*>(smem);  // [wave][output tile][row tile][row][output]
+    constexpr int AHEAD = NT == 1 ? (!E2M1 && PT == 4 ? 2 : 4) : (NT == 2 ? 2 : 1);
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int q = lane >> 4, K = g.s.K;
     const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
     const int tiles_k = (int)g.s.tiles_k, whole = K / 128;
-    const int64_t row_tile = (int64_t)blockIdx.x * tiles_k;
+    int64_t tile[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) tile[j] = min((int64_t)blockIdx.x * NT + j, g.s.tiles_n - 1) * tiles_k;
     struct Block {
-        Codes<E2M1> w;
-        Scales<ZEROS, E2M1 ? 0 : PT> s;
+        Codes<E2M1> w[NT];
+        std::conditional_t<E2M1, NoScales, Scales<ZEROS, PT>> s[NT];
     } blocks[AHEAD];
     auto load = [&](Block& b, int k) {
-        b.w.load(g, row_tile + k, lane);
-        b.s.load(g, row_tile + k, lane);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            b.w[j].load(g, tile[j] + k, lane);
+            b.s[j].load(g, tile[j] + k, lane);
+        }
     };
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
@@ -172,16 +196,20 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
             x[t] = g.c.a + m * g.c.a_stride + 8 * q;
     }
     if constexpr (STAGED) {
-        const int rows = (int)min((int64_t)16 * MT, g.c.M - m0), pieces = K / 8;
-        for (int r = 0; r < rows; ++r)
-            for (int p = threadIdx.x; p < pieces; p += blockDim.x)
-                *reinterpret_cast<u32x4*>(smem + 2 * (r * staged_stride(K) + 8 * p)) =
-                    *reinterpret_cast<const u32x4*>(g.c.a + (m0 + r) * g.c.a_stride + 8 * p);
+        const int pieces = K / 8, all = (int)min((int64_t)16 * MT, g.c.M - m0) * pieces;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < all; i += blockDim.x) {
+            const int r = i / pieces, p = i - r * pieces;
+            *reinterpret_cast<u32x4*>(smem + 2 * (r * staged_stride(K) + 8 * p)) =
+                *reinterpret_cast<const u32x4*>(g.c.a + (m0 + r) * g.c.a_stride + 8 * p);
+        }
         __syncthreads();
     }
-    f32x4 acc[MT];
+    f32x4 acc[NT][MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = kNone;
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[j][t] = kNone;
     // `last`: a tile that ends inside; steps past K take rows of zeros (their codes are 0)
     auto add = [&](const Block& b, int k, auto last) {
         bf16x8 xv[4][MT];
@@ -198,32 +226,44 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
         }
         if constexpr (E2M1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x8 v = b.w.step(i);
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) acc[t] = mfma16(v, xv[i][t], acc[t]);
-            }
+                for (int j = 0; j < NT; ++j) {
+                    const bf16x8 v = b.w[j].step(i);
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) acc[j][t] = mfma16(v, xv[i][t], acc[j][t]);
+                }
         } else {
             const bf16x8 ones = all_of(0x3F80u);
 #pragma unroll
             for (int p = 0; p < PT; ++p) {
-                f32x4 part[MT], sum[MT];
+                f32x4 part[NT][MT], sum[MT];
 #pragma unroll
-                for (int t = 0; t < MT; ++t) part[t] = sum[t] = kNone;
+                for (int t = 0; t < MT; ++t) {
+                    sum[t] = kNone;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) part[j][t] = kNone;
+                }
 #pragma unroll
                 for (int i = p * (4 / PT); i < (p + 1) * (4 / PT); ++i) {
-                    const bf16x8 v = b.w.step(i);
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) {
-                        part[t] = mfma16(v, xv[i][t], part[t]);
-                        sum[t] = mfma16(ones, xv[i][t], sum[t]);
+                    for (int t = 0; t < MT; ++t) sum[t] = mfma16(ones, xv[i][t], sum[t]);
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        const bf16x8 v = b.w[j].step(i);
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) part[j][t] = mfma16(v, xv[i][t], part[j][t]);
                     }
                 }
-                const f32x4 s = b.s.scale(p), z = b.s.zero(p);
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
+                for (int j = 0; j < NT; ++j) {
+                    const f32x4 s = b.s[j].scale(p), z = b.s[j].zero(p);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(s[e], fmaf(-z[e], sum[t][e], part[t][e]), acc[t][e]);
+                    for (int t = 0; t < MT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[j][t][e] = fmaf(s[e], fmaf(-z[e], sum[t][e], part[j][t][e]), acc[j][t][e]);
+                }
                 if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);  // no group's products before the last one's: spills
             }
         }
@@ -243,30 +283,42 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
     }
     if constexpr (STAGED) __syncthreads();  // the rows have been read
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-        *reinterpret_cast<f32x4*>(sums + ((wave * MT + t) * 16 + (lane & 15)) * 16 + 4 * q) = acc[t];
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            *reinterpret_cast<f32x4*>(sums + (((wave * NT + j) * MT + t) * 16 + (lane & 15)) * 16 + 4 * q) = acc[j][t];
     __syncthreads();
-    for (int i = threadIdx.x; i < MT * 64; i += blockDim.x) {
-        const int row = i >> 2, c = 4 * (i & 3);  // of 16 MT rows
-        if (m0 + row >= g.c.M) break;
-        f32x4 v = *reinterpret_cast<const f32x4*>(sums + row * 16 + c);
-        for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * MT * 16 + row) * 16 + c);
-        put4(g, m0 + row, (int)(blockIdx.x * 16) + c, v);
+    for (int i = threadIdx.x; i < NT * MT * 64; i += blockDim.x) {
+        const int c = 4 * (i & 3), row = (i >> 2) % (16 * MT), j = (i >> 2) / (16 * MT);
+        if (m0 + row >= g.c.M) continue;
+        f32x4 v = *reinterpret_cast<const f32x4*>(sums + (j * MT * 16 + row) * 16 + c);
+        for (int w = 1; w < waves; ++w)
+            v += *reinterpret_cast<const f32x4*>(sums + ((w * NT + j) * MT * 16 + row) * 16 + c);
+        put4(g, m0 + row, (int)((blockIdx.x * NT + j) * 16) + c, v);
     }
 }
 
 // ---------------------------------------------------------------------------
-// Many rows.  A workgroup of 2 x 2 waves computes 32 MI rows x 32 NI outputs, a
-// wave a quarter.  Rows pass through LDS in two stages of 128 inputs, copied
-// there by buffer loads; the weights go from memory to the registers of the
-// waves that use them, a stage ahead, and are widened there.
-template <int MI, int NI>
+// Many rows.  A workgroup of 2 x WN waves computes 32 MI rows x 16 NI WN outputs, a
+// wave 16 MI x 16 NI.  Rows, codes and scales pass through a ring of LDS stages of
+// 128 inputs, copied there by buffer loads that the kernel counts by hand; codes
+// are widened in the registers of the waves that use them.  A call with few tiles
+// splits its inputs over workgroups, whose sums a second kernel joins in order.
+__host__ __device__ constexpr int partial_width(int N) { return (N + 3) & ~3; }
+
+template <int MI, int NI, int WN>
 struct Wide {
-    static constexpr int TM = 32 * MI, TN = 32 * NI;
-    static constexpr int kRowBytes = TM * 256;          // two halves of 64 inputs, rows of 128 bytes each
-    static constexpr int kStage = kRowBytes + 2 * 1024;  // and INT4's scales and zero points
-    static constexpr int kCopies = TM / 16;    // of 1 KB, a wave and stage
-    static constexpr size_t kLds = 2 * kStage;
+    static constexpr int TM = 32 * MI, TN = 16 * NI * WN, kWaves = 2 * WN;
+    static constexpr int STAGES = MI == 1 ? 4 : 3;
+    static constexpr int kRowBytes = TM * 256;                    // two halves of 64 inputs, rows of 128 bytes each
+    static constexpr int kScales = kRowBytes + TN * 64;           // behind them the codes,
+    static constexpr int kScaleBytes = TN > 128 ? TN * 8 : 1024;  // scales (as of groups of 32)
+    static constexpr int kZeros = kScales + kScaleBytes;
+    static constexpr int kStage = kZeros + 1024;                  // and zero points
+    static constexpr int kCopies = TM / 4 / kWaves;               // of 1 KB of rows, a wave and stage,
+    static constexpr int kCodes = TN / 16 / kWaves;               // and of codes
+    static constexpr int kLoads = kCopies + kCodes;
+    static constexpr size_t kLds = STAGES * kStage;
 };
 
 // raw_buffer() in scalar registers.
@@ -277,19 +329,21 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, uint64_t bytes) {
     return b;
 }
 
-template <bool E2M1, bool ZEROS, int PT, int MI, int NI>
-__global__ __launch_bounds__(256, 2) void w4_wide_kernel(W4Args g) {
-    using S = Wide<MI, NI>;
+template <bool E2M1, bool ZEROS, int PT, int MI, int NI, int WN>
+__global__ __launch_bounds__(128 * WN, 2) void w4_wide_kernel(W4Args g, int splits, float* __restrict__ partial) {
+    using S = Wide<MI, NI, WN>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
     const int wm = wave & 1, wn = wave >> 1, tiles_k = (int)g.s.tiles_k;
+    const int split = (int)(blockIdx.x % (unsigned)splits), block = (int)(blockIdx.x / (unsigned)splits);
+    const int k0 = (int)((int64_t)tiles_k * split / splits), k1 = (int)((int64_t)tiles_k * (split + 1) / splits);
     // Tile of this workgroup (workgroup b runs on XCD b % 8): an XCD takes a run of
     // the walk along the rows, so that its rows and weights meet in its L2.
     const int nm = (int)((g.c.M + S::TM - 1) / S::TM), nn = (g.s.N + S::TN - 1) / S::TN;
     int tm, tn;
     {
-        const int tiles = nm * nn, xcd = (int)(blockIdx.x % 8);
-        const int i = xcd * (tiles / 8) + min(xcd, tiles % 8) + (int)(blockIdx.x / 8);
+        const int tiles = nm * nn, xcd = block % 8;
+        const int i = xcd * (tiles / 8) + min(xcd, tiles % 8) + block / 8;
         tn = i / nm;
         tm = i - tn * nm;
     }
@@ -298,56 +352,66 @@ __global__ __launch_bounds__(256, 2) void w4_wide_kernel(W4Args g) {
     const uint16_t* const base = g.c.a + m0 * g.c.a_stride;
     const u32x4 buf = buffer_of(base, ((uint64_t)(g.c.M - 1 - m0) * g.c.a_stride + g.s.K) * 2);
     // Copies: lane l fills slot l % 8 of row l / 8 of eight rows; piece p of row r is
-    // in slot p ^ (r & 7) (operand reads meet all banks).  Rows past M repeat the last.
-    uint32_t off[S::kCopies];
-#pragma unroll
-    for (int j = 0; j < S::kCopies; ++j) {
-        const int run = wave * S::kCopies + j, half = run / (S::TM / 8), r = 8 * (run % (S::TM / 8)) + (lane >> 3);
-        const int64_t row = min((int64_t)r, g.c.M - 1 - m0);
-        off[j] = (uint32_t)(row * g.c.a_stride * 2) + 128u * half + 16u * ((lane & 7) ^ (r & 7));
-    }
+    // in slot p ^ (r & 7) (operand reads meet all banks).  A wave's copies are runs
+    // of eight rows of one half; rows past M lie past the buffer's end.
+    static_assert(S::TM / 8 % S::kCopies == 0, "a wave's runs lie in one half");
+    const int run = wave * S::kCopies, first = 8 * (run % (S::TM / 8));
+    const uint32_t row_bytes = (uint32_t)g.c.a_stride * 2;
+    const uint32_t off = (lane >> 3) * row_bytes + 16u * ((lane & 7) ^ (lane >> 3));
+    const uint32_t first_off = first * row_bytes + 128u * (run / (S::TM / 8));
     const uint32_t lds0 = lds_addr(smem);
-    auto copy = [&](int k) {
-        const uint32_t to = lds0 + (k & 1) * S::kStage + wave * S::kCopies * 1024;
-#pragma unroll
-        for (int j = 0; j < S::kCopies; ++j) buffer_to_lds(buf, off[j], (uint32_t)k * 256u, to + j * 1024);
-    };
-    int64_t tile[NI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-        tile[i] = min((int64_t)(n0 / 16 + wn * NI + i), g.s.tiles_n - 1) * tiles_k;
-    // INT4: the workgroup's scales, 32 PT bytes a tile, and zero points, 16 PT, one
-    // copy each; lanes past the last tile repeat it.
     const int64_t tile0 = n0 / 16;
-    const int st = min(lane / (2 * PT), 2 * NI - 1), zt = min(lane / PT, 2 * NI - 1);
-    const uint32_t scale_off =
-        (uint32_t)(min(tile0 + st, g.s.tiles_n - 1) * tiles_k * (32 * PT)) + 16 * (lane % (2 * PT));
+    // Scales, 32 PT bytes a tile (E2M1 64), and zero points, 16 PT: a copy each of
+    // 64 lanes (two where the tiles have more); lanes past the last tile repeat it.
+    constexpr int kScaleLanes = E2M1 ? 4 : 2 * PT, kTiles = S::TN / 16;
+    constexpr int kScaleCopies = (kTiles * kScaleLanes + 63) / 64;
+    static_assert(kTiles * PT <= 64 && kScaleCopies * 1024 <= S::kScaleBytes && kScaleCopies < S::kWaves, "");
+    const int sl = lane + 64 * min(wave, kScaleCopies - 1);
+    const int st = min(sl / kScaleLanes, kTiles - 1), zt = min(lane / PT, kTiles - 1);
+    const uint32_t scale_off = (uint32_t)(min(tile0 + st, g.s.tiles_n - 1) * tiles_k * (16 * kScaleLanes)) +
+                               16 * (sl % kScaleLanes);
     const uint32_t zero_off = (uint32_t)(min(tile0 + zt, g.s.tiles_n - 1) * tiles_k * (16 * PT)) + 16 * (lane % PT);
     const u32x4 scale_buf = buffer_of(g.scales, g.s.scales_size());
     const u32x4 zero_buf = buffer_of(g.zeros, ZEROS ? g.s.zeros_size() : 0);
-    auto copy_scales = [&](int k) {
-        const uint32_t to = lds0 + (k & 1) * S::kStage + S::kRowBytes;
-        if (!E2M1 && wave == 0) buffer_to_lds(scale_buf, scale_off, (uint32_t)k * (32 * PT), to);
-        if (ZEROS && wave == 1) buffer_to_lds(zero_buf, zero_off, (uint32_t)k * (16 * PT), to + 1024);
-    };
-    auto scale = [&](int k, int i, int p) {
-        const uint2 s = *reinterpret_cast<const uint2*>(smem + (k & 1) * S::kStage + S::kRowBytes +
-                                                        ((wn * NI + i) * PT + p) * 32 + 8 * q);
-        return four_bf16(s);
-    };
-    auto zero = [&](int k, int i, int p) {
-        return four_bytes(*reinterpret_cast<const uint32_t*>(smem + (k & 1) * S::kStage + S::kRowBytes + 1024 +
-                                                             ((wn * NI + i) * PT + p) * 16 + 4 * q));
-    };
-    Codes<E2M1> cur[NI], next[NI];
-    auto load = [&](Codes<E2M1>* w, int k) {
+    const bool extra = wave < kScaleCopies || (ZEROS && wave == kScaleCopies);  // this wave's stages have a copy more
+    u32x4 code_buf[S::kCodes];  // of its tiles
 #pragma unroll
-        for (int i = 0; i < NI; ++i) w[i].load(g, tile[i] + k, lane);
+    for (int j = 0; j < S::kCodes; ++j)
+        code_buf[j] = buffer_of(g.codes + min(tile0 + wave * S::kCodes + j, g.s.tiles_n - 1) * tiles_k * 1024,
+                                (uint64_t)tiles_k * 1024);
+    auto copy = [&](int k, int slot) {
+        const uint32_t to = lds0 + slot * S::kStage;
+#pragma unroll
+        for (int j = 0; j < S::kCopies; ++j)
+            buffer_to_lds(buf, off, first_off + 8 * j * row_bytes + (uint32_t)k * 256u, to + (run + j) * 1024);
+#pragma unroll
+        for (int j = 0; j < S::kCodes; ++j)
+            buffer_to_lds(code_buf[j], 16 * lane, (uint32_t)k * 1024u, to + S::kRowBytes + (wave * S::kCodes + j) * 1024);
+        if (wave < kScaleCopies)
+            buffer_to_lds(scale_buf, scale_off, (uint32_t)k * (16 * kScaleLanes), to + S::kScales + wave * 1024);
+        else if (ZEROS && wave == kScaleCopies)
+            buffer_to_lds(zero_buf, zero_off, (uint32_t)k * (16 * PT), to + S::kZeros);
+    };
+    auto scale = [&](int slot, int i, int p) {
+        return four_bf16(*reinterpret_cast<const uint2*>(smem + slot * S::kStage + S::kScales +
+                                                         ((wn * NI + i) * 4 + q) * (8 * PT) + 8 * p));
+    };
+    auto zero = [&](int slot, int i, int p) {
+        return four_bytes(*reinterpret_cast<const uint32_t*>(smem + slot * S::kStage + S::kZeros +
+                                                             ((wn * NI + i) * 4 + q) * (4 * PT) + 4 * p));
+    };
+    auto codes = [&](int slot, int i) {
+        const char* const at = smem + slot * S::kStage;
+        Codes<E2M1> c;
+        c.w = *reinterpret_cast<const u32x4*>(at + S::kRowBytes + (wn * NI + i) * 1024 + 16 * lane);
+        if constexpr (E2M1)
+            c.bytes = *reinterpret_cast<const uint32_t*>(at + S::kScales + (wn * NI + i) * 64 + 4 * (lane & 15));
+        return c;
     };
     // rows 16 t + l % 16 of the wave's, piece 4 (i % 2) + q of half i / 2
     const uint32_t row = wm * (S::TM / 2) + (lane & 15);
-    auto rows = [&](int k, int i, int t) {
-        const uint32_t at = (k & 1) * S::kStage + (i >> 1) * (S::TM * 128) + (row + 16 * t) * 128 +
+    auto rows = [&](int slot, int i, int t) {
+        const uint32_t at = slot * S::kStage + (i >> 1) * (S::TM * 128) + (row + 16 * t) * 128 +
                             16 * ((4 * (i & 1) + q) ^ (row & 7));
         return *reinterpret_cast<const bf16x8*>(smem + at);
     };
@@ -357,8 +421,16 @@ __global__ __launch_bounds__(256, 2) void w4_wide_kernel(W4Args g) {
 #pragma unroll
         for (int t = 0; t < MI; ++t) acc[i][t] = kNone;
     constexpr int kSteps = E2M1 ? 1 : 4 / PT;  // products of 32 inputs between two scalings
+    // Small tiles: every product's chain apart, for there is little else to hide
+    // their latency; large ones start a tile's chain from its zero points' part, an
+    // output tile after the other, for their registers.
+    constexpr bool APART = MI <= 2 || E2M1;
     // `last`: the tile may end inside; steps past K take rows of zeros (their codes are 0)
-    auto add = [&](int k, auto last) {
+    auto add = [&](int k, int slot, auto last) {
+        Codes<E2M1> cur[NI];  // small tiles: all at once
+        if constexpr (APART)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) cur[i] = codes(slot, i);
 #pragma unroll
         for (int p = 0; p < 4 / kSteps; ++p) {
             bf16x8 x[kSteps][MI];
@@ -366,7 +438,7 @@ __global__ __launch_bounds__(256, 2) void w4_wide_kernel(W4Args g) {
             for (int j = 0; j < kSteps; ++j)
 #pragma unroll
                 for (int t = 0; t < MI; ++t) {
-                    x[j][t] = rows(k, p * kSteps + j, t);
+                    x[j][t] = rows(slot, p * kSteps + j, t);
                     if (decltype(last)::value && 128 * k + 32 * (p * kSteps + j) >= g.s.K) x[j][t] = all_of(0);
                 }
             if constexpr (E2M1) {
@@ -377,71 +449,115 @@ __global__ __launch_bounds__(256, 2) void w4_wide_kernel(W4Args g) {
                     for (int t = 0; t < MI; ++t) acc[i][t] = mfma16(v, x[0][t], acc[i][t]);
                 }
             } else {
-                const bf16x8 ones = all_of(ZEROS ? 0x3F80u : 0xC100u);  // 1 or -8
+                const bf16x8 ones = all_of(ZEROS || APART ? 0x3F80u : 0xC100u);  // 1 or -8
                 f32x4 sum[MI];
 #pragma unroll
                 for (int t = 0; t < MI; ++t) sum[t] = kNone;
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) {
+                for (int j = 0; j < kSteps; ++j)
 #pragma unroll
                     for (int t = 0; t < MI; ++t) sum[t] = mfma16(ones, x[j][t], sum[t]);
-                }
+                if constexpr (APART) {
+                    f32x4 part[NI][MI];
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    f32x4 part[MI];
-                    const f32x4 s = scale(k, i, p);
-                    if constexpr (ZEROS) {
-                        const f32x4 z = zero(k, i, p);
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int t = 0; t < MI; ++t) part[i][t] = kNone;
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            const bf16x8 v = cur[i].step(p * kSteps + j);
+#pragma unroll
+                            for (int t = 0; t < MI; ++t) part[i][t] = mfma16(v, x[j][t], part[i][t]);
+                        }
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) {
+                        const f32x4 s = scale(slot, i, p), z = ZEROS ? zero(slot, i, p) : f32x4{8.f, 8.f, 8.f, 8.f};
 #pragma unroll
                         for (int t = 0; t < MI; ++t)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) part[t][e] = -z[e] * sum[t][e];
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < MI; ++t) part[t] = sum[t];
+                            for (int e = 0; e < 4; ++e)
+                                acc[i][t][e] = fmaf(s[e], fmaf(-z[e], sum[t][e], part[i][t][e]), acc[i][t][e]);
                     }
+                } else {
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) {
-                            const bf16x8 v = cur[i].step(p * kSteps + j);
+                    for (int i = 0; i < NI; ++i) {
+                        f32x4 part[MI];
+                        const Codes<E2M1> own = codes(slot, i);
+                        const f32x4 s = scale(slot, i, p);
+                        if constexpr (ZEROS) {
+                            const f32x4 z = zero(slot, i, p);
 #pragma unroll
-                        for (int t = 0; t < MI; ++t) part[t] = mfma16(v, x[j][t], part[t]);
+                            for (int t = 0; t < MI; ++t)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) part[t][e] = -z[e] * sum[t][e];
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < MI; ++t) part[t] = sum[t];
+                        }
+#pragma unroll
+                        for (int j = 0; j < kSteps; ++j) {
+                            const bf16x8 v = own.step(p * kSteps + j);
+#pragma unroll
+                            for (int t = 0; t < MI; ++t) part[t] = mfma16(v, x[j][t], part[t]);
+                        }
+#pragma unroll
+                        for (int t = 0; t < MI; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(s[e], part[t][e], acc[i][t][e]);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-#pragma unroll
-                    for (int t = 0; t < MI; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(s[e], part[t][e], acc[i][t][e]);
-                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
     };
-    auto arrived = [] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    copy(0);
-    copy_scales(0);
-    load(cur, 0);
-    arrived();
-    for (int k = 0; k < tiles_k; ++k) {
-        if (k + 1 < tiles_k) {
-            copy(k + 1);
-            copy_scales(k + 1);
-            load(next, k + 1);
-        }
+    auto add_tile = [&](int k, int slot) {
         if (k + 1 < tiles_k)
-            add(k, std::false_type{});
+            add(k, slot, std::false_type{});
         else
-            add(k, std::true_type{});
-        arrived();
+            add(k, slot, std::true_type{});
+    };
+    constexpr int kAhead = S::STAGES - 1;  // stages on their way: all but the one that is being read
 #pragma unroll
-        for (int i = 0; i < NI; ++i) cur[i] = next[i];
+    for (int u = 0; u < kAhead; ++u)
+        if (k0 + u < k1) copy(k0 + u, u);
+    int slot = 0;
+    for (int k = k0; k < k1; ++k) {
+        if (k + kAhead - 1 >= k1)
+            wait_loads<0>();
+        else if (extra)
+            wait_loads<(kAhead - 1) * (S::kLoads + 1)>();
+        else
+            wait_loads<(kAhead - 1) * S::kLoads>();
+        barrier();  // this stage is there, and everyone has read the last one
+        if (k + kAhead < k1) copy(k + kAhead, slot == 0 ? S::STAGES - 1 : slot - 1);
+        add_tile(k, slot);
+        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
     }
 #pragma unroll
     for (int t = 0; t < MI; ++t)
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-            put4(g, m0 + row + 16 * t, n0 + 16 * (wn * NI + i) + 4 * q, acc[i][t]);
+        for (int i = 0; i < NI; ++i) {
+            const int64_t m = m0 + row + 16 * t;
+            const int n = n0 + 16 * (wn * NI + i) + 4 * q;
+            if (splits == 1)
+                put4(g, m, n, acc[i][t]);
+            else if (m < g.c.M && n < g.s.N)
+                *reinterpret_cast<f32x4*>(partial + (split * g.c.M + m) * partial_width(g.s.N) + n) = acc[i][t];
+        }
+}
+
+// The splits' parts of four outputs added in order.
+__global__ __launch_bounds__(256) void w4_join_kernel(W4Args g, int splits, const float* __restrict__ partial) {
+    const int width = partial_width(g.s.N);
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = g.c.M * width;
+    if (at >= all) return;
+    f32x4 v = *reinterpret_cast<const f32x4*>(partial + at);
+#pragma unroll 4
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(partial + s * all + at);
+    const int64_t m = at / width;
+    put4(g, m, (int)(at - m * width), v);
 }
 
 // ---------------------------------------------------------------------------
@@ -468,7 +584,7 @@ __device__ __forceinline__ Spot spot_of(const W4Shape& s) {
 }
 // Where a tile's scale (and zero point) of output r's group j lies.
 __device__ __forceinline__ int scale_place(const W4Shape& s, int r, int j) {
-    return s.e2m1 ? r * s.per_tile() + j : j * 16 + r;
+    return s.e2m1 ? r * s.per_tile() + j : (r >> 2) * 4 * s.per_tile() + 4 * j + (r & 3);
 }
 __device__ __forceinline__ uint32_t word_of(const uint32_t* code, bool e2m1) {
     uint32_t w = 0;
@@ -681,56 +797,108 @@ hipError_t launch_w4_unpack(const W4Shape& s, bool f32, const char* packed, void
 
 namespace {
 
-// Rows from which the wide kernel takes over; its offsets within a tile are 32 bits.
-bool takes_wide(const W4Shape&, int64_t M, int64_t a_stride) { return M > 64 && a_stride < 1 << 24; }
+// Which kernel a call takes, by its sizes alone (us of both sides, int4 with groups
+// of 128 unless said; weights out of the caches).
+//   Up to 16 rows: the rows kernel, 16 outputs a workgroup, from 512 tiles of
+//   outputs on 32 and from 1024 on 64: reading the rows once a workgroup is what
+//   bounds wider calls (L2 gives all CUs together 8.8 TB/s).  16 x 4096 x 4096 (16
+//   outputs / 32 / 64) 7.5 / 7.5 / 8.5, 16 x 8192 x 4096 11.5 / 8.1 / 8.8, 16 x
+//   16384 x 4096 19.8 / 13.0 / 9.9, 1 x 8192 x 4096 7.4 / 6.6 / 7.9, 1 x 32000 x
+//   4096 18.3 / 19.0 / 17.4.
+//   Up to 32 rows the same (32 x 16384 x 4096 34 / 20 / 13.5), but with groups of
+//   32, whose scales leave no registers for 64 outputs (24 / 83 at 32 / 64).
+//   Up to 64 rows the same where there is little to split (64 x 4096 x 1024 6.6
+//   against the wide kernel's 7.2; 64 x 4096 x 4096 18.2 against 13.5).
+//   Beyond: the wide kernel, in the largest tiles that make a workgroup for every
+//   CU: 2048 x 4096 x 1024 in tiles of 128 x 256 28.1, 64 x 128 30.5, 64 x 64 38;
+//   1024 x 4096 x 1024 26 / 17.5 / 21.  With fewer tiles of 64 x 64 than that, long
+//   sums are split until there are 512 workgroups (128 x 4096 x 4096 unsplit 24,
+//   in four 17.4; 512 x 1024 x 4096 20 / 17.3); short ones take tiles of 32 x 64
+//   (128 x 4096 x 1024 8.9 / 7.3, split in two 10.0).
+enum Kernel { kRows, kWide32x64, kWide64x64, kWide64x128, kWide128x256 };
+struct Plan {
+    Kernel kernel;
+    int splits;
+};
+Plan plan_of(const W4Shape& s, int64_t M) {
+    if (M <= 32 || (M <= 64 && s.tiles_k <= 8 && s.tiles_n <= 256)) return {kRows, 1};
+    auto tiles = [&](int tm, int tn) { return ((M + tm - 1) / tm) * ((s.N + tn - 1) / tn); };
+    if (tiles(128, 256) >= 256) return {kWide128x256, 1};
+    if (tiles(64, 128) >= 256) return {kWide64x128, 1};
+    const int64_t t = tiles(64, 64);
+    if (s.tiles_k <= 8) return {t >= 256 ? kWide64x64 : kWide32x64, 1};
+    const int64_t splits = std::min<int64_t>({512 / t, s.tiles_k / 4, 8});
+    return {kWide64x64, (int)std::max<int64_t>(splits, 1)};
+}
 
-template <bool E2M1, bool ZEROS, int PT, int MT>
+template <bool E2M1, bool ZEROS, int PT, int MT, int NT>
 void launch_rows(const W4Args& g, hipStream_t stream) {
     const int waves = g.s.tiles_k >= 8 ? 8 : 4;
-    const dim3 grid((unsigned)g.s.tiles_n, (unsigned)((g.c.M + 16 * MT - 1) / (16 * MT)));
-    const size_t sums = (size_t)waves * MT * 1024;
-    if constexpr (MT == 1) {
-        // 16 rows and their padding, or as many as there are
+    const dim3 grid((unsigned)((g.s.tiles_n + NT - 1) / NT), (unsigned)((g.c.M + 16 * MT - 1) / (16 * MT)));
+    const size_t sums = (size_t)waves * NT * MT * 1024;
+    if constexpr (MT == 1 && NT == 1) {
         const size_t rows = (size_t)g.c.M * staged_stride(g.s.K) * 2;
         if (rows <= kStaged) {
-            w4_rows_kernel<E2M1, ZEROS, PT, MT, true><<<grid, 64 * waves, std::max(rows, sums), stream>>>(g);
+            w4_rows_kernel<E2M1, ZEROS, PT, MT, NT, true><<<grid, 64 * waves, std::max(rows, sums), stream>>>(g);
             return;
         }
     }
-    w4_rows_kernel<E2M1, ZEROS, PT, MT, false><<<grid, 64 * waves, sums, stream>>>(g);
+    w4_rows_kernel<E2M1, ZEROS, PT, MT, NT, false><<<grid, 64 * waves, sums, stream>>>(g);
 }
 
-template <bool E2M1, bool ZEROS, int PT, int MI, int NI>
-void launch_wide(const W4Args& g, hipStream_t stream) {
-    using S = Wide<MI, NI>;
-    auto* k = &w4_wide_kernel<E2M1, ZEROS, PT, MI, NI>;
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
+template <bool E2M1, bool ZEROS, int PT, int MI, int NI, int WN>
+void launch_wide(const W4Args& g, int splits, float* partial, hipStream_t stream) {
+    using S = Wide<MI, NI, WN>;
+    auto* k = &w4_wide_kernel<E2M1, ZEROS, PT, MI, NI, WN>;
+    if (S::kLds > 64 * 1024)
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)S::kLds);
     const int64_t tiles = ((g.c.M + S::TM - 1) / S::TM) * ((g.s.N + S::TN - 1) / S::TN);
-    k<<<(unsigned)tiles, 256, S::kLds, stream>>>(g);
+    k<<<(unsigned)(tiles * splits), 128 * WN, S::kLds, stream>>>(g, splits, partial);
+    if (splits > 1)
+        w4_join_kernel<<<(unsigned)((g.c.M * partial_width(g.s.N) / 4 + 255) / 256), 256, 0, stream>>>(g, splits, partial);
 }
 
 }  // namespace
 
-size_t w4_workspace_bytes(const W4Shape&, int64_t) { return 0; }
+size_t w4_workspace_bytes(const W4Shape& s, int64_t M) {
+    const int splits = plan_of(s, M).splits;
+    return splits > 1 ? align256((size_t)M * partial_width(s.N) * 4 * splits) : 0;
+}
 
-hipError_t launch_linear_w4(const W4Shape& s, const W4Call& c, void*, hipStream_t stream) {
+hipError_t launch_linear_w4(const W4Shape& s, const W4Call& c, void* workspace, hipStream_t stream) {
     const W4Args g{s, c, c.packed, c.packed + s.codes_size(),
                    s.zeros ? reinterpret_cast<const uint8_t*>(c.packed + s.codes_size() + s.scales_size()) : nullptr};
+    // a tile's rows are within 32-bit offsets of its first
+    const Plan plan = c.a_stride < 1 << 24 ? plan_of(s, c.M) : Plan{kRows, 1};
     by_weights(s, [&](auto e2m1, auto zeros, auto pt) {
         constexpr bool E2M1 = decltype(e2m1)::value, ZEROS = decltype(zeros)::value;
         constexpr int PT = decltype(pt)::value;
-        if (takes_wide(s, c.M, c.a_stride)) {
-            auto tiles = [&](int t, int u) { return ((c.M + t - 1) / t) * ((s.N + u - 1) / u); };
-            if (tiles(128, 128) >= 256)
-                launch_wide<E2M1, ZEROS, PT, 4, 4>(g, stream);
+        float* const partial = static_cast<float*>(workspace);
+        switch (plan.kernel) {
+            case kWide32x64: return launch_wide<E2M1, ZEROS, PT, 1, 2, 2>(g, plan.splits, partial, stream);
+            case kWide64x64: return launch_wide<E2M1, ZEROS, PT, 2, 2, 2>(g, plan.splits, partial, stream);
+            case kWide64x128: return launch_wide<E2M1, ZEROS, PT, 2, 2, 4>(g, plan.splits, partial, stream);
+            case kWide128x256: return launch_wide<E2M1, ZEROS, PT, 4, 4, 4>(g, plan.splits, partial, stream);
+            case kRows: break;
+        }
+        if (c.M <= 16) {
+            if (s.tiles_n >= 1024)
+                launch_rows<E2M1, ZEROS, PT, 1, 4>(g, stream);
+            else if (s.tiles_n >= 512)
+                launch_rows<E2M1, ZEROS, PT, 1, 2>(g, stream);
             else
-                launch_wide<E2M1, ZEROS, PT, 2, 2>(g, stream);
-        } else if (c.M <= 16) {
-            launch_rows<E2M1, ZEROS, PT, 1>(g, stream);
+                launch_rows<E2M1, ZEROS, PT, 1, 1>(g, stream);
         } else if (c.M <= 32) {
-            launch_rows<E2M1, ZEROS, PT, 2>(g, stream);
-        } else {
-            launch_rows<E2M1, ZEROS, PT, 4>(g, stream);
+            constexpr int kMost = PT == 4 && !E2M1 ? 2 : 4;
+            if (s.tiles_n >= 1024)
+                launch_rows<E2M1, ZEROS, PT, 2, kMost>(g, stream);
+            else if (s.tiles_n >= 512)
+                launch_rows<E2M1, ZEROS, PT, 2, 2>(g, stream);
+            else
+                launch_rows<E2M1, ZEROS, PT, 2, 1>(g, stream);
+        } else {  // also many rows at a stride that a tile's 32-bit offsets do not span
+            launch_rows<E2M1, ZEROS, PT, 4, 1>(g, stream);
         }
     });
     return hipGetLastError();

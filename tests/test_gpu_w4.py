@@ -132,7 +132,11 @@ class Exact:
 # many rows; wide and long
 SIZES = [(1, 1, 32), (1, 16, 128), (2, 17, 96), (15, 33, 160), (16, 50, 1024), (17, 64, 288), (31, 48, 544), (33, 16, 2080),
          (48, 100, 256), (64, 31, 640), (65, 130, 384), (100, 257, 192), (128, 128, 512), (129, 129, 1056), (200, 96, 128),
-         (257, 320, 448), (513, 65, 96), (700, 512, 1024), (1, 2047, 4128), (3, 16, 16384), (8, 4100, 64)]
+         (257, 320, 448), (513, 65, 96), (700, 512, 1024), (1, 2047, 4128), (3, 16, 16384), (8, 4100, 64),
+         # wide calls of few rows (32 and 64 outputs a workgroup), sums split over workgroups, and the large tiles, each
+         # with rows and outputs that end inside one
+         (1, 8200, 160), (5, 16400, 96), (16, 16399, 64), (20, 8194, 96), (32, 16400, 288), (40, 4100, 64), (70, 200, 2112),
+         (64, 130, 4128), (1000, 1050, 96), (1030, 2100, 288), (1030, 2101, 1184), (2100, 4000, 160), (2177, 4100, 544)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=[f"{m}x{n}x{k}" for m, n, k in SIZES])
@@ -220,11 +224,12 @@ def test_linear_large_values(gpu):
             same(out, c.ref(bias=False) * 2.0 ** power)
 
 
-@pytest.mark.parametrize("M", [1, 40, 260])
+@pytest.mark.parametrize("M", [1, 40, 260, 90])
 def test_linear_streams_and_graphs(gpu, M):
     """On another stream, two at once with a workspace each, and captured and replayed over changing rows with eager calls
     between."""
-    c = Exact(M, 96, 640, TYPES[3], seed=4)
+    c = Exact(M, 96, 640 if M != 90 else 2144, TYPES[3], seed=4)  # 90 rows: split sums, joined through the workspace
+    assert (w4.workspace_bytes(c.cfg, M) > 0) == (M == 90)
     a, packed = c.args(gpu)
     a = a.contiguous()
     ref = c.ref(bias=False)
@@ -254,6 +259,21 @@ def test_linear_streams_and_graphs(gpu, M):
         torch.cuda.synchronize()
         same(out, k * ref)
         assert torch.equal(eager, out)
+
+
+def test_linear_rows_far_apart(gpu):
+    """Rows 2^24 elements apart: offsets past 32 bits."""
+    c = Exact(70, 40, 160, TYPES[3], seed=8)
+    a, packed = c.args(gpu)
+    far = torch.empty(70 << 24, dtype=torch.bfloat16, device=gpu).view(70, 1 << 24)
+    far[:, :160].copy_(a)
+    far[:, 160:320] = float("nan")
+    log("w4 far rows")
+    same(w4.lsh_linear_w4(c.cfg, far[:, :160], packed), c.ref(bias=False))
+    near = torch.empty(70 << 22, dtype=torch.bfloat16, device=gpu).view(70, 1 << 22)
+    near[:, :160].copy_(a)
+    near[:, 160:320] = float("nan")
+    same(w4.lsh_linear_w4(c.cfg, near[:, :160], packed), c.ref(bias=False))
 
 
 def test_bf16_products_of_the_same_weights(gpu):
