@@ -570,13 +570,14 @@ struct Spot {
     int n, k, word, pair;  // output, first input, word of the tile (of 256), row r
     bool in;
 };
+constexpr int kGridY = 32768;  // rows of tiles in the grid's second dimension
 __device__ __forceinline__ Spot spot_of(const W4Shape& s) {
     const int r = threadIdx.x >> 4, j = threadIdx.x & 15;
-    const int64_t tn = blockIdx.x / s.tiles_k, tk = blockIdx.x - tn * s.tiles_k;
+    const int64_t tn = (int64_t)blockIdx.z * kGridY + blockIdx.y;
     Spot p;
-    p.tile = blockIdx.x;
+    p.tile = tn * s.tiles_k + blockIdx.x;
     p.n = (int)(16 * tn) + r;
-    p.k = (int)(128 * tk) + 8 * j;
+    p.k = (int)(128 * blockIdx.x) + 8 * j;
     p.word = (16 * (j & 3) + r) * 4 + (j >> 2);
     p.pair = r;
     p.in = p.n < s.N && p.k < s.K;
@@ -596,92 +597,109 @@ __device__ __forceinline__ uint32_t code_at(uint32_t w, int e, bool e2m1) {
     return (w >> (e2m1 ? 4 * e : (e < 4 ? 8 * e : 8 * (e - 4) + 4))) & 15u;
 }
 
-// Over the aligned group of 2^k lanes (4, 8 or 16) that holds a group's values.
-template <typename F>
-__device__ __forceinline__ float group_fold(float x, int lanes, F f) {
-    for (int o = 1; o < lanes; o <<= 1) x = f(x, __shfl_xor(x, o));
+// Over the aligned group of LANES lanes that holds a group's values, by moves within
+// a row of sixteen.
+template <int LANES, typename F>
+__device__ __forceinline__ float group_fold(float x, F f) {
+    x = f(x, dpp_f32<kDppXor1>(x));
+    x = f(x, dpp_f32<kDppXor2>(x));
+    if constexpr (LANES > 4) x = f(x, dpp_f32<kDppHalfMirror>(x));
+    if constexpr (LANES > 8) x = f(x, dpp_f32<kDppMirror>(x));
     return x;
 }
 
-// The smallest bf16 value s with steps * s >= reach (finite), as its bits: one
-// of four from just below the rounded quotient on, compared exactly in fp64.
-__device__ __forceinline__ uint32_t scale_for(double reach, double steps) {
-    uint32_t b = __float_as_uint((float)(reach / steps)) >> 16;
+// The smallest bf16 value s with steps * s >= hi - lo (finite), as its bits: one of
+// four from just below the rounded quotient on, compared exactly in fp64.
+__device__ __forceinline__ uint32_t scale_for(float hi, float lo, float steps) {
+    const double reach = (double)hi - (double)lo;
+    uint32_t b = __float_as_uint((float)(reach * (1. / (double)steps))) >> 16;  // reach itself may pass fp32's range
     b = b > 0 ? b - 1 : 0;
 #pragma unroll
     for (int i = 0; i < 3; ++i)
-        if (steps * (double)bf16_bits_to_f32(b) < reach) ++b;
+        if ((double)steps * (double)bf16_bits_to_f32(b) < reach) ++b;
     return b;
 }
 
-template <bool F32>
+// x / s to the nearest whole number, ties to even, for a bf16 s > 0 and |x| <= 15.5
+// s, from a whole number at most one away: by the remainder, which one fused
+// operation gives exactly (n s has 12 bits, and x - n s no more than x's at s).
+__device__ __forceinline__ float put_right(float n, float x, float s) {
+    const float r = 2.f * fmaf(-n, s, x), off = fabsf(r);
+    return n + (off > s || (off == s && ((int)n & 1)) ? copysignf(1.f, r) : 0.f);
+}
+
+// HBM-bound but for short calls: 16384 x 4096 in fp32 to int4 with zero points 67 us
+// (302 MB, 4.5 TB/s); 106 with quotients in fp64, 86 with put_right() for every value.
+template <bool F32, bool E2M1, bool ZEROS, int PT>
 __global__ __launch_bounds__(256) void w4_quantize_kernel(W4Shape s, const void* __restrict__ w,
                                                           char* __restrict__ packed) {
+    constexpr int LANES = 16 / PT;  // of a group
     __shared__ uint32_t words[256];
     const Spot p = spot_of(s);
+    if (p.n - (int)(threadIdx.x >> 4) >= s.N) return;  // a row of tiles past the last: the same for the workgroup
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (p.in) {
-        const int64_t at = (int64_t)p.n * s.K + p.k;
-        if constexpr (F32) {
-            const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(w) + at);
-            const f32x4 lo = src[0], hi = src[1];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = lo[e], x[4 + e] = hi[e];
-        } else {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(w) + at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __uint_as_float(v[e] << 16);
-                x[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
-            }
-        }
-    }
-    float lo = 0.f, hi = 0.f, bad = 0.f;
+    if (p.in) load8<F32>(w, (int64_t)p.n * s.K + p.k, x);
+    float lo = 0.f, hi = 0.f, big = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        if (!(fabsf(x[e]) < __builtin_inff())) bad = 1.f;
+        if constexpr (ZEROS) lo = fminf(lo, x[e]);
+        if constexpr (ZEROS) hi = fmaxf(hi, x[e]);
+        // magnitudes as bits: those of infinities and NaN are the largest, and as floats fmaxf drops NaN
+        big = __uint_as_float(max(__float_as_uint(big), __float_as_uint(x[e]) & 0x7FFFFFFFu));
     }
-    const int lanes = s.group / 8;
-    lo = group_fold(lo, lanes, [](float a, float b) { return fminf(a, b); });
-    hi = group_fold(hi, lanes, [](float a, float b) { return fmaxf(a, b); });
-    bad = group_fold(bad, lanes, [](float a, float b) { return fmaxf(a, b); });
-    const int j = threadIdx.x & 15, per = s.per_tile(), at = scale_place(s, p.pair, j / lanes);
-    char* const scales = packed + s.codes_size() + p.tile * (16 * per * (int64_t)s.scale_bytes());
-    uint8_t* const zeros = reinterpret_cast<uint8_t*>(packed + s.codes_size() + s.scales_size()) + p.tile * 16 * per;
-    uint32_t code[8];
-    if (s.e2m1) {
+    auto most = [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); };
+    if constexpr (ZEROS) {
+        lo = group_fold<LANES>(lo, [](float a, float b) { return fminf(a, b); });
+        hi = group_fold<LANES>(hi, [](float a, float b) { return fmaxf(a, b); });
+    }
+    big = group_fold<LANES>(big, most);
+    const bool bad = __float_as_uint(big) >= 0x7F800000u;
+    const int j = threadIdx.x & 15, at = scale_place(s, p.pair, j / LANES);
+    char* const scales = packed + s.codes_size() + p.tile * (16 * PT * (E2M1 ? 1 : 2));
+    uint8_t* const zeros = reinterpret_cast<uint8_t*>(packed + s.codes_size() + s.scales_size()) + p.tile * 16 * PT;
+    uint32_t word = 0;
+    if constexpr (E2M1) {
         // the smallest exponent that brings the largest magnitude to 6 = 1.5 * 2^2 or below
-        const uint32_t big = __float_as_uint(fmaxf(hi, -lo));
-        const int byte = bad > 0.f ? 255 : max((int)(big >> 23) - 2 + ((big & 0x7FFFFFu) > 0x400000u ? 1 : 0), 0);
-        uint32_t c = 0;
+        const uint32_t bits = __float_as_uint(big);
+        const int byte = bad ? 255 : max((int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x400000u ? 1 : 0), 0);
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = bad > 0.f ? 0.f : ldexpf(x[e], 127 - byte);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[0], y[1], 1.f, 0);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[2], y[3], 1.f, 1);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[4], y[5], 1.f, 2);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[6], y[7], 1.f, 3);
-        words[p.word] = c;
-        if (j % lanes == 0) scales[at] = (char)(uint8_t)(p.in ? byte : 0);
+        for (int e = 0; e < 8; ++e) y[e] = ldexpf(x[e], 127 - byte);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, y[0], y[1], 1.f, 0);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, y[2], y[3], 1.f, 1);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, y[4], y[5], 1.f, 2);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, y[6], y[7], 1.f, 3);
+        if (j % LANES == 0) scales[at] = (char)(uint8_t)(p.in ? byte : 0);
     } else {
-        const double reach = s.zeros ? (double)hi - (double)lo : (double)fmaxf(hi, -lo);
-        uint32_t bits = scale_for(bad > 0.f ? 0. : reach, s.zeros ? 15. : 7.);
-        const double by = bits ? (double)bf16_bits_to_f32(bits) : 1.;
-        const double z = s.zeros ? fmin(rint(-(double)lo / by), 15.) : 8.;
+        if (bad) lo = hi = big = 0.f;
+        const uint32_t bits = ZEROS ? scale_for(hi, lo, 15.f) : scale_for(big, 0.f, 7.f);
+        float by = bits ? bf16_bits_to_f32(bits) : 1.f;
+        const float lift = by < 0x1p-100f ? 0x1p60f : 1.f;  // exact, and 1 / by stays within fp32
+        by *= lift;
+        const float inv = 1.f / by;
+        const float z = ZEROS ? fminf(put_right(rintf(-lo * lift * inv), -lo * lift, by), 15.f) : 8.f;
+        float n[8], far = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)  // quotients in fp64: values next to a border fall on their side of it
-            code[e] = bad > 0.f ? 0u : (uint32_t)fmin(fmax(rint((double)x[e] / by) + z, 0.), 15.);
-        if (bad > 0.f) bits = 0x7FC0u;
-        words[p.word] = p.in ? word_of(code, false) : 0u;
-        if (j % lanes == 0) {
-            reinterpret_cast<uint16_t*>(scales)[at] = (uint16_t)(p.in ? bits : 0u);
-            if (s.zeros) zeros[at] = (uint8_t)(p.in && !(bad > 0.f) ? (uint32_t)z : 0u);
+        for (int e = 0; e < 8; ++e) {
+            x[e] *= lift;
+            const float quot = x[e] * inv;  // within 2^-18 of the exact one
+            n[e] = rintf(quot);
+            far = fmaxf(far, fabsf(quot - n[e]));
+        }
+        if (__any(far > 0.49999f))  // a border may lie between
+#pragma unroll
+            for (int e = 0; e < 8; ++e) n[e] = put_right(n[e], x[e], by);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            word |= (uint32_t)fminf(fmaxf(n[e] + z, 0.f), 15.f) << (e < 4 ? 8 * e : 8 * (e - 4) + 4);
+        if (j % LANES == 0) {
+            reinterpret_cast<uint16_t*>(scales)[at] = (uint16_t)(!p.in ? 0u : bad ? 0x7FC0u : bits);
+            if constexpr (ZEROS) zeros[at] = (uint8_t)(p.in ? (uint32_t)z : 0u);
         }
     }
+    words[p.word] = p.in && !bad ? word : 0u;
     __syncthreads();
     reinterpret_cast<uint32_t*>(packed + p.tile * 1024)[threadIdx.x] = words[threadIdx.x];
 }
@@ -691,6 +709,7 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(W4Shape s, const uint8_t* 
                                                       const uint8_t* __restrict__ zeros, char* __restrict__ packed) {
     __shared__ uint32_t words[256];
     const Spot p = spot_of(s);
+    if (p.n - (int)(threadIdx.x >> 4) >= s.N) return;  // a row of tiles past the last: the same for the workgroup
     uint32_t w = 0;
     if (p.in) w = *reinterpret_cast<const uint32_t*>(codes + ((int64_t)p.n * s.K + p.k) / 2);
     if (!s.e2m1) {
@@ -724,35 +743,24 @@ __global__ __launch_bounds__(256) void w4_unpack_kernel(W4Shape s, const char* _
     if (!p.in) return;
     const uint32_t w = reinterpret_cast<const uint32_t*>(packed + p.tile * 1024)[p.word];
     const int j = threadIdx.x & 15, per = s.per_tile();
-    const int64_t at = p.tile * 16 * per + scale_place(s, p.pair, j / (s.group / 8));
+    const int64_t at = p.tile * 16 * per + scale_place(s, p.pair, (8 * j) / s.group);
     const char* const sc = packed + s.codes_size();
     float v[8];
     if (s.e2m1) {
         const uint32_t byte = (uint8_t)sc[at];
-        const float lowest[8] = {0.f, 0.5f, 1.f, 1.5f, 2.f, 3.f, 4.f, 6.f};
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 pairs[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1),
+                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3)};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t c = code_at(w, e, true);
-            const float a = byte == 255 ? __builtin_nanf("") : ldexpf(lowest[c & 7], (int)byte - 127);
-            v[e] = c & 8 ? -a : a;
-        }
+        for (int e = 0; e < 8; ++e)
+            v[e] = byte == 255 ? __builtin_nanf("") : ldexpf(pairs[e >> 1][e & 1], (int)byte - 127);
     } else {
         const float scale = bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(sc)[at]);
         const float z = s.zeros ? (float)(uint8_t)(packed + s.codes_size() + s.scales_size())[at] : 8.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = scale * ((float)code_at(w, e, false) - z);
     }
-    const int64_t to = (int64_t)p.n * s.K + p.k;
-    if constexpr (F32) {
-        f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(out) + to);
-        dst[0] = f32x4{v[0], v[1], v[2], v[3]};
-        dst[1] = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-        u32x4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + to) = y;
-    }
+    store8<F32>(out, (int64_t)p.n * s.K + p.k, v);
 }
 
 template <typename Go>
@@ -769,29 +777,36 @@ void by_weights(const W4Shape& s, Go go) {
         with(integral_constant<int, 1>{});
 }
 
-unsigned tiles(const W4Shape& s) { return (unsigned)(s.tiles_n * s.tiles_k); }
+dim3 tile_grid(const W4Shape& s) {
+    const int64_t y = std::min<int64_t>(s.tiles_n, kGridY);
+    return dim3((unsigned)s.tiles_k, (unsigned)y, (unsigned)((s.tiles_n + kGridY - 1) / kGridY));
+}
 
 }  // namespace
 
 hipError_t launch_w4_quantize(const W4Shape& s, bool f32, const void* w, char* packed, hipStream_t stream) {
-    if (f32)
-        w4_quantize_kernel<true><<<tiles(s), 256, 0, stream>>>(s, w, packed);
-    else
-        w4_quantize_kernel<false><<<tiles(s), 256, 0, stream>>>(s, w, packed);
+    by_weights(s, [&](auto e2m1, auto zeros, auto pt) {
+        constexpr bool E2M1 = decltype(e2m1)::value, ZEROS = decltype(zeros)::value;
+        constexpr int PT = decltype(pt)::value;
+        if (f32)
+            w4_quantize_kernel<true, E2M1, ZEROS, PT><<<tile_grid(s), 256, 0, stream>>>(s, w, packed);
+        else
+            w4_quantize_kernel<false, E2M1, ZEROS, PT><<<tile_grid(s), 256, 0, stream>>>(s, w, packed);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_w4_pack(const W4Shape& s, const uint8_t* codes, const void* scales, const uint8_t* zeros,
                           char* packed, hipStream_t stream) {
-    w4_pack_kernel<<<tiles(s), 256, 0, stream>>>(s, codes, scales, zeros, packed);
+    w4_pack_kernel<<<tile_grid(s), 256, 0, stream>>>(s, codes, scales, zeros, packed);
     return hipGetLastError();
 }
 
 hipError_t launch_w4_unpack(const W4Shape& s, bool f32, const char* packed, void* w, hipStream_t stream) {
     if (f32)
-        w4_unpack_kernel<true><<<tiles(s), 256, 0, stream>>>(s, packed, w);
+        w4_unpack_kernel<true><<<tile_grid(s), 256, 0, stream>>>(s, packed, w);
     else
-        w4_unpack_kernel<false><<<tiles(s), 256, 0, stream>>>(s, packed, w);
+        w4_unpack_kernel<false><<<tile_grid(s), 256, 0, stream>>>(s, packed, w);
     return hipGetLastError();
 }
 
