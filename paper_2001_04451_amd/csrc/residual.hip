@@ -186,9 +186,10 @@ __device__ __forceinline__ void norm_back(const ResidualArgs& a, RowSums<WAVES, 
     for (int e = 0; e < 8; ++e) d[e] = r * (d[e] - t - n[e] * s);
 }
 
-// partial: [workgroup][5][D]
-template <bool F32, int WAVES>
-__global__ __launch_bounds__(kThreads<WAVES>) void residual_bwd_kernel(
+// partial: [workgroup][5][D].  PLAIN: neither scale nor biases, whose sums and
+// weights then take no registers: four waves a SIMD in place of three.
+template <bool F32, bool PLAIN, int WAVES>
+__global__ __launch_bounds__(kThreads<WAVES>, PLAIN || WAVES == 16 ? 4 : 3) void residual_bwd_kernel(
     ResidualArgs a, const float* __restrict__ y, const void* __restrict__ f, const void* __restrict__ gate,
     const float* __restrict__ dy, const float* __restrict__ dz, ResidualGrads g, float* __restrict__ partial) {
     constexpr int ROWS = kRows<WAVES>;
@@ -197,9 +198,9 @@ __global__ __launch_bounds__(kThreads<WAVES>) void residual_bwd_kernel(
     const Place<WAVES> p(a.D);
     RowSums<WAVES, ROWS> sums{lds, 0, p.row, p.wave};
     float sc[8], pg[8], pb[8], rg[8], col[5][8];
-    weights8(a.scale, p.col, p.on, 1.f, sc);
+    weights8(PLAIN ? nullptr : a.scale, p.col, p.on, 1.f, sc);
     weights8(a.post_g, p.col, p.on, 1.f, pg);
-    weights8(a.post_b, p.col, p.on, 0.f, pb);
+    weights8(PLAIN ? nullptr : a.post_b, p.col, p.on, 0.f, pb);
     weights8(a.pre_g, p.col, p.on, 1.f, rg);
 #pragma unroll
     for (int i = 0; i < 5; ++i)
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kThreads<WAVES>) void residual_bwd_kernel(
                 v[e] = (v[e] - mv) * rv;
                 if (mine) {
                     col[3][e] = fmaf(dw[e], v[e], col[3][e]);
-                    col[4][e] += dw[e];
+                    if constexpr (!PLAIN) col[4][e] += dw[e];
                 }
                 dw[e] *= rg[e];
             }
@@ -247,9 +248,11 @@ __global__ __launch_bounds__(kThreads<WAVES>) void residual_bwd_kernel(
             h[e] = dm * sc[e] * slope;
             dv[e] *= a.alpha * sc[e] * gv;
             if (mine) {
-                col[0][e] = fmaf(dm, gv, col[0][e]);
                 col[1][e] = fmaf(dv[e], n[e], col[1][e]);
-                col[2][e] += dv[e];
+                if constexpr (!PLAIN) {
+                    col[0][e] = fmaf(dm, gv, col[0][e]);
+                    col[2][e] += dv[e];
+                }
             }
             dv[e] *= a.post ? pg[e] : 1.f;
         }
@@ -260,7 +263,7 @@ __global__ __launch_bounds__(kThreads<WAVES>) void residual_bwd_kernel(
     float* const out = partial + (int64_t)blockIdx.x * 5 * a.D;
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
-        if (!g.cols[i]) continue;  // uniform
+        if ((PLAIN && i != 1 && i != 3) || !g.cols[i]) continue;  // uniform
         if constexpr (ROWS == 1) {
             if (p.on) store8<true>(out, (int64_t)i * a.D + p.col, col[i]);
         } else {
@@ -277,23 +280,25 @@ __global__ __launch_bounds__(kThreads<WAVES>) void residual_bwd_kernel(
     }
 }
 
-// One workgroup for 64 columns of one weight: its workgroups' partial sums added
-// in fp64, in sixteen interleaved runs and then those in order.
-__global__ __launch_bounds__(1024) void residual_cols_kernel(const float* __restrict__ partial, int parts, int D,
-                                                             ResidualGrads g) {
-    __shared__ double run[16][64];
-    const int i = blockIdx.y, d = threadIdx.x & 63, s = threadIdx.x >> 6, c = min((int)blockIdx.x * 64 + d, D - 1);
+// One workgroup for 32 columns of one weight: its workgroups' partial sums added in
+// fp64, in 32 interleaved runs and then those in halves.
+constexpr int kRuns = 32, kRunCols = 32;
+__global__ __launch_bounds__(kRuns* kRunCols) void residual_cols_kernel(const float* __restrict__ partial, int parts,
+                                                                        int D, ResidualGrads g) {
+    __shared__ double run[kRuns][kRunCols];
+    const int i = blockIdx.y, d = threadIdx.x % kRunCols, s = threadIdx.x / kRunCols;
+    const int c = (int)blockIdx.x * kRunCols + d;
     float* const to = i == 0 ? g.cols[0] : i == 1 ? g.cols[1] : i == 2 ? g.cols[2] : i == 3 ? g.cols[3] : g.cols[4];
     if (!to) return;  // uniform
     double z = 0;
 #pragma unroll 8
-    for (int p = s; p < parts; p += 16) z += partial[((int64_t)p * 5 + i) * D + c];
+    for (int p = s; p < parts; p += kRuns) z += partial[((int64_t)p * 5 + i) * D + min(c, D - 1)];
     run[s][d] = z;
-    __syncthreads();
-    if (s == 0 && (int)blockIdx.x * 64 + d < D) {
-        for (int k = 1; k < 16; ++k) z += run[k][d];
-        to[c] = (float)z;
+    for (int h = kRuns / 2; h > 0; h /= 2) {
+        __syncthreads();
+        if (s < h) run[s][d] += run[s + h][d];
     }
+    if (s == 0 && c < D) to[c] = (float)run[0][d];
 }
 
 int waves_of(int D) {
@@ -304,10 +309,14 @@ int waves_of(int D) {
 int rows_of(int D) { return std::max(1, 4 / waves_of(D)); }
 // Workgroups: as many as are resident at once, at most.
 int64_t groups(const ResidualArgs& a, int waves_cu) {
-    return std::min<int64_t>((a.T + rows_of(a.D) - 1) / rows_of(a.D), 256 * waves_cu / std::max(4, waves_of(a.D)));
+    return std::min<int64_t>((a.T + rows_of(a.D) - 1) / rows_of(a.D), std::max(256, 256 * waves_cu / std::max(4, waves_of(a.D))));
 }
 int64_t fwd_groups(const ResidualArgs& a) { return groups(a, 32); }
-int64_t bwd_groups(const ResidualArgs& a) { return groups(a, 16); }
+// The backward's workgroups: of rows side by side, all resident at once (12 waves a
+// CU, 16 where neither scale nor biases take registers), so that no second round
+// of a few of them follows.
+int64_t bwd_groups(const ResidualArgs& a, bool plain) { return groups(a, plain || waves_of(a.D) == 16 ? 16 : 12); }
+bool is_plain(const ResidualArgs& a) { return !a.scale && !a.post_b && !a.pre_b; }
 
 template <typename Go>
 void by_width(int D, Go go) {
@@ -325,7 +334,7 @@ void by_width(int D, Go go) {
 bool residual_fits(const ResidualArgs&) { return true; }  // the grids are bounded by the chip's size
 
 size_t residual_workspace_bytes(const ResidualArgs& a) {
-    return align256((size_t)bwd_groups(a) * 5 * a.D * sizeof(float));
+    return align256((size_t)bwd_groups(a, true) * 5 * a.D * sizeof(float));  // the more of both
 }
 
 hipError_t launch_residual_fwd(const ResidualArgs& a, bool f32, const float* x, const void* f, const void* gate,
@@ -345,19 +354,21 @@ hipError_t launch_residual_bwd(const ResidualArgs& a, bool f32, const float* y, 
                                const float* dy, const float* dz, const ResidualGrads& g, void* workspace,
                                hipStream_t stream) {
     float* const partial = static_cast<float*>(workspace);
-    const unsigned grid = (unsigned)bwd_groups(a);
+    const bool plain = is_plain(a);
+    const unsigned grid = (unsigned)bwd_groups(a, plain);
     by_width(a.D, [&](auto w) {
         constexpr int W = decltype(w)::value;
+        auto go = [&](auto kernel) { kernel<<<grid, kThreads<W>, 0, stream>>>(a, y, f, gate, dy, dz, g, partial); };
         if (f32)
-            residual_bwd_kernel<true, W><<<grid, kThreads<W>, 0, stream>>>(a, y, f, gate, dy, dz, g, partial);
+            plain ? go(residual_bwd_kernel<true, true, W>) : go(residual_bwd_kernel<true, false, W>);
         else
-            residual_bwd_kernel<false, W><<<grid, kThreads<W>, 0, stream>>>(a, y, f, gate, dy, dz, g, partial);
+            plain ? go(residual_bwd_kernel<false, true, W>) : go(residual_bwd_kernel<false, false, W>);
     });
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     bool any = false;
     for (const float* c : g.cols) any = any || c;
     if (!any) return hipSuccess;
-    residual_cols_kernel<<<dim3((unsigned)((a.D + 63) / 64), 5), 1024, 0, stream>>>(partial, (int)grid, a.D, g);
+    residual_cols_kernel<<<dim3((unsigned)((a.D + kRunCols - 1) / kRunCols), 5), kRuns * kRunCols, 0, stream>>>(partial, (int)grid, a.D, g);
     return hipGetLastError();
 }
 

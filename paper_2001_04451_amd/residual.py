@@ -184,7 +184,12 @@ def lsh_residual_norm_fwd(cfg: ResidualConfig, x, f, gate, weights: ResidualWeig
     y = x.new_empty(shape) if y is None and x is not None else _take(y, shape, torch.float32, dev, "y")
     if z is not None and not cfg.pre:
         raise ValueError("z goes with pre")
-    z = _take(z, shape, own, dev, "z") if cfg.pre else None
+    if not cfg.pre:
+        z = None
+    elif z is None and f is not None:
+        z = f.new_empty(shape)
+    else:
+        z = _take(z, shape, own, dev, "z")
     p = lsh._ptr
     with lsh.on_device(dev):
         lsh._check("lsh_residual_norm_fwd",
