@@ -304,6 +304,7 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
 // 128 inputs, copied there by buffer loads that the kernel counts by hand; codes
 // are widened in the registers of the waves that use them.  A call with few tiles
 // splits its inputs over workgroups, whose sums a second kernel joins in order.
+constexpr int kMostSplits = 8;
 __host__ __device__ constexpr int partial_width(int N) { return (N + 3) & ~3; }
 
 template <int MI, int NI, int WN>
@@ -553,9 +554,13 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Args g, int splits, cons
     const int width = partial_width(g.s.N);
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = g.c.M * width;
     if (at >= all) return;
-    f32x4 v = *reinterpret_cast<const f32x4*>(partial + at);
-#pragma unroll 4
-    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(partial + s * all + at);
+    f32x4 part[kMostSplits];  // their loads in flight together
+#pragma unroll
+    for (int s = 0; s < kMostSplits; ++s)
+        part[s] = s < splits ? *reinterpret_cast<const f32x4*>(partial + s * all + at) : kNone;
+    f32x4 v = part[0];
+#pragma unroll
+    for (int s = 1; s < kMostSplits; ++s) v += part[s];
     const int64_t m = at / width;
     put4(g, m, (int)(at - m * width), v);
 }
@@ -825,7 +830,7 @@ namespace {
 //   Up to 64 rows the same where there is little to split (64 x 4096 x 1024 6.6
 //   against the wide kernel's 7.2; 64 x 4096 x 4096 18.2 against 13.5).
 //   Beyond: the wide kernel, in the largest tiles that make a workgroup for every
-//   CU: 2048 x 4096 x 1024 in tiles of 128 x 256 28.1, 64 x 128 30.5, 64 x 64 38;
+//   CU (and are not mostly past N): 2048 x 4096 x 1024 in tiles of 128 x 256 28.1, 64 x 128 30.5, 64 x 64 38;
 //   1024 x 4096 x 1024 26 / 17.5 / 21.  With fewer tiles of 64 x 64 than that, long
 //   sums are split until there are 512 workgroups (128 x 4096 x 4096 unsplit 24,
 //   in four 17.4; 512 x 1024 x 4096 20 / 17.3); short ones take tiles of 32 x 64
@@ -838,11 +843,11 @@ struct Plan {
 Plan plan_of(const W4Shape& s, int64_t M) {
     if (M <= 32 || (M <= 64 && s.tiles_k <= 8 && s.tiles_n <= 256)) return {kRows, 1};
     auto tiles = [&](int tm, int tn) { return ((M + tm - 1) / tm) * ((s.N + tn - 1) / tn); };
-    if (tiles(128, 256) >= 256) return {kWide128x256, 1};
-    if (tiles(64, 128) >= 256) return {kWide64x128, 1};
+    if (tiles(128, 256) >= 256 && s.N > 128) return {kWide128x256, 1};
+    if (tiles(64, 128) >= 256 && s.N > 64) return {kWide64x128, 1};
     const int64_t t = tiles(64, 64);
     if (s.tiles_k <= 8) return {t >= 256 ? kWide64x64 : kWide32x64, 1};
-    const int64_t splits = std::min<int64_t>({512 / t, s.tiles_k / 4, 8});
+    const int64_t splits = std::min<int64_t>({512 / t, s.tiles_k / 4, kMostSplits});
     return {kWide64x64, (int)std::max<int64_t>(splits, 1)};
 }
 

@@ -111,8 +111,9 @@ class ResidualWeights:
         object.__setattr__(self, "_checked", (cfg, device))
 
     def ref(self):
-        c = ResidualWeightsC(*[lsh._ptr(getattr(self, n)) for n in WEIGHTS])
-        return ctypes.byref(c)
+        p = lsh._ptr
+        return ctypes.byref(ResidualWeightsC(p(self.scale), p(self.post_g), p(self.post_b), p(self.pre_g),
+                                             p(self.pre_b)))
 
 
 def workspace_bytes(cfg: ResidualConfig) -> int:
@@ -147,13 +148,13 @@ def _inputs(cfg: ResidualConfig, f, gate, weights, like):
     weights.check(cfg, dev)
     if f is None:
         return cfg, None, dev
-    code, own = lsh._dtype_code(f), {"f_stride": _rows(f, cfg, "f", cfg.f_stride)}
+    code, f_stride, gate_stride = lsh._dtype_code(f), _rows(f, cfg, "f", cfg.f_stride), cfg.gate_stride
     if gate is not None:
-        own["gate_stride"] = _rows(gate, cfg, "gate", cfg.gate_stride)
+        gate_stride = _rows(gate, cfg, "gate", gate_stride)
         if gate.dtype != f.dtype or gate.device != dev:
             raise ValueError(f"gate is {gate.dtype} on {gate.device}, f {f.dtype} on {dev}")
-    if own.get("f_stride") != cfg.f_stride or own.get("gate_stride", cfg.gate_stride) != cfg.gate_stride:
-        cfg = replace(cfg, **own)
+    if f_stride != cfg.f_stride or gate_stride != cfg.gate_stride:
+        cfg = replace(cfg, f_stride=f_stride, gate_stride=gate_stride)
     return cfg, code, dev
 
 

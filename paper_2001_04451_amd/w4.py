@@ -95,12 +95,11 @@ def _packed(cfg: W4Config, packed, device) -> torch.Tensor:
     n = cfg.bytes()
     if packed is None:
         return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
-    if packed.dtype != torch.uint8 or packed.dim() != 1 or packed.numel() < n:
-        raise ValueError(f"packed has {packed.numel()} elements of {packed.dtype}, expected {n} of uint8 or more")
+    if packed.dtype != torch.uint8 or packed.numel() < n or not packed.is_contiguous():
+        raise ValueError(f"packed has {packed.numel()} elements of {packed.dtype}, expected {n} of uint8 or more, "
+                         "next to each other")
     if packed.device != device:
         raise ValueError(f"packed is on {packed.device}, the tensors on {device}")
-    if not packed.is_cuda or not packed.is_contiguous():
-        raise ValueError("packed must be contiguous memory of a GPU")
     return packed
 
 
@@ -137,6 +136,8 @@ def lsh_w4_pack(cfg: W4Config, codes, scales, zeros=None, packed=None) -> torch.
 
 def lsh_w4_unpack(cfg: W4Config, packed, dtype: torch.dtype = torch.float32, w=None) -> torch.Tensor:
     """The matrix w [N, K] that packed weights stand for, in fp32 (exact) or bf16 (lsh_w4_unpack)."""
+    if not packed.is_cuda:
+        raise ValueError("packed must be a GPU tensor")
     packed = _packed(cfg, packed, packed.device)
     if w is None:
         w = torch.empty((cfg.N, cfg.K), dtype=dtype, device=packed.device)
