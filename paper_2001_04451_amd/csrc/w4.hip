@@ -150,10 +150,14 @@ __device__ __forceinline__ void put4(const W4Args& g, int64_t m, int n, f32x4 v)
 }
 
 // ---------------------------------------------------------------------------
-// Few rows.  A workgroup takes 16 outputs of 16 MT rows; its waves take the
+// Few rows.  A workgroup takes 16 NT outputs of 16 MT rows; its waves take the
 // tiles of 128 inputs in turn, the codes of AHEAD of them on their way, and add
 // up in LDS.  Where the rows are short (STAGED) they pass through LDS once, while
 // the first codes are on their way; else a wave loads them tile by tile.
+// HBM-bound where the matrix is large: one row by 16384 x 16384 int4 30 us (4.6
+// TB/s), e2m1 26 (5.5), by 32000 x 4096 17 and 16; by 4096 x 1024 3.4, of which the
+// launch is 2.5.  Rows loaded tile by tile took 40 and 35 at 16384 x 16384, with
+// a tile at a time on its way 32.
 constexpr size_t kStaged = 34 * 1024;  // bytes of rows, at most
 __host__ __device__ constexpr int64_t staged_stride(int K) { return K + 32; }  // rows start 16 banks apart
 
@@ -304,6 +308,10 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
 // 128 inputs, copied there by buffer loads that the kernel counts by hand; codes
 // are widened in the registers of the waves that use them.  A call with few tiles
 // splits its inputs over workgroups, whose sums a second kernel joins in order.
+// 2048 x 4096 x 4096: int4 72 us (0.95 PFLOP/s), e2m1 57 (1.20; a bf16 product of
+// 8192^3 by the library reaches 1.39); 2048 x 4096 x 1024 25 and 21.  Bound by the
+// copies (8.8 TB/s out of L2, a workgroup a CU) with the first stages' and the
+// epilogue's latency; int4 issues a quarter more products for the sums of rows.
 constexpr int kMostSplits = 8;
 __host__ __device__ constexpr int partial_width(int N) { return (N + 3) & ~3; }
 
@@ -513,18 +521,12 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_wide_kernel(W4Args g, int spli
             }
         }
     };
-    auto add_tile = [&](int k, int slot) {
-        if (k + 1 < tiles_k)
-            add(k, slot, std::false_type{});
-        else
-            add(k, slot, std::true_type{});
-    };
     constexpr int kAhead = S::STAGES - 1;  // stages on their way: all but the one that is being read
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
         if (k0 + u < k1) copy(k0 + u, u);
     int slot = 0;
-    for (int k = k0; k < k1; ++k) {
+    auto stage = [&](int k, auto last) {
         if (k + kAhead - 1 >= k1)
             wait_loads<0>();
         else if (extra)
@@ -533,9 +535,13 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_wide_kernel(W4Args g, int spli
             wait_loads<(kAhead - 1) * S::kLoads>();
         barrier();  // this stage is there, and everyone has read the last one
         if (k + kAhead < k1) copy(k + kAhead, slot == 0 ? S::STAGES - 1 : slot - 1);
-        add_tile(k, slot);
+        add(k, slot, last);
         slot = slot + 1 == S::STAGES ? 0 : slot + 1;
-    }
+    };
+    // the tile that ends inside apart: two forms in one loop move the accumulators between them
+    const int whole = min(k1, g.s.K / 128);
+    for (int k = k0; k < whole; ++k) stage(k, std::false_type{});
+    if (whole < k1) stage(whole, std::true_type{});
 #pragma unroll
     for (int t = 0; t < MI; ++t)
 #pragma unroll
@@ -830,11 +836,12 @@ namespace {
 //   Up to 64 rows the same where there is little to split (64 x 4096 x 1024 6.6
 //   against the wide kernel's 7.2; 64 x 4096 x 4096 18.2 against 13.5).
 //   Beyond: the wide kernel, in the largest tiles that make a workgroup for every
-//   CU (and are not mostly past N): 2048 x 4096 x 1024 in tiles of 128 x 256 28.1, 64 x 128 30.5, 64 x 64 38;
-//   1024 x 4096 x 1024 26 / 17.5 / 21.  With fewer tiles of 64 x 64 than that, long
-//   sums are split until there are 512 workgroups (128 x 4096 x 4096 unsplit 24,
-//   in four 17.4; 512 x 1024 x 4096 20 / 17.3); short ones take tiles of 32 x 64
-//   (128 x 4096 x 1024 8.9 / 7.3, split in two 10.0).
+//   CU (and are not mostly past N): 2048 x 4096 x 1024 in tiles of 128 x 256 28.1,
+//   64 x 128 30.5, 64 x 64 38; 1024 x 4096 x 1024 26 / 17.5 / 21.  With fewer tiles
+//   of 64 x 64 than that, long sums are split until there are 512 workgroups (128 x
+//   4096 x 4096 unsplit 24, in four 17.4; 512 x 1024 x 4096 20 / 17.3); short ones
+//   take tiles of 32 x 64 (128 x 4096 x 1024 8.9 / 7.3, split in two 10.0).  (All of
+//   the wide kernel's since 5-15% faster, its tail apart from its loop.)
 enum Kernel { kRows, kWide32x64, kWide64x64, kWide64x128, kWide128x256 };
 struct Plan {
     Kernel kernel;
