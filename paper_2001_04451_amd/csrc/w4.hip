@@ -154,10 +154,9 @@ __device__ __forceinline__ void put4(const W4Args& g, int64_t m, int n, f32x4 v)
 // tiles of 128 inputs in turn, the codes of AHEAD of them on their way, and add
 // up in LDS.  Where the rows are short (STAGED) they pass through LDS once, while
 // the first codes are on their way; else a wave loads them tile by tile.
-// HBM-bound where the matrix is large: one row by 16384 x 16384 int4 30 us (4.6
-// TB/s), e2m1 26 (5.5), by 32000 x 4096 17 and 16; by 4096 x 1024 3.4, of which the
-// launch is 2.5.  Rows loaded tile by tile took 40 and 35 at 16384 x 16384, with
-// a tile at a time on its way 32.
+// HBM-bound where the matrix is large: one row by 16384 x 16384 26 us (5.3 TB/s in
+// int4, 5.5 in e2m1), by 32000 x 4096 17 and 16; by 4096 x 1024 3.1, of which the
+// launch is 2.5.
 constexpr size_t kStaged = 34 * 1024;  // bytes of rows, at most
 __host__ __device__ constexpr int64_t staged_stride(int K) { return K + 32; }  // rows start 16 banks apart
 
@@ -829,8 +828,8 @@ namespace {
 //   outputs on 32 and from 1024 on 64: reading the rows once a workgroup is what
 //   bounds wider calls (L2 gives all CUs together 8.8 TB/s).  16 x 4096 x 4096 (16
 //   outputs / 32 / 64) 7.5 / 7.5 / 8.5, 16 x 8192 x 4096 11.5 / 8.1 / 8.8, 16 x
-//   16384 x 4096 19.8 / 13.0 / 9.9, 1 x 8192 x 4096 7.4 / 6.6 / 7.9, 1 x 32000 x
-//   4096 18.3 / 19.0 / 17.4.
+//   16384 x 4096 19.8 / 13.0 / 9.9, 1 x 8192 x 4096 6.9 / 6.6 / 7.9, 1 x 32000 x
+//   4096 22.0 / 19.1 / 17.4.
 //   Up to 32 rows the same (32 x 16384 x 4096 34 / 20 / 13.5), but with groups of
 //   32, whose scales leave no registers for 64 outputs (24 / 83 at 32 / 64).
 //   Up to 64 rows the same where there is little to split (64 x 4096 x 1024 6.6
@@ -858,14 +857,22 @@ Plan plan_of(const W4Shape& s, int64_t M) {
     return {kWide64x64, (int)std::max<int64_t>(splits, 1)};
 }
 
+// Whether the rows kernel stages its rows: long ones that fit, where a wave goes
+// round often enough (1 x 16384 x 16384 26 us; tile by tile, 16, 32 or 64 outputs a
+// workgroup, 36 / 28 / 30; 1 x 4096 x 16384 10.4 and 12.2, but 16 x 4096 x 1024 4.1
+// and 3.6, 4 x 4096 x 4096 6.0 and 5.5).
+bool stages_rows(const W4Shape& s, int64_t M) {
+    return s.tiles_k >= 96 && (size_t)M * staged_stride(s.K) * 2 <= kStaged;
+}
+
 template <bool E2M1, bool ZEROS, int PT, int MT, int NT>
 void launch_rows(const W4Args& g, hipStream_t stream) {
     const int waves = g.s.tiles_k >= 8 ? 8 : 4;
     const dim3 grid((unsigned)((g.s.tiles_n + NT - 1) / NT), (unsigned)((g.c.M + 16 * MT - 1) / (16 * MT)));
     const size_t sums = (size_t)waves * NT * MT * 1024;
     if constexpr (MT == 1 && NT == 1) {
-        const size_t rows = (size_t)g.c.M * staged_stride(g.s.K) * 2;
-        if (rows <= kStaged) {
+        if (stages_rows(g.s, g.c.M)) {
+            const size_t rows = (size_t)g.c.M * staged_stride(g.s.K) * 2;
             w4_rows_kernel<E2M1, ZEROS, PT, MT, NT, true><<<grid, 64 * waves, std::max(rows, sums), stream>>>(g);
             return;
         }
@@ -910,9 +917,9 @@ hipError_t launch_linear_w4(const W4Shape& s, const W4Call& c, void* workspace, 
             case kRows: break;
         }
         if (c.M <= 16) {
-            if (s.tiles_n >= 1024)
+            if (s.tiles_n >= 1024 && !stages_rows(s, c.M))
                 launch_rows<E2M1, ZEROS, PT, 1, 4>(g, stream);
-            else if (s.tiles_n >= 512)
+            else if (s.tiles_n >= 512 && !stages_rows(s, c.M))
                 launch_rows<E2M1, ZEROS, PT, 1, 2>(g, stream);
             else
                 launch_rows<E2M1, ZEROS, PT, 1, 1>(g, stream);

@@ -132,7 +132,7 @@ class Exact:
 # many rows; wide and long
 SIZES = [(1, 1, 32), (1, 16, 128), (2, 17, 96), (15, 33, 160), (16, 50, 1024), (17, 64, 288), (31, 48, 544), (33, 16, 2080),
          (48, 100, 256), (64, 31, 640), (65, 130, 384), (100, 257, 192), (128, 128, 512), (129, 129, 1056), (200, 96, 128),
-         (257, 320, 448), (513, 65, 96), (700, 512, 1024), (1, 2047, 4128), (3, 16, 16384), (8, 4100, 64),
+         (257, 320, 448), (513, 65, 96), (700, 512, 1024), (1, 2047, 4128), (3, 16, 16384), (8, 4100, 64), (1, 8200, 16384), (1, 40, 12320),
          # wide calls of few rows (32 and 64 outputs a workgroup), sums split over workgroups, and the large tiles, each
          # with rows and outputs that end inside one
          (1, 8200, 160), (5, 16400, 96), (16, 16399, 64), (20, 8194, 96), (32, 16400, 288), (40, 4100, 64), (70, 200, 2112),
