@@ -23,7 +23,7 @@
  *   scale, gains and biases   [D] fp32
  *   dy, dz, dx, df, dgate     [T][D] fp32;  gradients of scale, gains and
  *                  biases    [D] fp32
- * Every pointer is 16-byte aligned.  Statistics and sums are fp32 (rows with
+ * T and D are 1 or more, every pointer is 16-byte aligned (LSH_ERR_INVALID otherwise).  Statistics and sums are fp32 (rows with
  * 2^-60 < |t| < 2^60 for their largest deviation are exact to fp32 rounding).
  * Supported: D a multiple of 8 up to 8192, T < 2^31, strides up to 2^31
  * (LSH_ERR_UNSUPPORTED otherwise).

@@ -39,7 +39,8 @@
  *            (packed) or >= K, a multiple of 8
  *   bias     [N] fp32 or NULL
  *   resid    [M][N] fp32 or NULL, out_f32 [M][N] fp32, out_bf16 [M][N] bf16
- * Every pointer is 16-byte aligned, packed 256.  Supported: K a multiple of
+ * Every pointer is 16-byte aligned, packed 256.  M, N and K are 1 or more (LSH_ERR_INVALID
+ * otherwise).  Supported: K a multiple of
  * 32 up to 2^17, N up to 2^22, N K < 2^35, M N < 2^31, M <= 2^21, a_stride <= 2^31
  * (LSH_ERR_UNSUPPORTED otherwise).
  */
@@ -80,12 +81,13 @@ int lsh_w4_unpack(const lsh_w4_config *cfg, lsh_dtype dtype, const void *packed,
 /* out_f32 = resid + sign * (a W^T + bias) when out_f32 is given, else
  * out_bf16 = bf16(a W^T + bias), with `relu` bf16(relu(a W^T + bias)); exactly
  * one of the two.  sign, resid and relu go with their output (relu with
- * out_f32 and resid with out_bf16 are LSH_ERR_INVALID).
+ * out_f32, resid or a sign other than 1 with out_bf16 are LSH_ERR_INVALID).
  * Codes enter the products as they are (exact in bf16) and sums are fp32; the
  * INT4 scales and zero points are applied to a group's sum, scale (sum a c -
- * zero sum a), so a row of `a` with an infinity gives NaN where W^T alone would
- * give an infinity.  Every row's result is formed in an order that depends on
- * the call's sizes alone: calls repeat bit for bit.
+ * zero sum a), so a row of `a` with an infinity, or with values that pass fp32's
+ * range in these sums, gives NaN where W^T alone would give an infinity or less.
+ * Every row's result is formed in an order that depends on the call's sizes and
+ * row stride alone: calls repeat bit for bit.
  *   workspace >= lsh_w4_workspace_bytes(cfg, M); its contents are free, and
  *   calls that may overlap need one each */
 int lsh_linear_w4(const lsh_w4_config *cfg, int64_t M, const void *a, int64_t a_stride, const void *packed,

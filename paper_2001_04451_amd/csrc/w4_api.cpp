@@ -89,14 +89,14 @@ int lsh_linear_w4(const lsh_w4_config* cfg, int64_t M, const void* a, int64_t a_
     if (a_stride != 0 && (a_stride < s.K || a_stride % 8 != 0)) return LSH_ERR_INVALID;
     if (a_stride > (int64_t)1 << 31) return LSH_ERR_UNSUPPORTED;
     if (!a || !packed || !aligned(a, 16) || !aligned(packed, 256)) return LSH_ERR_INVALID;
-    if (!out_f32 == !out_bf16 || (out_f32 && relu) || (out_bf16 && resid)) return LSH_ERR_INVALID;
+    if (!out_f32 == !out_bf16 || (out_f32 && relu) || (out_bf16 && (resid || sign != 1.f))) return LSH_ERR_INVALID;
     if (!std::isfinite(sign)) return LSH_ERR_INVALID;
     if (!aligned(bias, 16) || !aligned(resid, 16) || !aligned(out_f32, 16) || !aligned(out_bf16, 16))
         return LSH_ERR_INVALID;
     const size_t need = lsh::w4_workspace_bytes(s, M);
     if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return LSH_ERR_INVALID;
     const lsh::W4Call c{M,     a_stride ? a_stride : s.K, static_cast<const uint16_t*>(a), static_cast<const char*>(packed),
-                        bias,  resid,                     out_f32 ? sign : 1.f,            relu != 0,
+                        bias,  resid,                     sign,                            relu != 0,
                         out_f32, static_cast<uint16_t*>(out_bf16)};
     return status_of(lsh::launch_linear_w4(s, c, workspace, static_cast<hipStream_t>(stream)));
 }

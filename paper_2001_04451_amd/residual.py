@@ -71,6 +71,8 @@ class ResidualConfig:
     gate_stride: int = 0
 
     def c(self) -> ResidualConfigC:
+        if not 0 <= self.D < 1 << 31:  # a c_int32 would take it modulo 2^32
+            raise ValueError(f"D = {self.D} is out of range")
         return ResidualConfigC(self.T, self.f_stride, self.gate_stride, self.D, NORMS[self.norm], int(bool(self.post)),
                                int(bool(self.pre)), GATES[self.gate], self.alpha, self.eps)
 
@@ -93,10 +95,7 @@ class ResidualWeights:
     pre_b: torch.Tensor | None = None
 
     def check(self, cfg: ResidualConfig, device) -> None:
-        checked = self.__dict__.get("_checked")
-        if checked is not None and checked[0] is cfg and checked[1] == device:
-            return
-        for name in WEIGHTS:
+        for name in WEIGHTS:  # at every call: a parameter's storage may be exchanged for one of another type
             t = getattr(self, name)
             if t is None:
                 continue
@@ -108,7 +107,6 @@ class ResidualWeights:
                 raise ValueError(f"{name}_g is required with {name}")
             if not on and (getattr(self, name + "_g") is not None or getattr(self, name + "_b") is not None):
                 raise ValueError(f"{name}_g and {name}_b go with {name}")
-        object.__setattr__(self, "_checked", (cfg, device))
 
     def ref(self):
         p = lsh._ptr

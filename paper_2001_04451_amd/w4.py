@@ -56,6 +56,9 @@ class W4Config:
     zeros: bool = False
 
     def c(self) -> W4ConfigC:
+        for name, n in (("N", self.N), ("K", self.K), ("group", self.group)):
+            if not 0 <= n < 1 << 31:  # a c_int32 would take it modulo 2^32
+                raise ValueError(f"{name} = {n} is out of range")
         return W4ConfigC(self.N, self.K, TYPES[self.type], self.group, int(bool(self.zeros)))
 
     def ref(self):
@@ -186,6 +189,10 @@ def lsh_linear_w4(cfg: W4Config, a, packed, bias=None, resid=None, sign: float =
                   dtype: torch.dtype = torch.float32, out=None, workspace=None) -> torch.Tensor:
     """resid + sign (a W^T + bias) in fp32, or with dtype bfloat16 bf16(a W^T + bias), relu before the rounding
     with ``relu`` (lsh_linear_w4).  a [M, K] bf16, its rows at any stride that is a multiple of 8."""
+    if packed is None:
+        raise ValueError("packed is required")
+    if sign != 1.0 and dtype == torch.bfloat16:
+        raise ValueError("sign goes with float32")
     stride = _row_stride(a, cfg.K)
     dev, shape = a.device, (a.shape[0], cfg.N)
     packed = _packed(cfg, packed, dev)

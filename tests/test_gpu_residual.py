@@ -276,3 +276,14 @@ def test_as_the_blocks_layer_norm(gpu):
     _, z = residual.lsh_residual_norm_fwd(own, x, None, None, residual.ResidualWeights(pre_g=gain, pre_b=bias))
     # both round the same number to bf16, within fp32's error of each other: a step apart at most
     assert ((out - z.float().clamp(min=0)).abs() <= 2.0 ** -7 * z.float().abs() + 1e-6).all()
+
+
+def test_exchanged_weights_refused(gpu):
+    """A weight whose storage becomes bf16 after a first call (as a module's conversion does) is not read as fp32."""
+    cfg = residual.ResidualConfig(T=3, D=64, pre=False)
+    x, f = torch.ones(3, 64, device=gpu), torch.ones(3, 64, device=gpu, dtype=BF)
+    weights = residual.ResidualWeights(post_g=torch.nn.Parameter(torch.ones(64, device=gpu), requires_grad=False))
+    residual.lsh_residual_norm_fwd(cfg, x, f, None, weights)
+    weights.post_g.data = weights.post_g.data.to(BF)
+    with pytest.raises(ValueError, match="dtype"):
+        residual.lsh_residual_norm_fwd(cfg, x, f, None, weights)

@@ -92,7 +92,7 @@ def test_w4_arguments_refused(built):
     assert linear(stride=248) == linear(stride=260) == linear(stride=-8) == INVALID
     assert linear(stride=1 << 32) == UNSUPPORTED
     assert linear(f32=None) == linear(b16=FAKE) == linear(f32=ODD) == linear(f32=None, b16=ODD) == INVALID
-    assert linear(relu=1) == linear(f32=None, b16=FAKE, resid=FAKE) == INVALID
+    assert linear(relu=1) == linear(f32=None, b16=FAKE, resid=FAKE) == linear(f32=None, b16=FAKE, sign=-1.0) == INVALID
     assert linear(bias=ODD) == linear(resid=ODD) == INVALID
     assert linear(sign=float("nan")) == linear(sign=float("inf")) == INVALID
     for M in (4, 100, 2048):
@@ -101,6 +101,22 @@ def test_w4_arguments_refused(built):
             assert linear(M=M, ws=None) == linear(M=M, ws=ODD) == linear(M=M, n=need - 1) == INVALID
     wide = ctypes.byref(_w4(N=1 << 20).c())
     assert L.lsh_linear_w4(wide, 1 << 11, FAKE, 0, FAKE, None, None, 1.0, 0, FAKE, None, FAKE, BIG, None) == UNSUPPORTED
+
+
+def test_sizes_past_32_bits_refused(built):
+    """The C structures hold 32 bits: 2^32 + 64 would pass as 64."""
+    for bad in (dict(N=(1 << 32) + 64), dict(K=(1 << 32) + 64), dict(group=(1 << 32) + 32), dict(N=-1)):
+        with pytest.raises(ValueError, match="out of range"):
+            w4.weight_bytes(_w4(**bad))
+    with pytest.raises(ValueError, match="out of range"):
+        residual.workspace_bytes(_res(D=(1 << 32) + 64))
+
+
+def test_linear_without_weights_refused(built):
+    with pytest.raises(ValueError, match="packed"):
+        w4.lsh_linear_w4(_w4(), torch.zeros(1, 256, dtype=torch.bfloat16), None)
+    with pytest.raises(ValueError, match="sign"):
+        w4.lsh_linear_w4(_w4(), torch.zeros(1, 256, dtype=torch.bfloat16), torch.zeros(8), sign=-1.0, dtype=torch.bfloat16)
 
 
 def test_w4_sizes(built):
