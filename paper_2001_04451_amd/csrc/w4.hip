@@ -149,6 +149,30 @@ __device__ __forceinline__ void put4(const W4Args& g, int64_t m, int n, f32x4 v)
     }
 }
 
+// Outputs n + 4 q .. + 3 and 16 further of row m to bf16, N a multiple of 8: the four
+// lanes of a row trade them for n + 8 q .. + 7, so that the row's 64 bytes leave in
+// one store.
+__device__ __forceinline__ void put_pair(const W4Args& g, int64_t m, int n, int q, f32x4 a, f32x4 b) {
+    const int N = g.s.N;
+    if (g.c.bias) {
+        if (n + 4 * q < N) a += *reinterpret_cast<const f32x4*>(g.c.bias + n + 4 * q);
+        if (n + 16 + 4 * q < N) b += *reinterpret_cast<const f32x4*>(g.c.bias + n + 16 + 4 * q);
+    }
+    if (g.c.relu)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = a[e] < 0.f ? 0.f : a[e], b[e] = b[e] < 0.f ? 0.f : b[e];
+    u32x4 out;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const auto half = __builtin_amdgcn_permlane32_swap(pack_bf16x2(a[2 * e], a[2 * e + 1]),
+                                                           pack_bf16x2(b[2 * e], b[2 * e + 1]), false, false);
+        const auto row = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
+        out[e] = row[0];
+        out[2 + e] = row[1];
+    }
+    if (m < g.c.M && n + 8 * q < N) *reinterpret_cast<u32x4*>(g.c.out_bf16 + m * N + n + 8 * q) = out;
+}
+
 // ---------------------------------------------------------------------------
 // Few rows.  A workgroup takes 16 NT outputs of 16 MT rows; its waves take the
 // tiles of 128 inputs in turn, the codes of AHEAD of them on their way, and add
@@ -541,6 +565,14 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_wide_kernel(W4Args g, int spli
     const int whole = min(k1, g.s.K / 128);
     for (int k = k0; k < whole; ++k) stage(k, std::false_type{});
     if (whole < k1) stage(whole, std::true_type{});
+    if (splits == 1 && g.c.out_bf16 && (g.s.N & 7) == 0) {
+#pragma unroll
+        for (int t = 0; t < MI; ++t)
+#pragma unroll
+            for (int i = 0; i < NI; i += 2)
+                put_pair(g, m0 + row + 16 * t, n0 + 16 * (wn * NI + i), q, acc[i][t], acc[i + 1][t]);
+        return;
+    }
 #pragma unroll
     for (int t = 0; t < MI; ++t)
 #pragma unroll
