@@ -95,7 +95,18 @@ class ResidualWeights:
     pre_b: torch.Tensor | None = None
 
     def check(self, cfg: ResidualConfig, device) -> None:
-        for name in WEIGHTS:  # at every call: a parameter's storage may be exchanged for one of another type
+        shape, f32 = (cfg.D,), torch.float32
+        for t in (self.scale, self.post_g, self.post_b, self.pre_g, self.pre_b):
+            # at every call: a parameter's storage may be exchanged for one of another type
+            if t is not None and (t.dtype is not f32 or t.device != device or t.shape != shape or not t.is_contiguous()):
+                self._refuse(cfg, device)
+        if (self.post_g is not None) != bool(cfg.post) or (self.pre_g is not None) != bool(cfg.pre) or \
+                (self.post_b is not None and not cfg.post) or (self.pre_b is not None and not cfg.pre):
+            self._refuse(cfg, device)
+
+    def _refuse(self, cfg: ResidualConfig, device) -> None:
+        """Raises what check() has found, by name."""
+        for name in WEIGHTS:
             t = getattr(self, name)
             if t is None:
                 continue
