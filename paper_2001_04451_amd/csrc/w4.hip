@@ -331,8 +331,8 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
 // 128 inputs, copied there by buffer loads that the kernel counts by hand; codes
 // are widened in the registers of the waves that use them.  A call with few tiles
 // splits its inputs over workgroups, whose sums a second kernel joins in order.
-// 2048 x 4096 x 4096: int4 72 us (0.95 PFLOP/s), e2m1 57 (1.20; a bf16 product of
-// 8192^3 by the library reaches 1.39); 2048 x 4096 x 1024 25 and 21.  Bound by the
+// 2048 x 4096 x 4096: int4 71 us (0.97 PFLOP/s), e2m1 56 (1.22; a bf16 product of
+// 8192^3 by the library reaches 1.39); 2048 x 4096 x 1024 25 and 20.  Bound by the
 // copies (8.8 TB/s out of L2, a workgroup a CU) with the first stages' and the
 // epilogue's latency; int4 issues a quarter more products for the sums of rows.
 constexpr int kMostSplits = 8;
@@ -873,6 +873,10 @@ namespace {
 //   4096 x 4096 unsplit 24, in four 17.4; 512 x 1024 x 4096 20 / 17.3); short ones
 //   take tiles of 32 x 64 (128 x 4096 x 1024 8.9 / 7.3, split in two 10.0).  (All of
 //   the wide kernel's since 5-15% faster, its tail apart from its loop.)
+//   From 8192 inputs on the largest tiles are split into up to four where that makes
+//   192 to 256 workgroups of them: 512 x 8192 x 8192 101 -> 86 (e2m1 68 -> 65), 1000 x
+//   2048 x 8192 61 -> 47 (44 -> 40), 800 x 2048 x 16384 109 -> 76 (80 -> 61); with 288
+//   workgroups 300 x 8192 x 8192 88 -> 97, with 4096 inputs 512 x 4096 32 -> 34.
 enum Kernel { kRows, kWide32x64, kWide64x64, kWide64x128, kWide128x256 };
 struct Plan {
     Kernel kernel;
@@ -882,6 +886,8 @@ Plan plan_of(const W4Shape& s, int64_t M) {
     if (M <= 32 || (M <= 64 && s.tiles_k <= 8 && s.tiles_n <= 256)) return {kRows, 1};
     auto tiles = [&](int tm, int tn) { return ((M + tm - 1) / tm) * ((s.N + tn - 1) / tn); };
     if (tiles(128, 256) >= 256 && s.N > 128) return {kWide128x256, 1};
+    const int64_t large = tiles(128, 256), part = std::min<int64_t>(256 / large, 4);
+    if (s.N > 128 && large * part >= 192 && s.tiles_k >= std::max<int64_t>(64, 16 * part)) return {kWide128x256, (int)part};
     if (tiles(64, 128) >= 256 && s.N > 64) return {kWide64x128, 1};
     const int64_t t = tiles(64, 64);
     if (s.tiles_k <= 8) return {t >= 256 ? kWide64x64 : kWide32x64, 1};

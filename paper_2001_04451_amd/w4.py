@@ -91,7 +91,9 @@ def workspace_bytes(cfg: W4Config, M: int) -> int:
 
 def workspace(cfg: W4Config, M: int, device) -> torch.Tensor:
     """A workspace for lsh_linear_w4 of up to M rows; calls that may overlap need one each."""
-    return torch.empty(max(workspace_bytes(cfg, M), 256), dtype=torch.uint8, device=device)
+    # Fewer rows may need more, being split.  Tiles have a multiple of 64 rows, between which the need grows.
+    n = max([workspace_bytes(cfg, M)] + [workspace_bytes(cfg, m) for m in range(64, M, 64)])
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
 def _packed(cfg: W4Config, packed, device) -> torch.Tensor:

@@ -173,6 +173,38 @@ def test_linear_outputs(gpu, kind, M):
     assert (buf[:64] == 7).all() and (buf[64 + M * 77:] == 7).all() and (out == 7).all()
 
 
+@pytest.mark.parametrize("kind", [TYPES[1], TYPES[4], TYPES[6]], ids=[IDS[1], IDS[4], IDS[6]])
+def test_linear_exact_split_large_tiles(gpu, kind):
+    """The largest tiles with their inputs split: rows, outputs and inputs that end inside one."""
+    log("w4 split large", kind)
+    c = Exact(257, 4000, 8224, kind, seed=5)
+    a, packed = c.args(gpu)
+    y = c.ref()
+    bias = torch.from_numpy(c.bias).to(gpu)
+    same(w4.lsh_linear_w4(c.cfg, a, packed, bias), y)
+    same(w4.lsh_linear_w4(c.cfg, a, packed, bias, dtype=torch.bfloat16),
+         torch.from_numpy(y.astype(np.float32)).bfloat16().double().numpy())
+
+
+@pytest.mark.parametrize("size", [(66, 8, 256), (130, 72, 224), (130, 200, 1184), (513, 2056, 96), (1030, 2104, 288), (2100, 4024, 160)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("kind", [TYPES[1], TYPES[4], TYPES[6]], ids=[IDS[1], IDS[4], IDS[6]])
+def test_linear_bf16_rows(gpu, kind, size):
+    """bf16 results of a number of outputs that is a multiple of 8, in every size of tiles, with bias and relu, and what
+    lies behind them."""
+    log("w4 bf16 rows", kind, size)
+    M, N, K = size
+    c = Exact(M, N, K, kind, seed=N)
+    a, packed = c.args(gpu)
+    y = torch.from_numpy(c.ref().astype(np.float32)).bfloat16().double().numpy()
+    bias = torch.from_numpy(c.bias).to(gpu)
+    buf = torch.full((M * N + 128,), 7.0, dtype=torch.bfloat16, device=gpu)
+    out = buf[64:64 + M * N].view(M, N)
+    same(w4.lsh_linear_w4(c.cfg, a, packed, bias, dtype=torch.bfloat16, out=out), y)
+    same(w4.lsh_linear_w4(c.cfg, a, packed, bias, relu=True, dtype=torch.bfloat16, out=out), np.maximum(y, 0))
+    assert (buf[:64] == 7).all() and (buf[64 + M * N:] == 7).all()
+
+
 @pytest.mark.parametrize("M", [1, 16, 61, 130, 400])
 @pytest.mark.parametrize("kind", TYPES, ids=IDS)
 def test_linear_real(gpu, kind, M):

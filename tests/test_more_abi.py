@@ -119,6 +119,12 @@ def test_linear_without_weights_refused(built):
         w4.lsh_linear_w4(_w4(), torch.zeros(1, 256, dtype=torch.bfloat16), torch.zeros(8), sign=-1.0, dtype=torch.bfloat16)
 
 
+@pytest.mark.parametrize("N,K,M", [(4096, 4096, 700), (1000, 8224, 2100), (8192, 8192, 2049), (16, 32, 300)])
+def test_w4_workspace_of_up_to(built, N, K, M):
+    cfg = _w4(N=N, K=K)
+    assert w4.workspace(cfg, M, "cpu").numel() >= max(w4.workspace_bytes(cfg, m) for m in range(1, M + 1))
+
+
 def test_w4_sizes(built):
     """A quarter of bf16's bytes, the scales' and the tiles' rest."""
     assert w4.weight_bytes(_w4(N=4096, K=1024)) == 4096 * 1024 // 2 + 4096 * 8 * 2
