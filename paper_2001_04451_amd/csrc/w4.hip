@@ -876,7 +876,9 @@ namespace {
 //   From 8192 inputs on the largest tiles are split into up to four where that makes
 //   192 to 256 workgroups of them: 512 x 8192 x 8192 101 -> 86 (e2m1 68 -> 65), 1000 x
 //   2048 x 8192 61 -> 47 (44 -> 40), 800 x 2048 x 16384 109 -> 76 (80 -> 61); with 288
-//   workgroups 300 x 8192 x 8192 88 -> 97, with 4096 inputs 512 x 4096 32 -> 34.
+//   workgroups 300 x 8192 x 8192 88 -> 97, with 4096 inputs 512 x 4096 32 -> 34, half
+//   empty 64 x 16384 x 8192 37 -> 44; unsplit 1500 x 4096 x 8192 140 -> 130, but in
+//   groups of 32 with zero points 210 -> 237.
 enum Kernel { kRows, kWide32x64, kWide64x64, kWide64x128, kWide128x256 };
 struct Plan {
     Kernel kernel;
@@ -887,7 +889,9 @@ Plan plan_of(const W4Shape& s, int64_t M) {
     auto tiles = [&](int tm, int tn) { return ((M + tm - 1) / tm) * ((s.N + tn - 1) / tn); };
     if (tiles(128, 256) >= 256 && s.N > 128) return {kWide128x256, 1};
     const int64_t large = tiles(128, 256), part = std::min<int64_t>(256 / large, 4);
-    if (s.N > 128 && large * part >= 192 && s.tiles_k >= std::max<int64_t>(64, 16 * part)) return {kWide128x256, (int)part};
+    if (M > 64 && s.N > 128 && large * part >= 192 && s.tiles_k >= std::max<int64_t>(64, 16 * part) &&
+        (part > 1 || s.e2m1 || s.group > 32))
+        return {kWide128x256, (int)part};
     if (tiles(64, 128) >= 256 && s.N > 64) return {kWide64x128, 1};
     const int64_t t = tiles(64, 64);
     if (s.tiles_k <= 8) return {t >= 256 ? kWide64x64 : kWide32x64, 1};
