@@ -28,6 +28,33 @@ struct W4Shape {
     size_t bytes() const { return codes_size() + scales_size() + zeros_size(); }
 };
 
+// What lane `lane` of a wave reads of `a` to fill its LDS copies with, in bytes from
+// the first row of the workgroup's tile (TM rows) on, 256 k for tile k of 128 inputs
+// on top: the wave's copies are runs `run` + j of eight rows of one half (64 inputs),
+// 16 bytes a lane.  `after` rows follow the tile's first.  Rows past the last
+// one repeat it, and pieces past the end of a row its first piece of the tile (neither
+// is used), so that every byte read is a byte of the matrix and nothing rests on how a
+// buffer's bound counts a scalar offset (1% of a long call's time in place of offsets
+// in scalar registers: 2048 x 4096 x 1024 25.5 -> 25.7 us).
+template <int TM, int COPIES>
+struct W4RowCopies {
+    uint32_t at[COPIES], col;
+    __host__ __device__ W4RowCopies(int lane, int run, int64_t after, uint32_t row_bytes) {
+        // lane l fills slot l % 8 of row l / 8; piece p of row r is in slot p ^ (r & 7)
+        col = 128u * (run / (TM / 8)) + 16u * ((lane & 7) ^ (lane >> 3));
+        const int last = after < TM ? (int)after : TM - 1;
+        for (int j = 0; j < COPIES; ++j) {
+            const int row = 8 * (run % (TM / 8) + j) + (lane >> 3);
+            at[j] = (uint32_t)(row < last ? row : last) * row_bytes + col;
+        }
+    }
+    // Before the last tile, where it has `rest` bytes of each row's inputs (of 256).
+    __host__ __device__ void shorten(uint32_t rest) {
+        if (col < rest) return;
+        for (int j = 0; j < COPIES; ++j) at[j] -= col;
+    }
+};
+
 struct W4Call {
     int64_t M, a_stride;
     const uint16_t* a;

@@ -383,14 +383,9 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_wide_kernel(W4Args g, int spli
     const int n0 = tn * S::TN;
     const uint16_t* const base = g.c.a + m0 * g.c.a_stride;
     const u32x4 buf = buffer_of(base, ((uint64_t)(g.c.M - 1 - m0) * g.c.a_stride + g.s.K) * 2);
-    // Copies: lane l fills slot l % 8 of row l / 8 of eight rows; piece p of row r is
-    // in slot p ^ (r & 7) (operand reads meet all banks).  A wave's copies are runs
-    // of eight rows of one half; rows past M lie past the buffer's end.
     static_assert(S::TM / 8 % S::kCopies == 0, "a wave's runs lie in one half");
-    const int run = wave * S::kCopies, first = 8 * (run % (S::TM / 8));
-    const uint32_t row_bytes = (uint32_t)g.c.a_stride * 2;
-    const uint32_t off = (lane >> 3) * row_bytes + 16u * ((lane & 7) ^ (lane >> 3));
-    const uint32_t first_off = first * row_bytes + 128u * (run / (S::TM / 8));
+    const int run = wave * S::kCopies;
+    W4RowCopies<S::TM, S::kCopies> from(lane, run, g.c.M - 1 - m0, (uint32_t)g.c.a_stride * 2);
     const uint32_t lds0 = lds_addr(smem);
     const int64_t tile0 = n0 / 16;
     // Scales, 32 PT bytes a tile (E2M1 64), and zero points, 16 PT: a copy each of
@@ -413,9 +408,10 @@ __global__ __launch_bounds__(128 * WN, 2) void w4_wide_kernel(W4Args g, int spli
                                 (uint64_t)tiles_k * 1024);
     auto copy = [&](int k, int slot) {
         const uint32_t to = lds0 + slot * S::kStage;
+        if (128 * k + 128 > g.s.K) from.shorten((uint32_t)(g.s.K - 128 * k) * 2);  // the last tile, once
 #pragma unroll
         for (int j = 0; j < S::kCopies; ++j)
-            buffer_to_lds(buf, off, first_off + 8 * j * row_bytes + (uint32_t)k * 256u, to + (run + j) * 1024);
+            buffer_to_lds(buf, from.at[j], (uint32_t)k * 256u, to + (run + j) * 1024);
 #pragma unroll
         for (int j = 0; j < S::kCodes; ++j)
             buffer_to_lds(code_buf[j], 16 * lane, (uint32_t)k * 1024u, to + S::kRowBytes + (wave * S::kCodes + j) * 1024);
