@@ -210,15 +210,14 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
         if (wave + u * waves < whole) load(blocks[u], wave + u * waves);
-    // Rows past M are not loaded: what their lanes hold meets their own results alone.
+    // Rows past M repeat the last one: their lanes' values meet their own results alone,
+    // which are not stored.
     const uint16_t* x[MT];
-    bool there[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int64_t m = m0 + 16 * t + (lane & 15);
-        there[t] = m < g.c.M;
+        const int64_t m = min(m0 + 16 * t + (lane & 15), g.c.M - 1);
         if constexpr (STAGED)
-            x[t] = reinterpret_cast<const uint16_t*>(smem) + (16 * t + (lane & 15)) * staged_stride(K) + 8 * q;
+            x[t] = reinterpret_cast<const uint16_t*>(smem) + (m - m0) * staged_stride(K) + 8 * q;
         else
             x[t] = g.c.a + m * g.c.a_stride + 8 * q;
     }
@@ -242,14 +241,11 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
         bf16x8 xv[4][MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            if (there[t])
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!decltype(last)::value || 128 * k + 32 * i < K)
-                        xv[i][t] = *reinterpret_cast<const bf16x8*>(x[t] + 128 * k + 32 * i);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (decltype(last)::value && 128 * k + 32 * i >= K) xv[i][t] = all_of(0);
+                xv[i][t] = !decltype(last)::value || 128 * k + 32 * i < K
+                               ? *reinterpret_cast<const bf16x8*>(x[t] + 128 * k + 32 * i)
+                               : all_of(0);
         }
         if constexpr (E2M1) {
 #pragma unroll
