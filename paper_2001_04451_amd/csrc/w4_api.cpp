@@ -32,7 +32,7 @@ int check_w4(const lsh_w4_config* c, lsh::W4Shape* s) {
 
 int check_rows(const lsh::W4Shape& s, int64_t M) {
     if (M < 1) return LSH_ERR_INVALID;
-    return M > 1 << 21 || M >= ((int64_t)1 << 31) / s.N ? LSH_ERR_UNSUPPORTED : LSH_OK;
+    return M > 1 << 21 || M * s.N >= (int64_t)1 << 31 ? LSH_ERR_UNSUPPORTED : LSH_OK;
 }
 
 int check_dtype(int dtype) { return dtype == LSH_F32 || dtype == LSH_BF16 ? LSH_OK : LSH_ERR_INVALID; }

@@ -103,6 +103,15 @@ def test_w4_arguments_refused(built):
     assert L.lsh_linear_w4(wide, 1 << 11, FAKE, 0, FAKE, None, None, 1.0, 0, FAKE, None, FAKE, BIG, None) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("N", [1025, 1537, 50257, (1 << 22) - 15])
+def test_w4_rows_up_to_their_limit_taken(built, N):
+    """M N < 2^31, where N does not divide 2^31 too: the last M is turned away for the missing rows alone."""
+    most = ((1 << 31) - 1) // N
+    r = ctypes.byref(_w4(N=N, K=32).c())
+    status = lambda M: w4.lib().lsh_linear_w4(r, M, None, 0, FAKE, None, None, 1.0, 0, FAKE, None, FAKE, BIG, None)
+    assert most <= 1 << 21 and status(most) == INVALID and status(most + 1) == UNSUPPORTED
+
+
 def test_sizes_past_32_bits_refused(built):
     """The C structures hold 32 bits: 2^32 + 64 would pass as 64."""
     for bad in (dict(N=(1 << 32) + 64), dict(K=(1 << 32) + 64), dict(group=(1 << 32) + 32), dict(N=-1)):
