@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkArgs a, const void* __
                                                         float* __restrict__ dx, float* __restrict__ partial,
                                                         int gain_rows) {
     __shared__ Angles both[2];  // of the batch at hand and of the next
-    __shared__ float sums[kGroups][kHeadDim];
+    __shared__ __attribute__((aligned(16))) float sums[kGroups][kHeadDim];
     const int l = threadIdx.x & 7, group = threadIdx.x >> 3, H = a.Hq + a.Hk;
     const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
     float* mine = partial + (int64_t)blockIdx.x * gain_rows * kHeadDim;

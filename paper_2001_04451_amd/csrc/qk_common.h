@@ -10,8 +10,8 @@ constexpr int kMaxTokens = 16;  // whose angles a workgroup holds at a time
 
 // Of a workgroup's tokens: the angles of their pairs, and where their rows go.
 struct Angles {
-    float c[kMaxTokens][32];
-    float s[kMaxTokens][32];
+    alignas(16) float c[kMaxTokens][32];  // read four at a time
+    alignas(16) float s[kMaxTokens][32];
     int b[kMaxTokens], l[kMaxTokens];  // batch entry and position in it (L > 0)
 };
 

@@ -199,7 +199,7 @@ __global__ __launch_bounds__(kThreads<WAVES>, PLAIN || WAVES == 16 ? 4 : 3) void
     const float* __restrict__ dy, const float* __restrict__ dz, ResidualGrads g, float* __restrict__ partial) {
     constexpr int ROWS = kRows<WAVES>;
     __shared__ float lds[2][ROWS][2][WAVES];
-    __shared__ float cols[ROWS > 1 ? ROWS : 1][ROWS > 1 ? 512 * WAVES : 1];
+    __shared__ __attribute__((aligned(16))) float cols[ROWS > 1 ? ROWS : 1][ROWS > 1 ? 512 * WAVES : 1];
     const Place<WAVES> p(a.D);
     RowSums<WAVES, ROWS> sums{lds, 0, p.row, p.wave};
     float sc[8], pg[8], pb[8], rg[8], col[5][8];
