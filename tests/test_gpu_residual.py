@@ -117,6 +117,25 @@ def test_many_rows(gpu, T):
     check(Case(T, 72, BF, "layer", gate="sigmoid", seed=T), gpu)
 
 
+@pytest.mark.parametrize("plain", [False, True])
+@pytest.mark.parametrize("norm,post", [("rms", True), ("layer", True), ("rms", False)])
+@pytest.mark.parametrize("T,D", [(9000, 264), (4500, 520), (2500, 1032), (1100, 2056), (600, 4104)])
+def test_many_wide_rows(gpu, T, D, norm, post, plain):
+    """Workgroups that walk over several rows, of one wave to sixteen: an even and an odd number of sums a row, with all
+    weights and (`plain`) with gains alone; the same bits again."""
+    log("residual wide rows", T, D, norm, post, plain)
+    c = Case(T, D, F32 if plain else BF, norm, post, True, "sigmoid", scale=not plain, bias=not plain, seed=D)
+    y, z, grads = check(c, gpu)
+    F, G, w = c.up(c.f, gpu), c.up(c.gate, gpu), c.weights(gpu)
+    y1, z1 = residual.lsh_residual_norm_fwd(c.cfg, c.up(c.x, gpu), F, G, w)
+    assert torch.equal(y, y1) and torch.equal(z, z1)
+    x, f, gate, w64, _, _ = c.wide64()
+    y32 = R.forward(c.c, x, f, gate, w64)[0]["y"].astype(np.float32)
+    again = residual.lsh_residual_norm_bwd(c.cfg, c.up(y32, gpu), F, G, w, c.up(c.dy, gpu), c.up(c.dz, gpu))
+    for n, t in grads.items():
+        assert (t is None and again[n] is None) or torch.equal(t, again[n]), n
+
+
 @pytest.mark.parametrize("norm", ["rms", "layer"])
 def test_offset_rows(gpu, norm):
     """Rows whose mean is far from zero: the deviation is taken from the mean, not from squares."""
