@@ -14,7 +14,10 @@
  *                 group (8 otherwise); groups of 32, 64 or 128
  *   LSH_W4_E2M1   codes of lsh_cache.h (values 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
  *                 their negatives), w = value 2^(scale - 127), a scale byte for
- *                 each group of 32; byte 255 stands for NaN
+ *                 each group of 32; byte 255 stands for NaN.  Values that fp32
+ *                 does not hold (4 and 6 with byte 253, 2 and more with 254) are
+ *                 infinite, so quantising takes magnitudes from 3.5 * 2^126 on to
+ *                 infinities
  * They are held in one buffer in the order in which the products read them
  * (`packed`, lsh_w4_weight_bytes, 256-byte aligned), laid out once:
  *   lsh_w4_quantize   from a matrix in fp32 or bf16.  The scale is the smallest
@@ -26,7 +29,9 @@
  *                     than 15.  All of it is decided exactly.  A group with a
  *                     value that is not finite becomes NaN as a whole.
  *   lsh_w4_pack       from codes, scales and zero points that the caller has
- *   lsh_w4_unpack     the matrix of values that `packed` stands for
+ *   lsh_w4_unpack     the matrix of values that `packed` stands for (infinite
+ *                     past fp32's range, as 7 scale can be for INT4 groups near
+ *                     its end)
  *
  * Conventions are those of lsh.h (device pointers, caller-owned memory and
  * workspace, asynchronous calls on `stream`, lsh_status results, INVALID and

@@ -151,6 +151,112 @@ def test_linear_exact(gpu, kind, size):
     same(out, c.ref(bias=False))
 
 
+@pytest.mark.parametrize("N,K", [(48, 4256), (8200, 2336), (16400, 2336)])
+@pytest.mark.parametrize("kind", TYPES, ids=IDS)
+def test_linear_exact_few_rows_several_turns(gpu, kind, N, K):
+    """The rows kernel with 16, 32 and 64 outputs a workgroup and eight waves that each take several tiles of inputs, the
+    last one ending inside: one and two tiles of rows, full and not."""
+    c = Exact(32, N, K, kind, seed=N)
+    a, packed = c.args(gpu)
+    y = c.ref(bias=False)
+    for M in (1, 16, 20, 32):
+        log("w4 turns", kind, M, N, K)
+        same(w4.lsh_linear_w4(c.cfg, a[:M].contiguous(), packed), y[:M])
+
+
+# tiles of rows, sums joined, and the largest tiles split, with outputs stored four at a time and one by one
+@pytest.mark.parametrize("M,N,K", [(1, 76, 224), (1, 77, 224), (40, 76, 224), (40, 77, 224), (300, 76, 224), (300, 77, 224),
+                                   (70, 200, 2112), (70, 201, 2112), (257, 4000, 8224), (257, 4001, 8224)])
+@pytest.mark.parametrize("kind", [TYPES[1], TYPES[4], TYPES[6]], ids=[IDS[1], IDS[4], IDS[6]])
+def test_linear_outputs_of_every_path(gpu, kind, M, N, K):
+    """Residual and its sign, in place too, relu, and what lies around the outputs."""
+    log("w4 outputs of every path", kind, M, N, K)
+    c = Exact(M, N, K, kind, seed=M)
+    a, packed = c.args(gpu)
+    assert (w4.workspace_bytes(c.cfg, M) > 0) == (K > 224)
+    up = lambda t: torch.from_numpy(t).to(gpu)
+    bias, resid, y = up(c.bias), up(c.resid), c.ref()
+    for dtype in (torch.float32, torch.bfloat16):
+        buf = torch.full((64 + M * N + 64,), 7.0, dtype=dtype, device=gpu)
+        out = buf[64:64 + M * N].view(M, N)
+        if dtype == torch.float32:
+            for sign in (1.0, -1.0, 0.5):
+                w4.lsh_linear_w4(c.cfg, a, packed, bias, resid, sign=sign, out=out)
+                same(out, c.resid + sign * y)
+            out.copy_(resid)
+            w4.lsh_linear_w4(c.cfg, a, packed, bias, out, sign=-1.0, out=out)
+            same(out, c.resid - y)
+        else:
+            half = torch.from_numpy(y.astype(np.float32)).bfloat16().double().numpy()
+            w4.lsh_linear_w4(c.cfg, a, packed, bias, relu=True, dtype=dtype, out=out)
+            same(out, np.maximum(half, 0))
+        assert (buf[:64] == 7).all() and (buf[64 + M * N:] == 7).all()
+
+
+def test_linear_e2m1_scales_at_both_ends(gpu):
+    """The smallest scales, whose values are subnormal in bf16, and the largest whose values fp32 holds."""
+    N, K = 48, 256
+    cfg = config(N, K, TYPES[6])
+    for low, power in ((0, 20), (246, -30)):
+        for M in (1, 70):
+            rng = np.random.default_rng(M)
+            codes = rng.integers(0, 16, (N, K)).astype(np.uint8)
+            scales = np.repeat(low + np.arange(N) % 7, K // 32).reshape(N, -1).astype(np.uint8)  # one of a row: exact sums
+            a = rng.integers(-3, 4, (M, K)) * 2.0 ** power
+            log("w4 ends", low, M)
+            out = w4.lsh_linear_w4(cfg, torch.from_numpy(a).to(gpu).bfloat16(), pack(cfg, codes, scales, None, gpu))
+            same(out, W.linear(a, codes, scales, None, "e2m1", 32)[0])
+
+
+def test_quantize_at_the_end_of_fp32(gpu):
+    """Magnitudes whose nearest value passes fp32's range come back infinite, the others as they should."""
+    w = torch.zeros(1, 32)
+    w[0, :4] = torch.tensor([3.4e38, -2.9e38, 3.5 * 2.0 ** 126, 1e38])
+    step = 2.0 ** 126
+    same(w4.lsh_w4_unpack(config(1, 32, TYPES[6]), w4.lsh_w4_quantize(config(1, 32, TYPES[6]), w.to(gpu)))[:, :4],
+         np.array([[np.inf, -3 * step, np.inf, step]]))
+    for kind in TYPES[:6]:
+        cfg = config(1, 32, kind)
+        with np.errstate(over="ignore"):
+            ref = W.values(*W.quantize(w.double().numpy(), kind[0], kind[1], kind[2]), kind[0], kind[1]).astype(np.float32)
+        same(w4.lsh_w4_unpack(cfg, w4.lsh_w4_quantize(cfg, w.to(gpu))), ref.astype(np.float64))
+
+
+def test_packed_past_32_bits(gpu):
+    """5.4 GB of codes: offsets of tiles, scales and zero points past 2^32, in every pass that takes them."""
+    N, K = 82_000 + 3, 1 << 17
+    for kind in (TYPES[1], TYPES[6]):
+        cfg = config(N, K, kind)
+        g = torch.Generator(device=gpu).manual_seed(3)
+        draw = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, dtype=torch.uint8, device=gpu)
+        codes = draw(0, 256, N, K // 2)
+        e = draw(126, 129, N, K // 32)
+        scales = e if kind[0] == "e2m1" else (e.short() << 7).view(torch.bfloat16)
+        zps = draw(0, 16, N, K // 32) if kind[2] else None
+        log("w4 past 32 bits", kind, w4.weight_bytes(cfg))
+        packed = w4.lsh_w4_pack(cfg, codes, scales, zps)
+        some = [0, 1, 15, 16, 20_000, 32_767, 32_768, 40_000, 65_535, 65_536, 70_001, N - 19, N - 18, N - 3, N - 1]
+        part = codes[some].cpu().numpy()
+        c = np.stack([part & 15, part >> 4], -1).reshape(len(some), K)
+        z = None if zps is None else zps[some].cpu().numpy()
+        s = scales[some].cpu()
+        s = s.numpy() if kind[0] == "e2m1" else s.view(torch.int16).numpy().view(np.uint16)
+        value = W.values(c, s, z, kind[0], kind[1])
+        a = torch.randint(-1, 2, (200, K), generator=g, device=gpu).bfloat16()  # sums of quarters below 2^22: exact
+        y = a.double().cpu().numpy() @ value.T
+        for M in (1, 20, 200):
+            same(w4.lsh_linear_w4(cfg, a[:M].contiguous(), packed)[:, some], y[:M])
+        del codes, scales, e, zps, s, z
+        w = w4.lsh_w4_unpack(cfg, packed, torch.bfloat16)
+        same(w[some], value)
+        w4.lsh_w4_quantize(cfg, w, packed)
+        few = [0, 65_536, N - 1]
+        ref = W.values(*W.quantize(w[few].double().cpu().numpy(), kind[0], kind[1], kind[2]), kind[0], kind[1])
+        w = w4.lsh_w4_unpack(cfg, packed, torch.bfloat16, w)
+        same(w[few], torch.from_numpy(ref).bfloat16().double().numpy())
+        del packed, w
+
+
 @pytest.mark.parametrize("M", [1, 20, 70, 300])
 @pytest.mark.parametrize("kind", [TYPES[1], TYPES[4], TYPES[6]], ids=[IDS[1], IDS[4], IDS[6]])
 def test_linear_outputs(gpu, kind, M):
