@@ -16,6 +16,22 @@ struct ResidualGrads {
     float *dx, *df, *dgate;
     float* cols[5];  // dscale, dpost_g, dpost_b, dpre_g, dpre_b; null: not wanted
 };
+// Waves of a row, at 512 columns a wave.
+inline int residual_waves(int D) {
+    int w = 1;
+    while (512 * w < D) w *= 2;
+    return w;
+}
+// Workgroups (of four waves, or of those of a row) that the chip's 256 CUs hold at
+// once: those that fit a CU whole, by the waves that a SIMD holds with each kernel's
+// registers.  BwdPlain: neither scale nor biases.
+enum ResidualPass { kResidualFwd, kResidualBwd, kResidualBwdPlain };
+inline int residual_resident(ResidualPass pass, int D) {
+    const int waves = residual_waves(D);
+    const int simd = pass == kResidualFwd ? (waves == 1 ? 5 : 4) : pass == kResidualBwdPlain || waves == 16 ? 4 : 3;
+    return 256 * (4 * simd / (waves > 4 ? waves : 4));
+}
+
 bool residual_fits(const ResidualArgs& a);
 size_t residual_workspace_bytes(const ResidualArgs& a);
 hipError_t launch_residual_fwd(const ResidualArgs& a, bool f32, const float* x, const void* f, const void* gate,

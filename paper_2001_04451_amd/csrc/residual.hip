@@ -306,26 +306,19 @@ __global__ __launch_bounds__(kRuns* kRunCols) void residual_cols_kernel(const fl
     if (s == 0 && c < D) to[c] = (float)run[0][d];
 }
 
-int waves_of(int D) {
-    int w = 1;
-    while (512 * w < D) w *= 2;
-    return w;
+int rows_of(int D) { return std::max(1, 4 / residual_waves(D)); }
+// Workgroups: as many as are resident at once, at most, so that no second round of a
+// few of them follows.  65,536 rows of 256 forward 51 us (60 with 2048 workgroups in
+// place of 1280), of 1024 184 (187 with 2048 in place of 1024, 233 with 1280), 8192
+// rows of 4096 with all weights backward 196 (245 with 384 in place of 256).
+int64_t groups(const ResidualArgs& a, ResidualPass pass) {
+    return std::min<int64_t>((a.T + rows_of(a.D) - 1) / rows_of(a.D), residual_resident(pass, a.D));
 }
-int rows_of(int D) { return std::max(1, 4 / waves_of(D)); }
-// Workgroups: as many as are resident at once, at most.
-int64_t groups(const ResidualArgs& a, int waves_cu) {
-    return std::min<int64_t>((a.T + rows_of(a.D) - 1) / rows_of(a.D), std::max(256, 256 * waves_cu / std::max(4, waves_of(a.D))));
-}
-int64_t fwd_groups(const ResidualArgs& a) { return groups(a, 32); }
-// The backward's workgroups: of rows side by side, all resident at once (12 waves a
-// CU, 16 where neither scale nor biases take registers), so that no second round
-// of a few of them follows.
-int64_t bwd_groups(const ResidualArgs& a, bool plain) { return groups(a, plain || waves_of(a.D) == 16 ? 16 : 12); }
 bool is_plain(const ResidualArgs& a) { return !a.scale && !a.post_b && !a.pre_b; }
 
 template <typename Go>
 void by_width(int D, Go go) {
-    switch (waves_of(D)) {
+    switch (residual_waves(D)) {
         case 1: go(std::integral_constant<int, 1>{}); break;
         case 2: go(std::integral_constant<int, 2>{}); break;
         case 4: go(std::integral_constant<int, 4>{}); break;
@@ -339,14 +332,14 @@ void by_width(int D, Go go) {
 bool residual_fits(const ResidualArgs&) { return true; }  // the grids are bounded by the chip's size
 
 size_t residual_workspace_bytes(const ResidualArgs& a) {
-    return align256((size_t)bwd_groups(a, true) * 5 * a.D * sizeof(float));  // the more of both
+    return align256((size_t)groups(a, kResidualBwdPlain) * 5 * a.D * sizeof(float));  // the more of both
 }
 
 hipError_t launch_residual_fwd(const ResidualArgs& a, bool f32, const float* x, const void* f, const void* gate,
                                float* y, void* z, hipStream_t stream) {
     by_width(a.D, [&](auto w) {
         constexpr int W = decltype(w)::value;
-        const unsigned grid = (unsigned)fwd_groups(a);
+        const unsigned grid = (unsigned)groups(a, kResidualFwd);
         if (f32)
             residual_fwd_kernel<true, W><<<grid, kThreads<W>, 0, stream>>>(a, x, f, gate, y, z);
         else
@@ -360,7 +353,7 @@ hipError_t launch_residual_bwd(const ResidualArgs& a, bool f32, const float* y, 
                                hipStream_t stream) {
     float* const partial = static_cast<float*>(workspace);
     const bool plain = is_plain(a);
-    const unsigned grid = (unsigned)bwd_groups(a, plain);
+    const unsigned grid = (unsigned)groups(a, plain ? kResidualBwdPlain : kResidualBwd);
     by_width(a.D, [&](auto w) {
         constexpr int W = decltype(w)::value;
         auto go = [&](auto kernel) { kernel<<<grid, kThreads<W>, 0, stream>>>(a, y, f, gate, dy, dz, g, partial); };
