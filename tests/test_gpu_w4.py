@@ -222,6 +222,25 @@ def test_quantize_at_the_end_of_fp32(gpu):
         same(w4.lsh_w4_unpack(cfg, w4.lsh_w4_quantize(cfg, w.to(gpu))), ref.astype(np.float64))
 
 
+@pytest.mark.parametrize("kind", [TYPES[1], TYPES[4], TYPES[6]], ids=[IDS[1], IDS[4], IDS[6]])
+def test_more_rows_of_tiles_than_a_grid_dimension(gpu, kind):
+    """524,325 outputs: laid out, read back, quantised and multiplied past 32,768 tiles of them."""
+    N, K, cut = 32_768 * 16 + 37, 96, 16_384 * 16
+    log("w4 many tiles", kind)
+    c = Exact(20, N, K, kind, seed=7)
+    a, packed = c.args(gpu)
+    with np.errstate(over="ignore", invalid="ignore"):
+        same(w4.lsh_w4_unpack(c.cfg, packed), W.values(c.codes, c.scales, c.zps, kind[0], kind[1]))
+    y = c.ref(bias=False)
+    for M in (1, 20):
+        same(w4.lsh_linear_w4(c.cfg, a[:M].contiguous(), packed), y[:M])
+    w = torch.randn(N, K, generator=torch.Generator(device=gpu).manual_seed(1), device=gpu)
+    whole = w4.lsh_w4_unpack(c.cfg, w4.lsh_w4_quantize(c.cfg, w))
+    for part in (slice(0, cut), slice(cut, 2 * cut), slice(2 * cut, N)):
+        cfg = config(len(range(N)[part]), K, kind)
+        assert torch.equal(whole[part], w4.lsh_w4_unpack(cfg, w4.lsh_w4_quantize(cfg, w[part].contiguous())))
+
+
 def test_packed_past_32_bits(gpu):
     """5.4 GB of codes: offsets of tiles, scales and zero points past 2^32, in every pass that takes them."""
     N, K = 82_000 + 3, 1 << 17
