@@ -26,8 +26,8 @@ int check_w4(const lsh_w4_config* c, lsh::W4Shape* s) {
     if (e2m1 && c->zeros) return LSH_ERR_INVALID;
     if (c->K % 32 != 0 || c->K > 1 << 17 || c->N > 1 << 22) return LSH_ERR_UNSUPPORTED;
     *s = {c->N, c->K, e2m1, c->group, c->zeros != 0, ((int64_t)c->N + 15) / 16, ((int64_t)c->K + 127) / 128};
-    // one workgroup a tile to quantise, pack and unpack
-    return s->tiles_n * s->tiles_k <= lsh::kMaxWorkgroups ? LSH_OK : LSH_ERR_UNSUPPORTED;
+    // then scales and zero points lie within 32-bit offsets
+    return (int64_t)c->N * c->K < (int64_t)1 << 35 ? LSH_OK : LSH_ERR_UNSUPPORTED;
 }
 
 int check_rows(const lsh::W4Shape& s, int64_t M) {

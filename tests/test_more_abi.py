@@ -112,6 +112,15 @@ def test_w4_rows_up_to_their_limit_taken(built, N):
     assert most <= 1 << 21 and status(most) == INVALID and status(most + 1) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("N,K,taken", [(1 << 22, 8160, True), ((1 << 18) + 1, (1 << 17) - 32, True), (1 << 22, 8192, False),
+                                       (1 << 18, 1 << 17, False), ((1 << 18) - 1, 1 << 17, True)])
+def test_w4_matrices_up_to_their_limit_taken(built, N, K, taken):
+    """N K < 2^35, whatever the rest of the last tiles."""
+    assert (N * K < 1 << 35) == taken
+    for kind in (dict(group=32, zeros=True), dict(type="e2m1", group=32)):
+        assert (w4.weight_bytes(_w4(N=N, K=K, **kind)) > N * K // 2) == taken
+
+
 def test_sizes_past_32_bits_refused(built):
     """The C structures hold 32 bits: 2^32 + 64 would pass as 64."""
     for bad in (dict(N=(1 << 32) + 64), dict(K=(1 << 32) + 64), dict(group=(1 << 32) + 32), dict(N=-1)):
