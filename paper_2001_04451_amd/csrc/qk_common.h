@@ -19,14 +19,16 @@ struct Angles {
 __device__ __forceinline__ double revolutions(float freq) { return (double)freq * 0.15915494309189535; }
 
 // The angle of pair p of token t, reduced in fp64 so that only the fraction of a
-// revolution reaches fp32.
+// revolution reaches fp32.  Its rounding there, up to 2^-25 half turns, would turn by
+// more than the roundings of sine and cosine: what it leaves turns them on.
 __device__ __forceinline__ void form_angle(Angles& A, int t, int p, double pos, double f) {
     double rev = pos * f;
-    rev -= rint(rev);
+    rev = 2.0 * (rev - rint(rev));
+    const float half = (float)rev, rest = (float)(rev - (double)half) * 3.14159265f;
     float s, c;
-    sincospif((float)(2.0 * rev), &s, &c);
-    A.c[t][p] = c;
-    A.s[t][p] = s;
+    sincospif(half, &s, &c);
+    A.c[t][p] = fmaf(-s, rest, c);
+    A.s[t][p] = fmaf(c, rest, s);
 }
 
 // A lane's eight dimensions (8 l ..) turned by the angles of token t (by their

@@ -218,3 +218,26 @@ def test_binding_refusals(gpu):
         qk.lsh_qk_norm_rotate_fwd(c.cfg, x, gq, gk, freq[:8])
     with pytest.raises(ValueError, match="dk is required"):
         qk.lsh_qk_norm_rotate_bwd(c.cfg, x, gq, gk, freq, None, torch.zeros(6, 2, 64, device=gpu))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_are_as_exact_as_fp32_holds_them(gpu, interleaved):
+    """Sines and cosines of far positions, read off rows with one value of 8 (mean square 1, so the norm leaves them as they
+    are).  Each is rounded twice, by sine or cosine and by the turn through what the fp32 fraction leaves: 2^-24 / sqrt(12)
+    each in the root of the mean square, below 2^-25 together.  The fraction's own rounding would add pi 2^-25 / sqrt(3) in
+    half of the angles."""
+    T, H = 4096, 32
+    cfg = qk.QkConfig(T=T, L=0, Hq=H, Hk=0, rot=64, interleaved=interleaved, eps=0.0)
+    x = torch.zeros(T, H, 64)
+    first = 2 * torch.arange(H) if interleaved else torch.arange(H)
+    x[:, torch.arange(H), first] = 8.0
+    freq = (1.0 + torch.arange(H)).float().sqrt()
+    pos = torch.randint(-(1 << 20), 1 << 20, (T,), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    log("qk angles", interleaved)
+    q, _ = qk.lsh_qk_norm_rotate_fwd(cfg, x.view(T, H * 64).to(gpu), torch.ones(64, device=gpu), None, freq.to(gpu), pos.to(gpu))
+    q = q.view(T, H, 64).double().cpu() / 8
+    angle = pos.double()[:, None] * freq.double()
+    second = first + 1 if interleaved else first + 32
+    err = torch.stack([q[:, torch.arange(H), first] - angle.cos(), q[:, torch.arange(H), second] - angle.sin()])
+    assert err.square().mean().sqrt() <= 2.0 ** -25
+    assert err.abs().max() <= 2.0 ** -23  # and the worst of them: two roundings of a step each at most
