@@ -96,7 +96,7 @@ __device__ __forceinline__ void write_row(const CacheArgs& a, int64_t slot, bool
         if (slot >= 0 && (l & 3) == 0) (value ? a.v_scale : a.k_scale)[2 * slot + (l >> 2)] = (uint8_t)byte;
         if (a.shared && !value) widen8<TYPE>(w0, w1, x);
     }
-    if (!a.shared || value) return;  // the same for the whole wave
+    if (!a.shared || value) return;  // the same for the eight lanes of a row; what follows stays within them
     // 1 / length of the stored row, its values brought near one by the larger
     // block's exponent: neither their squares nor their sum leave fp32's range.
     const int top = group8_max_int(exp);
@@ -199,8 +199,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a, void* __re
 // out, keys and values into the cache.  A workgroup takes up to sixteen
 // consecutive tokens: finds their slots once, forms the angles of their positions
 // once (as the per-head norm does), and walks over their rows with the tokens
-// innermost, so that a wave's eight rows are of one head and leave as a run of a
-// page.  Keys go from fp32 to their codes in one rounding.
+// innermost, so that with eight tokens or more a wave's eight rows are of one head
+// and leave as a run of a page.  Keys go from fp32 to their codes in one rounding.
 // HBM-bound in long calls (9095 fp32 tokens of 16 + 4 + 4 heads into e2m1, 77 MB,
 // 16.5 us, 4.7 TB/s; 16K bf16 tokens of the same heads into bf16 24), short ones by
 // the chain first -> length -> table and the angles behind it (64 tokens 4.9 us, one
