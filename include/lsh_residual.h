@@ -93,7 +93,8 @@ int lsh_residual_norm_fwd(const lsh_residual_config *cfg, lsh_dtype dtype, const
  * repeat bit for bit.
  *   dy     NULL for 0 (with cfg->pre)
  *   grads  dx always, the others exactly where their input or weight is there
- *   workspace >= lsh_residual_workspace_bytes(cfg); its contents are free */
+ *   workspace >= lsh_residual_workspace_bytes(cfg); its contents are free, and
+ *   calls that may overlap need one each */
 int lsh_residual_norm_bwd(const lsh_residual_config *cfg, lsh_dtype dtype, const float *y, const void *f,
                           const void *gate, const lsh_residual_weights *w, const float *dy, const float *dz,
                           const lsh_residual_grads *grads, void *workspace, size_t workspace_bytes, void *stream);

@@ -34,8 +34,8 @@ struct W4Shape {
 // 16 bytes a lane.  `after` rows follow the tile's first.  Rows past the last
 // one repeat it, and pieces past the end of a row its first piece of the tile (neither
 // is used), so that every byte read is a byte of the matrix and nothing rests on how a
-// buffer's bound counts a scalar offset (1% of a long call's time in place of offsets
-// in scalar registers: 2048 x 4096 x 1024 25.5 -> 25.7 us).
+// buffer's bound counts a scalar offset (1% of a long call's time: 2048 x 4096 x 1024
+// with the offsets in scalar registers 25.5 us, so 25.7).
 template <int TM, int COPIES>
 struct W4RowCopies {
     uint32_t at[COPIES], col;

@@ -5,11 +5,10 @@
 // 16 waves and each value is read once, in 16-byte pieces; mean and deviation
 // are taken in two steps from registers.  A workgroup walks over rows and keeps
 // its threads' weights, and in the backward their columns' sums, in registers.
-// HBM-bound: 65,536 rows of 1024 (bf16, gate, both norms) forward 186-194 us (0.94
-// GB, 4.9 TB/s), backward 357 (1.88 GB, 5.3; 429 with 162 registers and workgroups
-// that came in two rounds); 5997 fp32 rows of 1000 with all weights 25 and 41 (4.8
-// and 4.7 TB/s).  16 rows of 4096 4.4 us: the launch, one trip to memory and two
-// barriers.
+// HBM-bound: 65,536 rows of 1024 (bf16, gate, both norms) forward 182 us (0.94 GB,
+// 5.2 TB/s), backward 357 (1.88 GB, 5.3; 429 with 162 registers and workgroups that
+// came in two rounds); 5997 fp32 rows of 1000 with all weights 25 and 41 (4.8 and 4.7
+// TB/s).  16 rows of 4096 4.4 us: the launch, one trip to memory and two barriers.
 #include "common.h"
 #include "launch_residual.h"
 
@@ -192,7 +191,9 @@ __device__ __forceinline__ void norm_back(const ResidualArgs& a, RowSums<WAVES, 
 }
 
 // partial: [workgroup][5][D].  PLAIN: neither scale nor biases, whose sums and
-// weights then take no registers: four waves a SIMD in place of three.
+// weights then take no registers: four waves a SIMD in place of three.  Sixteen waves
+// a row leave 128 registers, so that with scale or biases 51 (fp32) or 43 of them go
+// through scratch: 4096 bf16 rows of 8192 207 us, PLAIN 150, at much the same bytes.
 template <bool F32, bool PLAIN, int WAVES>
 __global__ __launch_bounds__(kThreads<WAVES>, PLAIN || WAVES == 16 ? 4 : 3) void residual_bwd_kernel(
     ResidualArgs a, const float* __restrict__ y, const void* __restrict__ f, const void* __restrict__ gate,
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(kRuns* kRunCols) void residual_cols_kernel(const fl
 int rows_of(int D) { return std::max(1, 4 / residual_waves(D)); }
 // Workgroups: as many as are resident at once, at most, so that no second round of a
 // few of them follows.  65,536 rows of 256 forward 51 us (60 with 2048 workgroups in
-// place of 1280), of 1024 184 (187 with 2048 in place of 1024, 233 with 1280), 8192
+// place of 1280), of 1024 181 to 184 (2048 in place of 1024 the same, 1280 233), 8192
 // rows of 4096 with all weights backward 196 (245 with 384 in place of 256).
 int64_t groups(const ResidualArgs& a, ResidualPass pass) {
     return std::min<int64_t>((a.T + rows_of(a.D) - 1) / rows_of(a.D), residual_resident(pass, a.D));

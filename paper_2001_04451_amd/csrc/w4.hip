@@ -178,8 +178,8 @@ __device__ __forceinline__ void put_pair(const W4Args& g, int64_t m, int n, int 
 // tiles of 128 inputs in turn, the codes of AHEAD of them on their way, and add
 // up in LDS.  Where the rows are short (STAGED) they pass through LDS once, while
 // the first codes are on their way; else a wave loads them tile by tile.
-// HBM-bound where the matrix is large: one row by 16384 x 16384 26 us (5.3 TB/s in
-// int4, 5.5 in e2m1), by 32000 x 4096 17 and 16; by 4096 x 1024 3.1, of which the
+// HBM-bound where the matrix is large: one row by 16384 x 16384 26 us in int4 (5.2
+// TB/s), 24 in e2m1 (5.9), by 32000 x 4096 16 and 15; by 4096 x 1024 3.0, of which the
 // launch is 2.5.
 constexpr size_t kStaged = 34 * 1024;  // bytes of rows, at most
 __host__ __device__ constexpr int64_t staged_stride(int K) { return K + 32; }  // rows start 16 banks apart
@@ -327,8 +327,8 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args g) {
 // 128 inputs, copied there by buffer loads that the kernel counts by hand; codes
 // are widened in the registers of the waves that use them.  A call with few tiles
 // splits its inputs over workgroups, whose sums a second kernel joins in order.
-// 2048 x 4096 x 4096: int4 71 us (0.97 PFLOP/s), e2m1 56 (1.22; a bf16 product of
-// 8192^3 by the library reaches 1.39); 2048 x 4096 x 1024 25 and 20.  Bound by the
+// 2048 x 4096 x 4096: int4 70 us (0.98 PFLOP/s), e2m1 56 (1.23; a bf16 product of
+// 8192^3 by the library reaches 1.39); 2048 x 4096 x 1024 23 and 19.  Bound by the
 // copies (8.8 TB/s out of L2, a workgroup a CU) with the first stages' and the
 // epilogue's latency; int4 issues a quarter more products for the sums of rows.
 constexpr int kMostSplits = 8;
@@ -851,26 +851,33 @@ namespace {
 //   Up to 16 rows: the rows kernel, 16 outputs a workgroup, from 512 tiles of
 //   outputs on 32 and from 1024 on 64: reading the rows once a workgroup is what
 //   bounds wider calls (L2 gives all CUs together 8.8 TB/s).  16 x 4096 x 4096 (16
-//   outputs / 32 / 64) 7.5 / 7.5 / 8.5, 16 x 8192 x 4096 11.5 / 8.1 / 8.8, 16 x
-//   16384 x 4096 19.8 / 13.0 / 9.9, 1 x 8192 x 4096 6.9 / 6.6 / 7.9, 1 x 32000 x
-//   4096 22.0 / 19.1 / 17.4.
-//   Up to 32 rows the same (32 x 16384 x 4096 34 / 20 / 13.5), but with groups of
-//   32, whose scales leave no registers for 64 outputs (24 / 83 at 32 / 64).
-//   Up to 64 rows the same where there is little to split (64 x 4096 x 1024 6.6
-//   against the wide kernel's 7.2; 64 x 4096 x 4096 18.2 against 13.5).
+//   outputs / 32 / 64) 7.4 / 7.5 / 8.6, 16 x 8192 x 4096 11.6 / 8.1 / 8.8, 16 x
+//   16384 x 4096 19.5 / 12.7 / 9.7, 1 x 8192 x 4096 6.8 / 6.3 / 7.7, 1 x 32000 x
+//   4096 22.5 / 17.6 / 16.0.
+//   Up to 32 rows the same (32 x 16384 x 4096 33 / 20 / 13.6), but with groups of
+//   32, whose scales leave no registers for 64 outputs (23 / 40 at 32 / 64, with
+//   zero points 23 / 88).
+//   Up to 64 rows the same where there is little to split: 64 x 4096 x 1024 6.6
+//   against the wide kernel's 6.8 (e2m1 6.5 and 5.8, groups of 32 with zero points
+//   6.9 and 8.7), 40 rows of it 5.5 and 6.8 (5.6 and 5.8, 5.9 and 8.7), but 64 x 4096
+//   x 4096 18.1 and 14.3.
 //   Beyond: the wide kernel, in the largest tiles that make a workgroup for every
-//   CU (and are not mostly past N): 2048 x 4096 x 1024 in tiles of 128 x 256 28.1,
-//   64 x 128 30.5, 64 x 64 38; 1024 x 4096 x 1024 26 / 17.5 / 21.  With fewer tiles
-//   of 64 x 64 than that, long sums are split until there are 512 workgroups (128 x
-//   4096 x 4096 unsplit 24, in four 17.4; 512 x 1024 x 4096 20 / 17.3); short ones
-//   take tiles of 32 x 64 (128 x 4096 x 1024 8.9 / 7.3, split in two 10.0).  (All of
-//   the wide kernel's since 5-15% faster, its tail apart from its loop.)
+//   CU (and are not mostly past N): 2048 x 4096 x 1024 in tiles of 128 x 256 23.2,
+//   64 x 128 28.5, 64 x 64 35; 1024 x 4096 x 1024 20.8 / 16.3 / 18.9.  With fewer
+//   tiles of 64 x 64 than that, long sums are split until there are 512 workgroups
+//   (128 x 4096 x 4096 unsplit 24.0, in four 17.4; 512 x 1024 x 4096 24.1 / 17.1);
+//   short ones take tiles of 32 x 64 (128 x 4096 x 1024 8.1 / 7.0, split in two 9.8).
 //   From 8192 inputs on the largest tiles are split into up to four where that makes
-//   192 to 256 workgroups of them: 512 x 8192 x 8192 101 -> 86 (e2m1 68 -> 65), 1000 x
-//   2048 x 8192 61 -> 47 (44 -> 40), 800 x 2048 x 16384 109 -> 76 (80 -> 61); with 288
-//   workgroups 300 x 8192 x 8192 88 -> 97, with 4096 inputs 512 x 4096 32 -> 34, half
-//   empty 64 x 16384 x 8192 37 -> 44; unsplit 1500 x 4096 x 8192 140 -> 130, but in
-//   groups of 32 with zero points 210 -> 237.
+//   192 to 256 workgroups of them: 512 x 8192 x 8192 93 -> 80 (e2m1 68 -> 65), 1000 x
+//   2048 x 8192 61 -> 47 (44 -> 40), 800 x 2048 x 16384 110 -> 77 (80 -> 62); with 288
+//   workgroups 300 x 8192 x 8192 89 -> 100, with 4096 inputs 512 x 4096 32 -> 34, half
+//   empty 64 x 16384 x 8192 37 -> 45; unsplit 1500 x 4096 x 8192 145 -> 131, but in
+//   groups of 32 with zero points 210 -> 241.
+//   What the rule does not look at: how far the largest tiles' last round fills the
+//   chip (257 to 511 of them take as long as 512) and how much of them lies past M.
+//   There it is behind tiles of 64 x 128: 2048 x 5120 x 5120 164 and 155, 2048 x 4112
+//   x 4096 132 and 116, 1024 x 9216 x 4096 132 and 115, 520 x 16384 x 4096 132 and
+//   112, 64 x 131072 x 4096 141 and 103 (e2m1 116 and 79).
 enum Kernel { kRows, kWide32x64, kWide64x64, kWide64x128, kWide128x256 };
 struct Plan {
     Kernel kernel;
@@ -893,8 +900,8 @@ Plan plan_of(const W4Shape& s, int64_t M) {
 
 // Whether the rows kernel stages its rows: long ones that fit, where a wave goes
 // round often enough (1 x 16384 x 16384 26 us; tile by tile, 16, 32 or 64 outputs a
-// workgroup, 36 / 28 / 30; 1 x 4096 x 16384 10.4 and 12.2, but 16 x 4096 x 1024 4.1
-// and 3.6, 4 x 4096 x 4096 6.0 and 5.5).
+// workgroup, 34 / 27 / 28; 1 x 4096 x 16384 10.1 and 11.2, but 16 x 4096 x 1024 4.1
+// and 3.7, 4 x 4096 x 4096 6.0 and 5.5).
 bool stages_rows(const W4Shape& s, int64_t M) {
     return s.tiles_k >= 96 && (size_t)M * staged_stride(s.K) * 2 <= kStaged;
 }
